@@ -250,12 +250,192 @@ int massive_set_timing(massive_ctx* ctx, int groups);
  * Synchronises the context's streams. */
 int massive_get_timing(massive_ctx* ctx, double* out_ms, int64_t* out_calls);
 
+/* ------------------------------------------------------------------------
+ * Operators of a training step on what massive_sample gathers: rows held in
+ * few bits, the mean over a sampled block, a layer's product and the step on
+ * the weights, with their gradients.
+ *
+ * They take no context. Every call checks its arguments on the host, enqueues
+ * its kernels on `stream` and returns without waiting; it allocates nothing
+ * and keeps nothing. Pointers are device memory of the current device unless
+ * said otherwise, and a table of packed rows may also be pinned host memory.
+ * What a call reads and writes must not overlap, except where an argument is
+ * documented as updated in place. Arrays hold 32-bit or bf16 values
+ * (MASSIVE_F32, MASSIVE_BF16) at their natural alignment; strides are in
+ * elements. Sums, products' accumulators and statistics are fp32; a result is
+ * rounded once, to nearest even, where it is stored. Results do not depend on
+ * the order in which the device runs a call's blocks: the same call on the
+ * same inputs gives the same bits. An empty extent (no rows, no tensors) is
+ * MASSIVE_OK and does nothing. On failure the message is in
+ * massive_last_error(NULL).
+ */
+#define MASSIVE_F32 0
+#define MASSIVE_BF16 1
+#define MASSIVE_PACKED 2 /* rows of massive_row_format (massive_block_mean) */
+
+/* Rows of d values held in 8 or 4 bits. The columns form groups of `group`
+ * (a power of two from 16 to 512; 0 for one group of the whole row, which is
+ * also what a group of d columns or more is); the last may be short. A row is
+ * its codes, padded with zeros to four bytes, then each group's floats:
+ *   8 bits: int8 codes c in [-127, 127] and step = max|x| / 127; stands for
+ *     c * step;
+ *   4 bits: codes c in [0, 15], even columns in the low nibbles, and the
+ *     group's least value lo and step = (max - lo) / 15; stands for
+ *     lo + c * step.
+ * c is the nearest code, ties to the even one. A group whose max|x| (8 bits)
+ * or max - lo (4 bits) is under 2^-119 has step 0. A group that holds a value
+ * that is not finite, or whose max - lo is not, has a step of NaN: all of it
+ * reads as NaN. Rows are a multiple of four bytes, so massive_init takes them
+ * as feature rows. */
+typedef struct {
+  int32_t d;         /* values per row, 1..1048576                              */
+  int32_t bits;      /* 8 or 4                                                  */
+  int32_t group;     /* columns per group, or 0                                 */
+  int32_t reserved;  /* 0                                                       */
+  int64_t row_bytes; /* bytes from row to row: 0 for the least, or a multiple of
+                        four that is at least that                              */
+} massive_row_format;
+
+/* Checks a format and writes its least row size, and the offset of the first
+ * group's floats in a row (each pointer may be NULL). */
+int massive_row_layout(const massive_row_format* fmt, int64_t* row_bytes, int64_t* floats_at);
+
+/* Writes n rows to a table of table_rows rows: row i of src (row i starting at
+ * src + i * src_stride) to row slots[i], or to row i if slots is NULL. A slot
+ * outside [0, table_rows) is left out. The others must be distinct: a row that
+ * two sources share holds neither. Padding bytes between rows are not
+ * written. */
+int massive_pack_rows(const massive_row_format* fmt, const void* src, int32_t src_type, int64_t src_stride, int64_t n,
+                      const int32_t* slots, void* table, int64_t table_rows, void* stream);
+
+/* Reads n rows of a table: row index[i], or row i if index is NULL, to row i
+ * of out. An index outside [0, table_rows) reads as a row of zeros. */
+int massive_unpack_rows(const massive_row_format* fmt, const void* table, int64_t table_rows, const int32_t* index,
+                        int64_t n, void* out, int32_t out_type, int64_t out_stride, void* stream);
+
+/* One sampled block (a hop of massive_batch) or any CSR of its kind: row i of
+ * n lists indices[indptr[i] .. indptr[i+1]), source rows in [0, rows); edges
+ * is the room in indices, and offsets beyond it are cut to it. An index
+ * outside [0, rows) stands for a row of zeros (it counts in the mean). */
+typedef struct {
+  const int32_t* indptr;  /* [n + 1] */
+  const int32_t* indices; /* [edges] */
+  int64_t n, edges, rows;
+} massive_block;
+
+/* out[i] = mean of x[j] over row i's list, d columns; zeros for an empty list.
+ * x_type MASSIVE_PACKED: x holds rows of fmt (fmt->d = d; x_stride ignored),
+ * otherwise fmt is NULL. */
+int massive_block_mean(const massive_block* block, const void* x, int32_t x_type, int64_t x_stride,
+                       const massive_row_format* fmt, int32_t d, void* out, int32_t out_type, int64_t out_stride,
+                       void* stream);
+
+/* Bytes of workspace of massive_block_mean_backward. */
+int massive_block_mean_workspace(const massive_block* block, int64_t* bytes);
+
+/* The gradient: dx[j] = sum over the entries of j, in the order of the rows
+ * that list it, of dout[i] / (length of row i); plus add[j] for j < add_rows
+ * (the gradient that the block's own rows, the first of its sources, get from
+ * elsewhere; add may be NULL). All arrays have one type; dx is [rows, d].
+ * workspace: massive_block_mean_workspace's bytes, 16-byte aligned. */
+int massive_block_mean_backward(const massive_block* block, const void* dout, int32_t type, int64_t dout_stride,
+                                int32_t d, const void* add, int64_t add_stride, int64_t add_rows, void* dx,
+                                int64_t dx_stride, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Activations of massive_linear: the identity, max(z, 0), z * Phi(z) with the
+ * normal distribution's Phi, z / (1 + exp(-z)) */
+#define MASSIVE_ACT_NONE 0
+#define MASSIVE_ACT_RELU 1
+#define MASSIVE_ACT_GELU 2
+#define MASSIVE_ACT_SILU 3
+
+/* A layer: z = [x | x2] w^T + bias, y = act(z) + residual, over `rows` rows.
+ * x2 (k2 columns; NULL and 0 for none), bias and residual are optional, and
+ * so is pre, which receives z for the backward pass. All arrays have one
+ * type. A pointer may not be both read and written. */
+typedef struct {
+  const void* x;        /* [rows, k]                                          */
+  const void* x_second; /* [rows, k_second] or NULL                           */
+  const void* w;        /* [n, k + k_second], each output's weights in a row  */
+  const void* bias;     /* [n] or NULL                                        */
+  const void* residual; /* [rows, n] or NULL                                  */
+  void* y;              /* [rows, n]                                          */
+  void* pre;            /* [rows, n] or NULL                                  */
+  int64_t rows;
+  int64_t x_stride, x_second_stride, w_stride, residual_stride, y_stride, pre_stride;
+  int32_t n, k, k_second;
+  int32_t type, act;
+} massive_linear_args;
+
+int massive_linear(const massive_linear_args* args, void* stream);
+
+/* The layer's gradients: dz = dy * act'(pre), dx = dz w (columns of x and x2
+ * apart), dw = dz^T [x | x2], dbias = sum of dz over the rows. dx, dx_second,
+ * dw and dbias may each be NULL; the residual's gradient is dy. pre is z as
+ * massive_linear wrote it (for relu, y without a residual serves as well), and
+ * NULL for MASSIVE_ACT_NONE. */
+typedef struct {
+  const void *dy, *pre, *x, *x_second, *w;
+  void *dx, *dx_second, *dw, *dbias;
+  int64_t rows;
+  int64_t dy_stride, pre_stride, x_stride, x_second_stride, w_stride, dx_stride, dx_second_stride, dw_stride;
+  int32_t n, k, k_second;
+  int32_t type, act;
+} massive_linear_grads;
+
+/* Bytes of workspace of massive_linear_backward (0 if neither dw nor dbias is
+ * asked for). */
+int massive_linear_workspace(const massive_linear_grads* args, int64_t* bytes);
+int massive_linear_backward(const massive_linear_grads* args, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* One tensor of an AdamW step, n values. Everything but grad is updated in
+ * place. With state_bits 32, m and v are float[n] and the scales are NULL.
+ * With state_bits 8, m is int8[n] and v uint8[n], and each 256 values share a
+ * scale, m_scale and v_scale being float[ceil(n / 256)]:
+ *   m = c |c| s with c = round(sqrt(|m| / s)) and the sign of m, s = max|m| / 127^2;
+ *   v = c^4 s with c = round((v / s)^(1/4)), at least 1 where v > 0,
+ *   s = max v / 255^4.
+ * A block whose max|m| is under 2^-112 (max v under 2^-94) holds zeros, and
+ * one that holds a value that is not finite reads as NaN. States start as
+ * zeros. copy, if not NULL, receives the new values as bf16. */
+typedef struct {
+  void* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;
+  int64_t n;
+} massive_adamw_tensor;
+
+typedef struct {
+  double lr, beta_first, beta_second, eps, weight_decay;
+  int64_t t;          /* the step's number, from 1 */
+  int32_t state_bits; /* 32 or 8 */
+  int32_t param_type, grad_type;
+  int32_t reserved;   /* 0 */
+} massive_adamw_args;
+
+/* A step on all tensors of a host array:
+ *   p *= 1 - lr * weight_decay
+ *   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
+ *   p -= lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+ * with the new m and v in 32 bits, before they are held in 8. The array is
+ * read during the call only. */
+int massive_adamw(const massive_adamw_tensor* tensors, int64_t count, const massive_adamw_args* args, void* stream);
+
+/* What 8-bit states stand for, as floats: n codes of m and of v with their
+ * scales, to m_out and v_out. */
+int massive_adamw_states(const void* m, const void* v, const float* m_scale, const float* v_scale, int64_t n,
+                         float* m_out, float* v_out, void* stream);
+
 /* Frees every device and host resource of the context; NULL is a no-op.
  * Always MASSIVE_OK. */
 int massive_destroy(massive_ctx* ctx);
 
 /* Message of the last failure on this context (ctx == NULL: of the last
- * failed massive_init on this thread). Never NULL. */
+ * failed massive_init or operator call on this thread). Never NULL. */
 const char* massive_last_error(const massive_ctx* ctx);
 
 #ifdef __cplusplus

@@ -3,7 +3,7 @@ import os
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "massive.hip")
+SRCS = [os.path.join(HERE, "csrc", name) for name in ("massive.hip", "operators.hip")]
 LIB = os.path.join(HERE, "libmassive.so")
 ARCH = os.environ.get("MASSIVE_OFFLOAD_ARCH", "gfx950")
 
@@ -19,11 +19,27 @@ FLAGS = [
 
 def build(verbose: bool = False) -> str:
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = ["hipcc"] + FLAGS + [SRC, "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
-    os.replace(tmp, LIB)
+    # the sources compile side by side
+    objects = ["%s.%s.o" % (tmp, os.path.basename(src)) for src in SRCS]
+    compiles = [["hipcc"] + [f for f in FLAGS if f != "-shared"] + ["-c", src, "-o", o] for src, o in zip(SRCS, objects)]
+    link = ["hipcc", "-shared", "-fPIC", "--offload-arch=" + ARCH] + objects + ["-o", tmp]
+    try:
+        running = []
+        for cmd in compiles:
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            running.append(subprocess.Popen(cmd))
+        for cmd, status in zip(compiles, [p.wait() for p in running]):
+            if status:
+                raise subprocess.CalledProcessError(status, cmd)
+        if verbose:
+            print(" ".join(link), flush=True)
+        subprocess.check_call(link)
+        os.replace(tmp, LIB)
+    finally:
+        for f in objects + [tmp]:
+            if os.path.exists(f):
+                os.remove(f)
     return LIB
 
 

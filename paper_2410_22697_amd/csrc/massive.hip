@@ -33,6 +33,7 @@
 
 #include "../../include/massive.h"
 #include "buffer_kernels.hpp"
+#include "call_error.hpp"
 #include "common.hpp"
 #include "gather_pool.hpp"
 #include "launch_rules.hpp"
@@ -54,6 +55,20 @@ inline unsigned grid_for(int64_t n, int nt, int64_t cap = 16384) {
 }
 
 }  // namespace
+
+int ms::call_error(int code, const char* fmt, ...) noexcept {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  try {
+    g_init_error = buf;
+  } catch (const std::exception&) {  // no memory for the message: the code still says what failed
+    g_init_error.clear();
+  }
+  return code;
+}
 
 // ------------------------------------------------------------- no-alloc path
 // massive_sample_noalloc takes a step's per-step buffers (sizes, the two

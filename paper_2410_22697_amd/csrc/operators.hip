@@ -1,0 +1,617 @@
+// operators.hip - the C ABI's operators of a training step: packed rows, the
+// mean over a sampled block, a layer's product, the AdamW step. Argument checks
+// and launches; the kernels are in the headers included here. A call only
+// enqueues: it allocates nothing, waits for nothing and keeps nothing.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <tuple>
+#include <type_traits>
+
+#include "../../include/massive.h"
+#include "adamw_kernels.hpp"
+#include "block_kernels.hpp"
+#include "call_error.hpp"
+#include "linear_kernels.hpp"
+#include "rows_kernels.hpp"
+
+namespace {
+
+using ms::bf16;
+using ms::call_error;
+
+constexpr int64_t kMostBlocks = 1 << 23;  // of a launch: 256 threads each stay below 2^32 in all
+
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t round_up(int64_t a, int64_t b) { return cdiv(a, b) * b; }
+
+#define REFUSE(...) return call_error(MASSIVE_EINVAL, __VA_ARGS__)
+
+// Enqueues a kernel and returns its own status (an error that some earlier call
+// left behind is neither reported nor cleared).
+template <typename... P, typename... A>
+int launch(const char* what, void (*kernel)(P...), int64_t blocks, int threads, size_t lds, void* stream, A... args) {
+  std::tuple<P...> held(static_cast<P>(args)...);  // the arguments in the kernel's own types
+  const hipError_t e = std::apply(
+      [&](P&... a) {
+        void* ptrs[] = {(void*)&a...};
+        return hipLaunchKernel((const void*)kernel, dim3((unsigned)blocks), dim3((unsigned)threads), ptrs, lds, (hipStream_t)stream);
+      },
+      held);
+  return e == hipSuccess ? MASSIVE_OK : call_error(MASSIVE_EHIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+bool is_type(int32_t t) { return t == MASSIVE_F32 || t == MASSIVE_BF16; }
+int size_of(int32_t t) { return t == MASSIVE_F32 ? 4 : 2; }
+bool aligned(const void* p, int64_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+// -------------------------------------------------------------- packed rows
+int check_format(const massive_row_format* f, ms::PackedRows* out, int64_t* least) {
+  if (!f) REFUSE("the row format is NULL");
+  if (f->d < 1 || f->d > (1 << 20)) REFUSE("d must be in 1..1048576");
+  if (f->bits != 8 && f->bits != 4) REFUSE("bits must be 8 or 4");
+  if (f->group != 0 && (f->group < 16 || f->group > 512 || (f->group & (f->group - 1))))
+    REFUSE("group must be 0 or a power of two from 16 to 512");
+  if (f->reserved != 0) REFUSE("reserved must be 0");
+  const bool whole = f->group == 0 || f->group >= f->d;
+  const int64_t groups = whole ? 1 : cdiv(f->d, f->group);
+  out->d = f->d;
+  out->group_log2 = whole ? 31 : __builtin_ctz((unsigned)f->group);
+  out->floats_at = (int32_t)(4 * cdiv((int64_t)f->d * f->bits, 32));
+  *least = out->floats_at + 4 * groups * (f->bits == 8 ? 1 : 2);
+  out->row_bytes = f->row_bytes ? f->row_bytes : *least;
+  if (out->row_bytes < *least || out->row_bytes % 4)
+    REFUSE("row_bytes must be 0 or a multiple of 4 that is at least %lld", (long long)*least);
+  return MASSIVE_OK;
+}
+
+// Lanes that share a row of d columns, q a lane: the power of two that covers
+// it, at most a wave.
+int team_of(int64_t d, int q) {
+  int t = 1;
+  while (t < MS_WAVE && (int64_t)t * q < d) t *= 2;
+  return t;
+}
+
+template <typename F>
+int with_team(int team, F f) {
+  switch (team) {
+    case 1: return f(std::integral_constant<int, 1>());
+    case 2: return f(std::integral_constant<int, 2>());
+    case 4: return f(std::integral_constant<int, 4>());
+    case 8: return f(std::integral_constant<int, 8>());
+    case 16: return f(std::integral_constant<int, 16>());
+    case 32: return f(std::integral_constant<int, 32>());
+    default: return f(std::integral_constant<int, 64>());
+  }
+}
+template <typename F>
+int with_type(int32_t type, F f) {
+  return type == MASSIVE_F32 ? f((float*)nullptr) : f((bf16*)nullptr);
+}
+template <typename F>
+int with_bits(int bits, F f) {
+  return bits == 8 ? f(std::integral_constant<int, 8>()) : f(std::integral_constant<int, 4>());
+}
+
+int pack_rows(const massive_row_format* fmt, const void* src, int32_t src_type, int64_t src_stride, int64_t n,
+              const int32_t* slots, void* table, int64_t table_rows, void* stream) {
+  ms::PackedRows f;
+  int64_t least;
+  if (int rc = check_format(fmt, &f, &least)) return rc;
+  if (!is_type(src_type)) REFUSE("src_type must be MASSIVE_F32 or MASSIVE_BF16");
+  if (n < 0 || table_rows < 0) REFUSE("n and table_rows must not be negative");
+  if (n == 0 || table_rows == 0) return MASSIVE_OK;
+  if (!src || !table) REFUSE("src / table are NULL");
+  if (src_stride < f.d) REFUSE("src_stride is below d");
+  if (!aligned(src, size_of(src_type)) || !aligned(slots, 4) || !aligned(table, 4)) REFUSE("src, slots or table is not aligned");
+  const int team = team_of(f.d, ms::kRowsQ);
+  const int64_t blocks = std::min(cdiv(n, ms::kRowsNT / team), kMostBlocks);
+  return with_type(src_type, [&](auto* s) {
+    using S = std::remove_pointer_t<decltype(s)>;
+    return with_bits(fmt->bits, [&](auto bits) {
+      return with_team(team, [&](auto t) {
+        return launch("massive_pack_rows", ms::k_pack_rows<S, bits(), t()>, blocks, ms::kRowsNT, 0, stream, (const S*)src,
+                      src_stride, n, slots, (uint8_t*)table, table_rows, f);
+      });
+    });
+  });
+}
+
+int unpack_rows(const massive_row_format* fmt, const void* table, int64_t table_rows, const int32_t* index, int64_t n,
+                void* out, int32_t out_type, int64_t out_stride, void* stream) {
+  ms::PackedRows f;
+  int64_t least;
+  if (int rc = check_format(fmt, &f, &least)) return rc;
+  if (!is_type(out_type)) REFUSE("out_type must be MASSIVE_F32 or MASSIVE_BF16");
+  if (n < 0 || table_rows < 0) REFUSE("n and table_rows must not be negative");
+  if (n == 0) return MASSIVE_OK;
+  if (!out || (table_rows > 0 && !table)) REFUSE("table / out are NULL");
+  if (out_stride < f.d) REFUSE("out_stride is below d");
+  if (!aligned(out, size_of(out_type)) || !aligned(index, 4) || !aligned(table, 4)) REFUSE("table, index or out is not aligned");
+  const int team = team_of(f.d, ms::kRowsQ);
+  const int64_t blocks = std::min(cdiv(n, ms::kRowsNT / team), kMostBlocks);
+  return with_type(out_type, [&](auto* o) {
+    using O = std::remove_pointer_t<decltype(o)>;
+    return with_bits(fmt->bits, [&](auto bits) {
+      return with_team(team, [&](auto t) {
+        return launch("massive_unpack_rows", ms::k_unpack_rows<O, bits(), t()>, blocks, ms::kRowsNT, 0, stream,
+                      (const uint8_t*)table, table_rows, index, n, (O*)out, out_stride, f);
+      });
+    });
+  });
+}
+
+// --------------------------------------------------------------- block mean
+constexpr int64_t kMostIds = (int64_t(1) << 31) - 1;  // rows and edges are counted in int32
+
+int check_block(const massive_block* b) {
+  if (!b) REFUSE("the block is NULL");
+  if (b->n < 0 || b->edges < 0 || b->rows < 0) REFUSE("n, edges and rows must not be negative");
+  if (b->n > kMostIds - 1 || b->edges > kMostIds - 1 || b->rows > kMostIds - 1) REFUSE("n, edges and rows must be below 2^31 - 1");
+  if (b->n > 0 && !b->indptr) REFUSE("indptr is NULL");
+  if (b->edges > 0 && !b->indices) REFUSE("indices is NULL");
+  if (!aligned(b->indptr, 4) || !aligned(b->indices, 4)) REFUSE("indptr or indices is not aligned");
+  return MASSIVE_OK;
+}
+
+int block_mean(const massive_block* b, const void* x, int32_t x_type, int64_t x_stride, const massive_row_format* fmt,
+               int32_t d, void* out, int32_t out_type, int64_t out_stride, void* stream) {
+  if (int rc = check_block(b)) return rc;
+  if (!is_type(out_type)) REFUSE("out_type must be MASSIVE_F32 or MASSIVE_BF16");
+  if (!is_type(x_type) && x_type != MASSIVE_PACKED) REFUSE("x_type must be MASSIVE_F32, MASSIVE_BF16 or MASSIVE_PACKED");
+  if (d < 1) REFUSE("d must be at least 1");
+  ms::PackedRows f = {};
+  f.d = d;
+  if (x_type == MASSIVE_PACKED) {
+    int64_t least;
+    if (int rc = check_format(fmt, &f, &least)) return rc;
+    if (fmt->d != d) REFUSE("d is %d, the row format's %d", d, fmt->d);
+  } else {
+    if (fmt) REFUSE("a row format is given, and x_type is not MASSIVE_PACKED");
+    if (x_stride < d) REFUSE("x_stride is below d");
+  }
+  if (b->n == 0) return MASSIVE_OK;
+  if (!out || (b->rows > 0 && !x)) REFUSE("x / out are NULL");
+  if (out_stride < d) REFUSE("out_stride is below d");
+  if (!aligned(out, size_of(out_type)) || !aligned(x, x_type == MASSIVE_PACKED ? 4 : size_of(x_type)))
+    REFUSE("x or out is not aligned");
+  // the lists' ends are read before their entries: without room for any, none is read
+  auto go = [&](auto* s, auto* o, auto bits, auto q) {
+    using S = std::remove_pointer_t<decltype(s)>;
+    using O = std::remove_pointer_t<decltype(o)>;
+    const int team = team_of(d, q());
+    return with_team(team, [&](auto t) {
+      return launch("massive_block_mean", ms::k_block_mean<S, bits(), O, q(), t()>,
+                    std::min(cdiv(b->n, ms::kMeanNT / team), kMostBlocks), ms::kMeanNT, 0, stream, b->indptr, b->indices, b->n,
+                    b->edges, x, b->rows, x_stride, f, (O*)out, out_stride);
+    });
+  };
+  return with_type(out_type, [&](auto* o) {
+    if (x_type == MASSIVE_PACKED)
+      return with_bits(fmt->bits, [&](auto bits) { return go((float*)nullptr, o, bits, std::integral_constant<int, 8>()); });
+    if (x_type == MASSIVE_F32)
+      return go((float*)nullptr, o, std::integral_constant<int, 0>(), std::integral_constant<int, 4>());
+    return go((bf16*)nullptr, o, std::integral_constant<int, 0>(), std::integral_constant<int, 8>());
+  });
+}
+
+// The backward pass's workspace: two lists of pairs, the chunks' counts, the
+// digits' totals, the sources' spans.
+struct MeanPlan {
+  int passes, bits;        // digits of the sort
+  int chunks;
+  int64_t chunk;
+  int64_t keys[2], vals[2], counts, totals, spans, bytes;
+};
+MeanPlan mean_plan(const massive_block* b) {
+  MeanPlan p = {};
+  int need = 1;
+  while ((int64_t(1) << need) <= b->rows) ++need;  // keys go up to rows
+  p.passes = (int)cdiv(need, ms::kDigitBits);
+  p.bits = (int)cdiv(need, p.passes);
+  p.chunk = std::max<int64_t>(ms::kChunkLeast, round_up(cdiv(b->edges, ms::kChunksMost), MS_WAVE));
+  p.chunks = (int)cdiv(b->edges, p.chunk);
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += round_up(bytes, 16);
+    return here;
+  };
+  for (int i = 0; i < 2; ++i) p.keys[i] = take(4 * b->edges);
+  for (int i = 0; i < 2; ++i) p.vals[i] = take(4 * b->edges);
+  p.counts = take(4 * (int64_t)p.chunks << p.bits);
+  p.totals = take(int64_t(4) << p.bits);
+  p.spans = take(8 * b->rows);
+  p.bytes = at;
+  return p;
+}
+
+int block_mean_backward(const massive_block* b, const void* dout, int32_t type, int64_t dout_stride, int32_t d,
+                        const void* add, int64_t add_stride, int64_t add_rows, void* dx, int64_t dx_stride, void* workspace,
+                        int64_t workspace_bytes, void* stream) {
+  if (int rc = check_block(b)) return rc;
+  if (!is_type(type)) REFUSE("type must be MASSIVE_F32 or MASSIVE_BF16");
+  if (d < 1) REFUSE("d must be at least 1");
+  if (add_rows < 0 || add_rows > b->rows) REFUSE("add_rows must be in 0..rows");
+  if (!add) add_rows = 0;
+  if (add_rows > 0 && add_stride < d) REFUSE("add_stride is below d");
+  if (b->rows == 0) return MASSIVE_OK;
+  if (!dx || (b->n > 0 && !dout)) REFUSE("dout / dx are NULL");
+  if (dx_stride < d || (b->n > 0 && dout_stride < d)) REFUSE("dout_stride or dx_stride is below d");
+  const int size = size_of(type);
+  if (!aligned(dout, size) || !aligned(add, size) || !aligned(dx, size)) REFUSE("dout, add or dx is not aligned");
+  const MeanPlan p = mean_plan(b);
+  if (!workspace || workspace_bytes < p.bytes)
+    return call_error(MASSIVE_ECAPACITY, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0),
+                      (long long)p.bytes);
+  if (!aligned(workspace, 16)) REFUSE("workspace is not 16-byte aligned");
+  char* w = (char*)workspace;
+  uint32_t* keys[2] = {(uint32_t*)(w + p.keys[0]), (uint32_t*)(w + p.keys[1])};
+  int32_t* vals[2] = {(int32_t*)(w + p.vals[0]), (int32_t*)(w + p.vals[1])};
+  int32_t *counts = (int32_t*)(w + p.counts), *totals = (int32_t*)(w + p.totals);
+  int2* spans = (int2*)(w + p.spans);
+  const char* what = "massive_block_mean_backward";
+  const int nt = ms::kSortWaves * MS_WAVE;
+  // without a row no edge belongs to one
+  const int chunks = b->n > 0 ? p.chunks : 0;
+  const int64_t sort_blocks = cdiv(std::max(chunks, 1), ms::kSortWaves);
+  const size_t digits = sizeof(int32_t) << p.bits;
+  if (int rc = launch(what, ms::k_edges, std::max(sort_blocks, std::min<int64_t>(cdiv(b->rows, nt), 512)), nt,
+                      ms::kSortWaves * digits, stream, b->indptr, b->indices, b->n, b->edges, b->rows, p.chunk, chunks, p.bits,
+                      keys[0], vals[0], counts, spans))
+    return rc;
+  int at = 0;
+  for (int pass = 0; chunks > 0 && pass < p.passes; ++pass) {
+    const int shift = pass * p.bits;
+    if (pass > 0)
+      if (int rc = launch(what, ms::k_digits, sort_blocks, nt, ms::kSortWaves * digits, stream, keys[at], b->edges, p.chunk, chunks,
+                          shift, p.bits, counts))
+        return rc;
+    if (int rc = launch(what, ms::k_places, cdiv(1 << p.bits, MS_WAVE), ms::kPlacesWaves * MS_WAVE, 0, stream, counts, chunks,
+                        p.bits, totals))
+      return rc;
+    if (int rc = launch(what, ms::k_move, sort_blocks, nt, (1 + ms::kSortWaves) * digits, stream, keys[at], vals[at], b->edges,
+                        p.chunk, chunks, shift, p.bits, counts, totals, keys[1 - at], vals[1 - at]))
+      return rc;
+    at = 1 - at;
+  }
+  if (chunks > 0)
+    if (int rc = launch(what, ms::k_spans, std::min<int64_t>(cdiv(b->edges, ms::kMeanNT), 4096), ms::kMeanNT, 0, stream, keys[at],
+                        b->edges, b->rows, spans))
+      return rc;
+  return with_type(type, [&](auto* t) {
+    using D = std::remove_pointer_t<decltype(t)>;
+    constexpr int q = sizeof(D) == 4 ? 4 : 8;
+    const int team = team_of(d, q);
+    return with_team(team, [&](auto lanes) {
+      return launch(what, ms::k_block_mean_backward<D, q, lanes()>, std::min(cdiv(b->rows, ms::kMeanNT / team), kMostBlocks),
+                    ms::kMeanNT, 0, stream, spans, vals[at], b->indptr, b->edges, b->rows, (const D*)dout, dout_stride, d,
+                    (const D*)add, add_stride, add_rows, (D*)dx, dx_stride);
+    });
+  });
+}
+
+// ------------------------------------------------------------------- linear
+constexpr int64_t kMostRows = int64_t(1) << 29;  // tiles of 64 rows stay within a launch
+
+template <typename T>
+ms::Operand<T> operand(const void* p, int64_t stride, int64_t R, int64_t K, const void* pre = nullptr, int64_t pre_stride = 0,
+                       int act = MASSIVE_ACT_NONE) {
+  return ms::Operand<T>{(const T*)p, (const T*)pre, stride, pre_stride, R, K, act};
+}
+
+int check_layer(int64_t rows, int32_t n, int32_t k, int32_t k_second, int32_t type, int32_t act, const void* x_second) {
+  if (!is_type(type)) REFUSE("type must be MASSIVE_F32 or MASSIVE_BF16");
+  if (act < MASSIVE_ACT_NONE || act > MASSIVE_ACT_SILU) REFUSE("act is not one of MASSIVE_ACT_*");
+  if (rows < 0 || rows > kMostRows) REFUSE("rows must be in 0..2^29");
+  if (n < 1 || k < 1 || k_second < 0 || n > (1 << 20) || k > (1 << 20) || k_second > (1 << 20))
+    REFUSE("n and k must be in 1..2^20, k_second in 0..2^20");
+  if ((k_second > 0) != (x_second != nullptr) && rows > 0) REFUSE("k_second columns and x_second go together");
+  return MASSIVE_OK;
+}
+
+// Squares of 128 where they give the chip enough blocks, else of 64; 64 columns
+// where no more are asked for.
+template <typename F>
+int with_tile(int64_t rows, int64_t cols, F f) {
+  if (cols <= 64 && cdiv(rows, 128) >= 256)
+    return f(std::integral_constant<int, 128>(), std::integral_constant<int, 64>());
+  if (cols > 64 && cdiv(rows, 128) * cdiv(cols, 128) >= 256)
+    return f(std::integral_constant<int, 128>(), std::integral_constant<int, 128>());
+  return f(std::integral_constant<int, 64>(), std::integral_constant<int, 64>());
+}
+
+template <typename T>
+int linear(const massive_linear_args* a, void* stream) {
+  ms::LinearForward<T> f;
+  const int64_t k = a->k;
+  f.x[0] = operand<T>(a->x, a->x_stride, a->rows, k);
+  f.x[1] = operand<T>(a->x_second, a->x_second_stride, a->rows, a->k_second);
+  f.w[0] = operand<T>(a->w, a->w_stride, a->n, k);
+  f.w[1] = operand<T>((const T*)a->w + k, a->w_stride, a->n, a->k_second);
+  f.bias = (const T*)a->bias;
+  f.residual = (const T*)a->residual;
+  f.y = (T*)a->y;
+  f.pre = (T*)a->pre;
+  f.residual_stride = a->residual_stride;
+  f.y_stride = a->y_stride;
+  f.pre_stride = a->pre_stride;
+  f.rows = a->rows;
+  f.n = a->n;
+  f.act = a->act;
+  return with_tile(a->rows, a->n, [&](auto bm, auto bn) {
+    const int tiles_n = (int)cdiv(a->n, bn());
+    const int64_t blocks = cdiv(a->rows, bm()) * tiles_n;
+    if (blocks > kMostBlocks) REFUSE("too many rows and outputs for one call");
+    return launch("massive_linear", ms::k_linear<T, bm(), bn()>, blocks, ms::kLinNT, 0, stream, f, tiles_n, blocks);
+  });
+}
+
+// How dw's rows are split: enough parts for the chip, none shorter than 512
+// rows.
+struct DwPlan {
+  int bm, bn, tiles_n, tiles[2];
+  int64_t part, parts, dw_floats, bytes;
+};
+DwPlan dw_plan(const massive_linear_grads* a) {
+  DwPlan p = {};
+  p.bm = a->n <= 64 ? 64 : 128;
+  p.bn = a->k <= 64 && a->k_second <= 64 ? 64 : 128;
+  if (p.bm != p.bn) p.bm = p.bn = 64;
+  p.tiles_n = (int)cdiv(a->n, p.bm);
+  p.tiles[0] = (int)cdiv(a->k, p.bn);
+  p.tiles[1] = (int)cdiv(a->k_second, p.bn);
+  const int64_t tiles = (int64_t)p.tiles_n * (p.tiles[0] + p.tiles[1]);
+  const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 512));
+  p.part = round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, 768 / tiles))), 64);
+  p.parts = cdiv(a->rows, p.part);
+  p.dw_floats = a->dw ? p.parts * a->n * ((int64_t)a->k + a->k_second) : 0;
+  p.bytes = 4 * (round_up(p.dw_floats, 4) + (a->dbias ? p.parts * a->n : 0));
+  return p;
+}
+
+int check_grads(const massive_linear_grads* a) {
+  if (!a) REFUSE("args is NULL");
+  return check_layer(a->rows, a->n, a->k, a->k_second, a->type, a->act, a->x_second);
+}
+
+template <typename T>
+int linear_backward(const massive_linear_grads* a, void* workspace, void* stream) {
+  const bool slope = a->act != MASSIVE_ACT_NONE;
+  const int64_t k[2] = {a->k, a->k_second};
+  if (a->dx || a->dx_second) {
+    ms::LinearDx<T> f;
+    f.dz = operand<T>(a->dy, a->dy_stride, a->rows, a->n, a->pre, a->pre_stride, a->act);
+    for (int s = 0; s < 2; ++s) f.w[s] = operand<T>((const T*)a->w + (s ? k[0] : 0), a->w_stride, k[s], a->n);
+    f.dx[0] = (T*)a->dx;
+    f.dx[1] = (T*)a->dx_second;
+    f.dx_stride[0] = a->dx_stride;
+    f.dx_stride[1] = a->dx_second_stride;
+    f.rows = a->rows;
+    f.k[0] = a->k;
+    f.k[1] = a->k_second;
+    const int64_t cols = (a->dx ? k[0] : 0) + (a->dx_second ? k[1] : 0);
+    const int rc = with_tile(a->rows, cols, [&](auto bm, auto bn) {
+      for (int s = 0; s < 2; ++s) f.tiles[s] = f.dx[s] ? (int)cdiv(k[s], bn()) : 0;
+      const int64_t blocks = cdiv(a->rows, bm()) * (f.tiles[0] + f.tiles[1]);
+      if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
+      return slope ? launch("massive_linear_backward", ms::k_linear_dx<T, true, bm(), bn()>, blocks, ms::kLinNT, 0, stream, f, blocks)
+                   : launch("massive_linear_backward", ms::k_linear_dx<T, false, bm(), bn()>, blocks, ms::kLinNT, 0, stream, f, blocks);
+    });
+    if (rc) return rc;
+  }
+  if (!a->dw && !a->dbias) return MASSIVE_OK;
+  const DwPlan p = dw_plan(a);
+  ms::LinearDw<T> f;
+  f.dz = operand<T>(a->dy, a->dy_stride, a->n, a->rows, a->pre, a->pre_stride, a->act);
+  f.x[0] = operand<T>(a->x, a->x_stride, k[0], a->rows);
+  f.x[1] = operand<T>(a->x_second, a->x_second_stride, k[1], a->rows);
+  f.dw = a->dw ? (float*)workspace : nullptr;
+  f.dbias = a->dbias ? (float*)workspace + round_up(p.dw_floats, 4) : nullptr;
+  f.rows = a->rows;
+  f.part = p.part;
+  f.n = a->n;
+  for (int s = 0; s < 2; ++s) {
+    f.k[s] = (int)k[s];
+    f.tiles[s] = p.tiles[s];
+  }
+  f.tiles_n = p.tiles_n;
+  const int64_t blocks = p.parts * p.tiles_n * (p.tiles[0] + p.tiles[1]);
+  if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
+  auto go = [&](auto b) {
+    return slope ? launch("massive_linear_backward", ms::k_linear_dw<T, true, b(), b()>, blocks, ms::kLinNT, 0, stream, f, blocks)
+                 : launch("massive_linear_backward", ms::k_linear_dw<T, false, b(), b()>, blocks, ms::kLinNT, 0, stream, f, blocks);
+  };
+  const int rc = p.bm == 128 ? go(std::integral_constant<int, 128>()) : go(std::integral_constant<int, 64>());
+  if (rc) return rc;
+  const int64_t values = (int64_t)a->n * ((a->dw ? k[0] + k[1] : 0) + (a->dbias ? 1 : 0));
+  return launch("massive_linear_backward", ms::k_linear_join<T>, std::min<int64_t>(cdiv(values, ms::kLinNT), 4096), ms::kLinNT, 0,
+                stream, (const float*)f.dw, (const float*)f.dbias, p.parts, a->n, (int)(k[0] + k[1]), (T*)a->dw, a->dw_stride,
+                (T*)a->dbias);
+}
+
+// -------------------------------------------------------------------- AdamW
+int adamw(const massive_adamw_tensor* tensors, int64_t count, const massive_adamw_args* a, void* stream) {
+  if (!a) REFUSE("args is NULL");
+  if (count < 0 || (count > 0 && !tensors)) REFUSE("tensors is NULL or count negative");
+  if (a->state_bits != 32 && a->state_bits != 8) REFUSE("state_bits must be 32 or 8");
+  if (!is_type(a->param_type) || !is_type(a->grad_type)) REFUSE("param_type and grad_type must be MASSIVE_F32 or MASSIVE_BF16");
+  if (a->t < 1) REFUSE("t counts steps from 1");
+  if (a->reserved != 0) REFUSE("reserved must be 0");
+  if (!(a->beta_first >= 0 && a->beta_first < 1 && a->beta_second >= 0 && a->beta_second < 1))
+    REFUSE("the betas must be in [0, 1)");
+  if (!(a->lr >= 0 && a->eps >= 0 && a->weight_decay >= 0) || !std::isfinite(a->lr) || !std::isfinite(a->eps) ||
+      !std::isfinite(a->weight_decay))
+    REFUSE("lr, eps and weight_decay must be finite and not negative");
+  const bool eight = a->state_bits == 8;
+  for (int64_t i = 0; i < count; ++i) {
+    const massive_adamw_tensor& t = tensors[i];
+    if (t.n < 0 || t.n > kMostBlocks * ms::kAdamwBlock / 2) REFUSE("tensor %lld: n must be in 0..2^34", (long long)i);
+    if (t.n == 0) continue;
+    if (!t.param || !t.grad || !t.m || !t.v) REFUSE("tensor %lld: param, grad, m or v is NULL", (long long)i);
+    if (eight != (t.m_scale && t.v_scale) || (!eight && (t.m_scale || t.v_scale)))
+      REFUSE("tensor %lld: states of 8 bits have scales, of 32 bits none", (long long)i);
+    if (!aligned(t.param, size_of(a->param_type)) || !aligned(t.grad, size_of(a->grad_type)) || !aligned(t.copy, 2) ||
+        !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4) || (!eight && (!aligned(t.m, 4) || !aligned(t.v, 4))))
+      REFUSE("tensor %lld: an array is not aligned", (long long)i);
+  }
+  ms::AdamwLaunch l;
+  l.decay = (float)(1.0 - a->lr * a->weight_decay);
+  l.b1 = (float)a->beta_first;
+  l.b1c = (float)(1.0 - a->beta_first);
+  l.b2 = (float)a->beta_second;
+  l.b2c = (float)(1.0 - a->beta_second);
+  l.lr = (float)(a->lr / (1.0 - std::pow(a->beta_first, (double)a->t)));
+  l.v_factor = (float)(1.0 / std::sqrt(1.0 - std::pow(a->beta_second, (double)a->t)));
+  l.eps = (float)a->eps;
+  for (int64_t i = 0; i < count;) {
+    l.count = 0;
+    int64_t blocks = 0;
+    for (; i < count && l.count < ms::kAdamwTensors; ++i) {
+      const massive_adamw_tensor& t = tensors[i];
+      if (t.n == 0) continue;
+      const int64_t more = cdiv(t.n, ms::kAdamwBlock);
+      if (l.count > 0 && blocks + more > kMostBlocks) break;
+      l.t[l.count] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, (bf16*)t.copy, t.n};
+      l.first[l.count++] = (int32_t)blocks;
+      blocks += more;
+    }
+    if (l.count == 0) break;
+    l.first[l.count] = (int32_t)blocks;
+    const int rc = with_type(a->param_type, [&](auto* p) {
+      using P = std::remove_pointer_t<decltype(p)>;
+      return with_type(a->grad_type, [&](auto* g) {
+        using G = std::remove_pointer_t<decltype(g)>;
+        return eight ? launch("massive_adamw", ms::k_adamw<P, G, 8>, blocks, ms::kAdamwNT, 0, stream, l)
+                     : launch("massive_adamw", ms::k_adamw<P, G, 32>, blocks, ms::kAdamwNT, 0, stream, l);
+      });
+    });
+    if (rc) return rc;
+  }
+  return MASSIVE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int massive_row_layout(const massive_row_format* fmt, int64_t* row_bytes, int64_t* floats_at) {
+  ms::PackedRows f;
+  int64_t least;
+  if (int rc = check_format(fmt, &f, &least)) return rc;
+  if (row_bytes) *row_bytes = least;
+  if (floats_at) *floats_at = f.floats_at;
+  return MASSIVE_OK;
+}
+
+int massive_pack_rows(const massive_row_format* fmt, const void* src, int32_t src_type, int64_t src_stride, int64_t n,
+                      const int32_t* slots, void* table, int64_t table_rows, void* stream) {
+  return pack_rows(fmt, src, src_type, src_stride, n, slots, table, table_rows, stream);
+}
+
+int massive_unpack_rows(const massive_row_format* fmt, const void* table, int64_t table_rows, const int32_t* index, int64_t n,
+                        void* out, int32_t out_type, int64_t out_stride, void* stream) {
+  return unpack_rows(fmt, table, table_rows, index, n, out, out_type, out_stride, stream);
+}
+
+int massive_block_mean(const massive_block* block, const void* x, int32_t x_type, int64_t x_stride,
+                       const massive_row_format* fmt, int32_t d, void* out, int32_t out_type, int64_t out_stride, void* stream) {
+  return block_mean(block, x, x_type, x_stride, fmt, d, out, out_type, out_stride, stream);
+}
+
+int massive_block_mean_workspace(const massive_block* block, int64_t* bytes) {
+  if (!bytes) REFUSE("bytes is NULL");
+  if (int rc = check_block(block)) return rc;
+  *bytes = mean_plan(block).bytes;
+  return MASSIVE_OK;
+}
+
+int massive_block_mean_backward(const massive_block* block, const void* dout, int32_t type, int64_t dout_stride, int32_t d,
+                                const void* add, int64_t add_stride, int64_t add_rows, void* dx, int64_t dx_stride,
+                                void* workspace, int64_t workspace_bytes, void* stream) {
+  return block_mean_backward(block, dout, type, dout_stride, d, add, add_stride, add_rows, dx, dx_stride, workspace,
+                             workspace_bytes, stream);
+}
+
+int massive_linear(const massive_linear_args* a, void* stream) {
+  if (!a) REFUSE("args is NULL");
+  if (int rc = check_layer(a->rows, a->n, a->k, a->k_second, a->type, a->act, a->x_second)) return rc;
+  if (a->rows == 0) return MASSIVE_OK;
+  if (!a->x || !a->w || !a->y) REFUSE("x / w / y are NULL");
+  if (a->x_stride < a->k || (a->x_second && a->x_second_stride < a->k_second) ||
+      a->w_stride < (int64_t)a->k + a->k_second || a->y_stride < a->n || (a->residual && a->residual_stride < a->n) ||
+      (a->pre && a->pre_stride < a->n))
+    REFUSE("a stride is below its rows' length");
+  const int size = size_of(a->type);
+  for (const void* p : {a->x, a->x_second, a->w, a->bias, a->residual, (const void*)a->y, (const void*)a->pre})
+    if (!aligned(p, size)) REFUSE("an array is not aligned");
+  return a->type == MASSIVE_F32 ? linear<float>(a, stream) : linear<bf16>(a, stream);
+}
+
+int massive_linear_workspace(const massive_linear_grads* a, int64_t* bytes) {
+  if (!bytes) REFUSE("bytes is NULL");
+  if (int rc = check_grads(a)) return rc;
+  *bytes = a->rows == 0 || (!a->dw && !a->dbias) ? 0 : dw_plan(a).bytes;
+  return MASSIVE_OK;
+}
+
+int massive_linear_backward(const massive_linear_grads* a, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (int rc = check_grads(a)) return rc;
+  const bool dz = a->dx || a->dx_second || a->dw || a->dbias;
+  if (!dz) return MASSIVE_OK;
+  if (a->dx_second && !a->k_second) REFUSE("dx_second without a second input");
+  const int64_t k = (int64_t)a->k + a->k_second;
+  if (a->dw && a->dw_stride < k) REFUSE("a stride is below its rows' length");
+  if (a->rows > 0) {
+    if (!a->dy || (a->act != MASSIVE_ACT_NONE && !a->pre)) REFUSE("dy / pre are NULL");
+    if ((a->dx || a->dx_second) && !a->w) REFUSE("w is NULL");
+    if ((a->dw || a->dbias) && !a->x) REFUSE("x is NULL");
+    if (a->dy_stride < a->n || (a->act != MASSIVE_ACT_NONE && a->pre_stride < a->n) || (a->x && a->x_stride < a->k) ||
+        (a->x_second && a->x_second_stride < a->k_second) || (a->w && a->w_stride < k) || (a->dx && a->dx_stride < a->k) ||
+        (a->dx_second && a->dx_second_stride < a->k_second))
+      REFUSE("a stride is below its rows' length");
+  }
+  const int size = size_of(a->type);
+  for (const void* p : {a->dy, a->pre, a->x, a->x_second, a->w, (const void*)a->dx, (const void*)a->dx_second,
+                        (const void*)a->dw, (const void*)a->dbias})
+    if (!aligned(p, size)) REFUSE("an array is not aligned");
+  if (a->rows == 0) {  // sums over no rows
+    const int64_t values = (int64_t)a->n * ((a->dw ? k : 0) + (a->dbias ? 1 : 0));
+    if (values == 0) return MASSIVE_OK;
+    const int64_t blocks = std::min<int64_t>(cdiv(values, ms::kLinNT), 4096);
+    // the pointers only say which of the two are asked for: with no parts nothing is read
+    const float *dw = (const float*)a->dw, *db = (const float*)a->dbias;
+    return a->type == MASSIVE_F32
+               ? launch("massive_linear_backward", ms::k_linear_join<float>, blocks, ms::kLinNT, 0, stream, dw, db, int64_t(0),
+                        a->n, (int)k, (float*)a->dw, a->dw_stride, (float*)a->dbias)
+               : launch("massive_linear_backward", ms::k_linear_join<bf16>, blocks, ms::kLinNT, 0, stream, dw, db, int64_t(0),
+                        a->n, (int)k, (bf16*)a->dw, a->dw_stride, (bf16*)a->dbias);
+  }
+  if (a->dw || a->dbias) {
+    const int64_t need = dw_plan(a).bytes;
+    if (!workspace || workspace_bytes < need)
+      return call_error(MASSIVE_ECAPACITY, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0),
+                        (long long)need);
+    if (!aligned(workspace, 16)) REFUSE("workspace is not 16-byte aligned");
+  }
+  return a->type == MASSIVE_F32 ? linear_backward<float>(a, workspace, stream) : linear_backward<bf16>(a, workspace, stream);
+}
+
+int massive_adamw(const massive_adamw_tensor* tensors, int64_t count, const massive_adamw_args* args, void* stream) {
+  return adamw(tensors, count, args, stream);
+}
+
+int massive_adamw_states(const void* m, const void* v, const float* m_scale, const float* v_scale, int64_t n, float* m_out,
+                         float* v_out, void* stream) {
+  if (n < 0) REFUSE("n must not be negative");
+  if (n == 0) return MASSIVE_OK;
+  if (!m || !v || !m_scale || !v_scale || !m_out || !v_out) REFUSE("an array is NULL");
+  if (!aligned(m_scale, 4) || !aligned(v_scale, 4) || !aligned(m_out, 4) || !aligned(v_out, 4)) REFUSE("an array is not aligned");
+  return launch("massive_adamw_states", ms::k_adamw_states, std::min(cdiv(n, ms::kAdamwNT * ms::kAdamwQ), kMostBlocks),
+                ms::kAdamwNT, 0, stream, (const int8_t*)m, (const uint8_t*)v, m_scale, v_scale, n, m_out, v_out);
+}
+
+}  // extern "C"

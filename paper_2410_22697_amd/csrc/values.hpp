@@ -1,0 +1,106 @@
+// values.hpp - rows of 32-bit, bf16 or packed values, as the operators' kernels
+// read and write them: a few neighbouring columns of one row at a time.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace ms {
+
+typedef __bf16 bf16;
+
+// Vectors at the alignment of their elements: rows of any stride are read in
+// whole vectors, which global memory takes at any address.
+template <typename T, int Q>
+struct ColsOf {
+  typedef T type __attribute__((ext_vector_type(Q), aligned(sizeof(T))));
+};
+template <typename T, int Q>
+using cols_t = typename ColsOf<T, Q>::type;
+
+// Columns [0, valid) of the Q at p as fp32, `fill` in the others.
+template <typename T, int Q>
+__device__ __forceinline__ void load_cols(const T* p, int valid, float* x, float fill = 0.0f) {
+  if (valid >= Q) {
+    const cols_t<T, Q> v = *reinterpret_cast<const cols_t<T, Q>*>(p);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) x[q] = (float)v[q];
+  } else {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) x[q] = q < valid ? (float)p[q] : fill;
+  }
+}
+
+// Stores columns [0, valid) of x, rounded to nearest even.
+template <typename T, int Q>
+__device__ __forceinline__ void store_cols(T* p, int valid, const float* x) {
+  if (valid >= Q) {
+    cols_t<T, Q> v;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) v[q] = (T)x[q];
+    *reinterpret_cast<cols_t<T, Q>*>(p) = v;
+  } else {
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+      if (q < valid) p[q] = (T)x[q];
+  }
+}
+
+// The layout of packed rows (massive_row_format): codes from byte 0, the
+// groups' floats from floats_at on.
+struct PackedRows {
+  int32_t d;          // values per row
+  int32_t group_log2; // columns per group as a power of two, or 31: one group
+  int32_t floats_at;
+  int64_t row_bytes;
+};
+
+// Where a row lies in a table, null for an index outside it.
+__device__ __forceinline__ const uint8_t* packed_row(const uint8_t* table, int64_t rows, int64_t i, int64_t row_bytes) {
+  return i >= 0 && i < rows ? table + i * row_bytes : nullptr;
+}
+
+// Q columns of a packed row from column c on (c a multiple of Q): codes and
+// their group's floats, one load each, and the values that they stand for.
+template <int BITS, int Q>
+struct PackedCols {
+  static constexpr int kBytes = Q * BITS / 8;  // 2, 4 or 8
+  uint32_t w[kBytes > 4 ? 2 : 1];
+  float step, lo;
+
+  __device__ __forceinline__ void load(const uint8_t* row, const PackedRows& f, int c) {
+    const uint8_t* p = row + (int64_t)c * BITS / 8;
+    if constexpr (kBytes == 2) {
+      w[0] = *reinterpret_cast<const uint16_t*>(p);
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+      // a row's codes end on four bytes, not on eight
+      if constexpr (kBytes == 8) w[1] = c + 4 < f.d ? *reinterpret_cast<const uint32_t*>(p + 4) : 0u;
+    }
+    const int g = c >> f.group_log2;
+    const float* s = reinterpret_cast<const float*>(row + f.floats_at);
+    if constexpr (BITS == 8) {
+      step = s[g];
+      lo = 0.0f;
+    } else {
+      lo = s[2 * g];
+      step = s[2 * g + 1];
+    }
+  }
+  __device__ __forceinline__ void none() {
+    w[0] = 0;
+    if constexpr (kBytes == 8) w[1] = 0;
+    step = lo = 0.0f;
+  }
+  __device__ __forceinline__ void values(float* x) const {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if constexpr (BITS == 8)
+        x[q] = (float)(int8_t)(w[q / 4] >> (8 * (q % 4))) * step;
+      else
+        x[q] = lo + (float)((w[q / 8] >> (4 * (q % 8))) & 15u) * step;
+    }
+  }
+};
+
+}  // namespace ms

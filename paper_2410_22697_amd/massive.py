@@ -24,7 +24,10 @@ _NAMES = {EINVAL: "EINVAL", ECAPACITY: "ECAPACITY", ENOMEM: "ENOMEM", EHIP: "EHI
 EXPORTS = ("massive_init", "massive_output_bounds", "massive_sample", "massive_sample_noalloc", "massive_sample_async",
            "massive_batch_wait", "massive_evict_step", "massive_get_counters", "massive_get_state",
            "massive_get_buffer_rows", "massive_info", "massive_set_timing", "massive_get_timing",
-           "massive_destroy", "massive_last_error")
+           "massive_destroy", "massive_last_error",
+           "massive_row_layout", "massive_pack_rows", "massive_unpack_rows", "massive_block_mean",
+           "massive_block_mean_workspace", "massive_block_mean_backward", "massive_linear", "massive_linear_workspace",
+           "massive_linear_backward", "massive_adamw", "massive_adamw_states")
 
 
 class MassiveError(RuntimeError):

@@ -1,0 +1,478 @@
+"""What a training step does with the rows that `Massive` gathers (the
+operators of include/massive.h): rows held in few bits, the mean over a sampled
+block, a layer and the step on its weights.
+
+As in the rest of the binding, Python only checks and marshals arguments: every
+operator runs in the library's HIP kernels, on the current stream of the
+tensors' device, and returns without waiting. Outputs and workspaces come from
+torch's allocator. `linear` and `block_mean` take part in autograd; their
+gradients are also there as calls of their own. Wrong arguments raise
+ValueError here, or MassiveError where the library refuses them.
+"""
+import ctypes
+from typing import List, Optional, Sequence, Tuple
+
+import torch
+
+from . import massive
+from .massive import OK, MassiveError
+
+F32, BF16, PACKED = 0, 1, 2
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+_vp, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+
+
+class _Format(ctypes.Structure):
+    _fields_ = [("d", _i32), ("bits", _i32), ("group", _i32), ("reserved", _i32), ("row_bytes", _i64)]
+
+
+class _Block(ctypes.Structure):
+    _fields_ = [("indptr", _vp), ("indices", _vp), ("n", _i64), ("edges", _i64), ("rows", _i64)]
+
+
+class _LinearArgs(ctypes.Structure):
+    _fields_ = [(f, _vp) for f in ("x", "x_second", "w", "bias", "residual", "y", "pre")] + [("rows", _i64)] + \
+        [(f, _i64) for f in ("x_stride", "x_second_stride", "w_stride", "residual_stride", "y_stride", "pre_stride")] + \
+        [(f, _i32) for f in ("n", "k", "k_second", "type", "act")]
+
+
+class _LinearGrads(ctypes.Structure):
+    _fields_ = [(f, _vp) for f in ("dy", "pre", "x", "x_second", "w", "dx", "dx_second", "dw", "dbias")] + [("rows", _i64)] + \
+        [(f, _i64) for f in ("dy_stride", "pre_stride", "x_stride", "x_second_stride", "w_stride", "dx_stride",
+                             "dx_second_stride", "dw_stride")] + \
+        [(f, _i32) for f in ("n", "k", "k_second", "type", "act")]
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [(f, _vp) for f in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", _i64)]
+
+
+class _AdamwArgs(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_double) for f in ("lr", "beta_first", "beta_second", "eps", "weight_decay")] + \
+        [("t", _i64)] + [(f, _i32) for f in ("state_bits", "param_type", "grad_type", "reserved")]
+
+
+_lib = None
+
+
+def _load():
+    global _lib
+    if _lib is None:
+        lib = massive.load()
+        p = ctypes.POINTER
+        lib.massive_row_layout.argtypes = [p(_Format), p(_i64), p(_i64)]
+        lib.massive_pack_rows.argtypes = [p(_Format), _vp, _i32, _i64, _i64, _vp, _vp, _i64, _vp]
+        lib.massive_unpack_rows.argtypes = [p(_Format), _vp, _i64, _vp, _i64, _vp, _i32, _i64, _vp]
+        lib.massive_block_mean.argtypes = [p(_Block), _vp, _i32, _i64, p(_Format), _i32, _vp, _i32, _i64, _vp]
+        lib.massive_block_mean_workspace.argtypes = [p(_Block), p(_i64)]
+        lib.massive_block_mean_backward.argtypes = [p(_Block), _vp, _i32, _i64, _i32, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp]
+        lib.massive_linear.argtypes = [p(_LinearArgs), _vp]
+        lib.massive_linear_workspace.argtypes = [p(_LinearGrads), p(_i64)]
+        lib.massive_linear_backward.argtypes = [p(_LinearGrads), _vp, _i64, _vp]
+        lib.massive_adamw.argtypes = [p(_AdamwTensor), _i64, p(_AdamwArgs), _vp]
+        lib.massive_adamw_states.argtypes = [_vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp]
+        _lib = lib
+    return _lib
+
+
+def _check(rc):
+    if rc != OK:
+        raise MassiveError(rc, _lib.massive_last_error(None).decode())
+
+
+def _stream(device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _on_gpu(*tensors):
+    """All tensors given lie on the current GPU: the library launches there."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("operators take device (cuda) tensors, not one on %s" % t.device)
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError("a tensor lies on %s, and cuda:%d is the current device" % (t.device, here))
+
+
+def _matrix(t, name, cols=None, rows=None, dtype=None) -> int:
+    """The row stride of a 2-d tensor whose rows are contiguous; checks its shape and type."""
+    if t.dim() != 2 or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a 2-d tensor with contiguous rows" % name)
+    if t.dtype not in _TYPES or (dtype is not None and t.dtype != dtype):
+        raise ValueError("%s is %s, and must be %s" % (name, t.dtype, dtype or "float32 or bfloat16"))
+    if (cols is not None and t.shape[1] != cols) or (rows is not None and t.shape[0] != rows):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), ("any" if rows is None else rows, "any" if cols is None else cols)))
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError("%s has rows that overlap" % name)
+    # a row count of one or none leaves the stride open
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _ids(t, name) -> int:
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous 1-d int32 tensor" % name)
+    return t.numel()
+
+
+# ------------------------------------------------------------------ packed rows
+class RowFormat:
+    """Rows of d values in 8 or 4 bits: `group` columns share a step (8 bits) or
+    a least value and a step (4 bits); 0 for the whole row, else a power of two
+    from 16 to 512. row_bytes, a multiple of 4, is the bytes of a row of a
+    table (the least by default), and what `Massive` is given as its row_bytes
+    for features held this way."""
+
+    def __init__(self, d: int, bits: int = 8, group: int = 0, row_bytes: int = 0):
+        for name, value in (("d", d), ("bits", bits), ("group", group)):
+            if not -2 ** 31 <= int(value) < 2 ** 31:
+                raise ValueError("%s is out of range" % name)
+        self.c = _Format(int(d), int(bits), int(group), 0, int(row_bytes))
+        least, floats_at = _i64(), _i64()
+        lib = _load()
+        _check(lib.massive_row_layout(ctypes.byref(self.c), ctypes.byref(least), ctypes.byref(floats_at)))
+        self.d, self.bits, self.group = int(d), int(bits), int(group)
+        self.least_bytes, self.floats_at = int(least.value), int(floats_at.value)
+        self.row_bytes = self.c.row_bytes = int(row_bytes) or self.least_bytes
+
+    def __repr__(self):
+        return "RowFormat(d=%d, bits=%d, group=%d, row_bytes=%d)" % (self.d, self.bits, self.group, self.row_bytes)
+
+
+def _table(t, fmt, name="table", pinned=False) -> int:
+    """Rows of a table: a contiguous uint8 tensor [rows, row_bytes], on the GPU or (to be read) pinned."""
+    if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[1] != fmt.row_bytes or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous uint8 tensor of rows of %d bytes" % (name, fmt.row_bytes))
+    if not (pinned and not t.is_cuda and t.is_pinned()):
+        _on_gpu(t)
+    return t.shape[0]
+
+
+def pack_rows(x, fmt: RowFormat, out=None, slots=None):
+    """Writes x's rows (float32 or bfloat16, [n, d]) in fmt to rows slots[i]
+    (int32, distinct; one outside the table is left out) of the uint8 table
+    `out`, or to its first n rows without slots. Without out, a new table of n
+    rows. Returns the table."""
+    stride = _matrix(x, "x", cols=fmt.d)
+    _on_gpu(x, slots)
+    n = x.shape[0]
+    if slots is not None and _ids(slots, "slots") != n:
+        raise ValueError("x has %d rows, and there are %d slots" % (n, slots.numel()))
+    if out is None:
+        if slots is not None:
+            raise ValueError("slots without a table to write to")
+        out = torch.empty((n, fmt.row_bytes), dtype=torch.uint8, device=x.device)
+        if fmt.row_bytes != fmt.least_bytes:
+            out[:, fmt.least_bytes:] = 0
+    rows = _table(out, fmt, "out")
+    if slots is None and rows < n:
+        raise ValueError("out has %d rows, and x %d" % (rows, n))
+    _check(_load().massive_pack_rows(ctypes.byref(fmt.c), x.data_ptr(), _TYPES[x.dtype], stride, n,
+                                     None if slots is None else slots.data_ptr(), out.data_ptr(), rows, _stream(x.device)))
+    return out
+
+
+def unpack_rows(table, fmt: RowFormat, index=None, dtype=torch.float32, out=None):
+    """Reads rows index[i] (int32; one outside the table reads as zeros), or
+    every row without an index, of a table on the GPU or in pinned memory, to
+    a new tensor of dtype, or to `out`."""
+    rows = _table(table, fmt, pinned=True)
+    _on_gpu(index, out)
+    n = rows if index is None else _ids(index, "index")
+    if out is None:
+        if dtype not in _TYPES:
+            raise ValueError("dtype must be float32 or bfloat16, not %s" % dtype)
+        device = table.device if table.is_cuda else torch.device("cuda", torch.cuda.current_device())
+        out = torch.empty((n, fmt.d), dtype=dtype, device=device)
+    stride = _matrix(out, "out", cols=fmt.d, rows=n)
+    _check(_load().massive_unpack_rows(ctypes.byref(fmt.c), table.data_ptr(), rows, None if index is None else index.data_ptr(), n,
+                                       out.data_ptr(), _TYPES[out.dtype], stride, _stream(out.device)))
+    return out
+
+
+# ------------------------------------------------------------------- block mean
+def _block(indptr, indices, rows) -> _Block:
+    n = _ids(indptr, "indptr") - 1
+    if n < 0:
+        raise ValueError("indptr needs a row's end at least")
+    return _Block(indptr.data_ptr(), indices.data_ptr(), n, _ids(indices, "indices"), int(rows))
+
+
+def _block_mean(x, indptr, indices, fmt, dtype):
+    _on_gpu(indptr, indices)
+    if fmt is not None:
+        rows, d, kind, stride, c = _table(x, fmt, "x", pinned=True), fmt.d, PACKED, 0, ctypes.byref(fmt.c)
+        dtype = dtype or torch.float32
+    else:
+        stride = _matrix(x, "x")
+        _on_gpu(x)
+        (rows, d), kind, c = x.shape, _TYPES[x.dtype], None
+        dtype = dtype or x.dtype
+    if dtype not in _TYPES:
+        raise ValueError("dtype must be float32 or bfloat16, not %s" % dtype)
+    b = _block(indptr, indices, rows)
+    out = torch.empty((b.n, d), dtype=dtype, device=indptr.device)
+    _check(_load().massive_block_mean(ctypes.byref(b), x.data_ptr(), kind, stride, c, d, out.data_ptr(), _TYPES[dtype], d,
+                                      _stream(out.device)))
+    return out
+
+
+class _BlockMean(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, indptr, indices, dtype):
+        ctx.save_for_backward(indptr, indices)
+        ctx.rows, ctx.dtype = x.shape[0], x.dtype
+        return _block_mean(x, indptr, indices, None, dtype)
+
+    @staticmethod
+    def backward(ctx, dout):
+        indptr, indices = ctx.saved_tensors
+        # summed in the gradient's type, and given in the input's
+        return block_mean_backward(dout.contiguous(), indptr, indices, ctx.rows).to(ctx.dtype), None, None, None
+
+
+def block_mean(x, indptr, indices, fmt: Optional[RowFormat] = None, dtype=None):
+    """[n, d]: the mean of x's rows indices[indptr[i]:indptr[i + 1]], zeros for
+    an empty list. indptr (n + 1) and indices are int32, such as hop k's of a
+    batch: `bb.indptr[k][:n + 1]`, `bb.indices[k][:e]`, with x the rows of the
+    next frontier. x is float32 or bfloat16, or with fmt a table of packed
+    rows. The result has x's type (float32 for packed rows) unless dtype says
+    otherwise. An index outside x stands for a row of zeros."""
+    if fmt is None and x.requires_grad and torch.is_grad_enabled():
+        return _BlockMean.apply(x, indptr, indices, dtype)
+    return _block_mean(x, indptr, indices, fmt, dtype)
+
+
+def block_mean_backward(dout, indptr, indices, rows: int, add=None):
+    """The gradient [rows, d] of block_mean's x, in dout's type: row j sums
+    dout[i] / length(i) over the rows i that list j, in their order; plus
+    add[j] for the first len(add) rows."""
+    stride = _matrix(dout, "dout")
+    _on_gpu(dout, indptr, indices, add)
+    b = _block(indptr, indices, rows)
+    if dout.shape[0] != b.n:
+        raise ValueError("dout has %d rows, and the block %d" % (dout.shape[0], b.n))
+    d = dout.shape[1]
+    add_stride = 0 if add is None else _matrix(add, "add", cols=d, dtype=dout.dtype)
+    add_rows = 0 if add is None else add.shape[0]
+    if add_rows > rows:
+        raise ValueError("add has %d rows, more than the %d of the gradient" % (add_rows, rows))
+    lib = _load()
+    dx = torch.empty((int(rows), d), dtype=dout.dtype, device=dout.device)
+    need = _i64()
+    _check(lib.massive_block_mean_workspace(ctypes.byref(b), ctypes.byref(need)))
+    work = torch.empty(max(need.value, 16), dtype=torch.uint8, device=dout.device)
+    _check(lib.massive_block_mean_backward(ctypes.byref(b), dout.data_ptr(), _TYPES[dout.dtype], stride, d,
+                                           add.data_ptr() if add_rows else None, add_stride, add_rows, dx.data_ptr(), d,
+                                           work.data_ptr(), work.numel(), _stream(dout.device)))
+    return dx
+
+
+# ----------------------------------------------------------------------- linear
+def _activation(act) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s, not %r" % (", ".join(ACTIVATIONS), act))
+    return ACTIVATIONS[act]
+
+
+def _layer(x, weight, x2):
+    """Checks the inputs and weights of a layer; (rows, n, k, k2)."""
+    _matrix(x, "x")
+    rows, k = x.shape
+    k2 = 0
+    if x2 is not None:
+        _matrix(x2, "x2", rows=rows, dtype=x.dtype)
+        k2 = x2.shape[1]
+    _matrix(weight, "weight", cols=k + k2, dtype=x.dtype)
+    return rows, weight.shape[0], k, k2
+
+
+def _vector(t, name, n, dtype):
+    if t.dim() != 1 or t.numel() != n or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous 1-d tensor of %d values of %s" % (name, n, dtype))
+
+
+def _stride(t, cols):
+    return cols if t is None or t.shape[0] <= 1 else t.stride(0)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _linear(x, weight, bias, act, residual, x2, save_pre):
+    code = _activation(act)
+    rows, n, k, k2 = _layer(x, weight, x2)
+    _on_gpu(x, weight, bias, residual, x2)
+    if bias is not None:
+        _vector(bias, "bias", n, x.dtype)
+    if residual is not None:
+        _matrix(residual, "residual", cols=n, rows=rows, dtype=x.dtype)
+    y = torch.empty((rows, n), dtype=x.dtype, device=x.device)
+    pre = torch.empty_like(y) if save_pre else None
+    a = _LinearArgs(x.data_ptr(), _ptr(x2), weight.data_ptr(), _ptr(bias), _ptr(residual), y.data_ptr(), _ptr(pre), rows,
+                    _stride(x, k), _stride(x2, k2), _stride(weight, k + k2), _stride(residual, n), n, n, n, k, k2,
+                    _TYPES[x.dtype], code)
+    _check(_load().massive_linear(ctypes.byref(a), _stream(x.device)))
+    return y, pre
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, act, residual, x2):
+        # relu's own output says where its slope is 1, unless a residual was added to it
+        keep = act in ("gelu", "silu") or (act == "relu" and residual is not None)
+        y, pre = _linear(x, weight, bias, act, residual, x2, keep)
+        ctx.save_for_backward(x, weight, x2, pre if keep else (y if act == "relu" else None))
+        ctx.act, ctx.bias = act, bias is not None
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, x2, pre = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dy = dy.contiguous()
+        dx, dx2, dw, db = linear_backward(dy, x, weight, ctx.act, pre, x2, bias=ctx.bias and need[2], need_dx=need[0],
+                                          need_dx2=need[5], need_dw=need[1])
+        return dx, dw, db, None, dy if need[4] else None, dx2
+
+
+def linear(x, weight, bias=None, act: str = "none", residual=None, x2=None, save_pre: bool = False):
+    """act([x | x2] weight^T + bias) + residual, with act "none", "relu",
+    "gelu" (z times the normal distribution's Phi(z)) or "silu". x [rows, k],
+    x2 [rows, k2], weight [n, k + k2], bias [n], residual [rows, n]; all of one
+    type, float32 or bfloat16, rows of any stride. With save_pre, returns the
+    activation's argument too, for linear_backward."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, residual, x2)):
+        if save_pre:
+            raise ValueError("save_pre is for calls outside autograd")
+        return _Linear.apply(x, weight, bias, act, residual, x2)
+    y, pre = _linear(x, weight, bias, act, residual, x2, save_pre)
+    return (y, pre) if save_pre else y
+
+
+def linear_backward(dy, x, weight, act: str = "none", pre=None, x2=None, bias: bool = True, need_dx: bool = True,
+                    need_dx2: bool = True, need_dw: bool = True):
+    """(dx, dx2, dweight, dbias) of `linear`, None for those not asked for or
+    not there. pre is what linear returned with save_pre (for relu without a
+    residual, y serves as well), None for act "none". The residual's gradient
+    is dy."""
+    code = _activation(act)
+    rows, n, k, k2 = _layer(x, weight, x2)
+    _on_gpu(dy, x, weight, x2, pre)
+    _matrix(dy, "dy", cols=n, rows=rows, dtype=x.dtype)
+    if (pre is None) != (code == 0):
+        raise ValueError("pre goes with an activation, and only with one")
+    if pre is not None:
+        _matrix(pre, "pre", cols=n, rows=rows, dtype=x.dtype)
+    new = lambda *shape: torch.empty(shape, dtype=x.dtype, device=x.device)  # noqa: E731
+    dx = new(rows, k) if need_dx else None
+    dx2 = new(rows, k2) if need_dx2 and x2 is not None else None
+    dw = new(n, k + k2) if need_dw else None
+    db = new(n) if bias else None
+    g = _LinearGrads(dy.data_ptr(), _ptr(pre), x.data_ptr(), _ptr(x2), weight.data_ptr(), _ptr(dx), _ptr(dx2), _ptr(dw), _ptr(db),
+                     rows, _stride(dy, n), _stride(pre, n), _stride(x, k), _stride(x2, k2), _stride(weight, k + k2), k, k2, k + k2,
+                     n, k, k2, _TYPES[x.dtype], code)
+    lib = _load()
+    need = _i64()
+    _check(lib.massive_linear_workspace(ctypes.byref(g), ctypes.byref(need)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
+    _check(lib.massive_linear_backward(ctypes.byref(g), _ptr(work), need.value, _stream(x.device)))
+    return dx, dx2, dw, db
+
+
+# ------------------------------------------------------------------------ AdamW
+class AdamW:
+    """AdamW over a list of tensors, contiguous and of one type (float32 or
+    bfloat16), updated in place by `step`. state_bits 32 keeps the two moments
+    as float32, 8 as bytes with a float32 scale for each 256 values. copies: for
+    each parameter a bfloat16 tensor of its shape that receives the new values,
+    or None.
+
+    The states of all tensors lie in flat arrays, each tensor's from a multiple
+    of 256 values on (`starts`)."""
+
+    def __init__(self, params: Sequence, lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 0.01, state_bits: int = 32, copies: Optional[Sequence] = None):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("no parameters")
+        if state_bits not in (32, 8):
+            raise ValueError("state_bits must be 32 or 8")
+        self.copies = [None] * len(self.params) if copies is None else list(copies)
+        if len(self.copies) != len(self.params):
+            raise ValueError("%d parameters, and %d copies" % (len(self.params), len(self.copies)))
+        self.dtype = self.params[0].dtype
+        if self.dtype not in _TYPES:
+            raise ValueError("parameters must be float32 or bfloat16, not %s" % self.dtype)
+        _on_gpu(*self.params, *self.copies)
+        for p, c in zip(self.params, self.copies):
+            if p.dtype != self.dtype or not p.is_contiguous():
+                raise ValueError("parameters must be contiguous and of one type")
+            if c is not None and (c.dtype != torch.bfloat16 or c.shape != p.shape or not c.is_contiguous()):
+                raise ValueError("a copy must be a contiguous bfloat16 tensor of its parameter's shape")
+        self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
+        self.state_bits, self.t = state_bits, 0
+        device = self.params[0].device
+        self.starts: List[int] = []
+        total = 0
+        for p in self.params:
+            self.starts.append(total)
+            total += -(-p.numel() // 256) * 256
+        self.total = total
+        if state_bits == 32:
+            self.m, self.v = (torch.zeros(total, device=device) for _ in range(2))
+            self.m_scale = self.v_scale = None
+        else:
+            self.m = torch.zeros(total, dtype=torch.int8, device=device)
+            self.v = torch.zeros(total, dtype=torch.uint8, device=device)
+            self.m_scale, self.v_scale = (torch.zeros(total // 256, device=device) for _ in range(2))
+        self._list = (_AdamwTensor * len(self.params))()
+        size = self.m.element_size()
+        for e, p, c, a in zip(self._list, self.params, self.copies, self.starts):
+            e.m, e.v, e.n = self.m.data_ptr() + a * size, self.v.data_ptr() + a * size, p.numel()
+            if state_bits == 8:
+                e.m_scale, e.v_scale = (s.data_ptr() + a // 256 * 4 for s in (self.m_scale, self.v_scale))
+
+    def step(self, grads: Optional[Sequence] = None):
+        """One step. grads: a contiguous tensor of each parameter's shape, all
+        of one type (float32 or bfloat16); by default the parameters' .grad.
+        A parameter whose gradient is None stays as it is."""
+        grads = [p.grad for p in self.params] if grads is None else list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError("%d parameters, and %d gradients" % (len(self.params), len(grads)))
+        dtype = None
+        here = self.params[0].device
+        for e, p, c, g, a in zip(self._list, self.params, self.copies, grads, self.starts):
+            if g is None:
+                e.n = 0
+                continue
+            if g.numel() != p.numel() or not g.is_contiguous() or g.device != here:
+                raise ValueError("a gradient must be a contiguous tensor of its parameter's shape, on %s" % here)
+            if dtype is None:
+                dtype = g.dtype
+            if g.dtype != dtype or dtype not in _TYPES:
+                raise ValueError("gradients must be of one type, float32 or bfloat16")
+            # (a parameter's memory may have been replaced since the last step)
+            e.param, e.grad, e.n = p.data_ptr(), g.data_ptr(), p.numel()
+            e.copy = None if c is None else c.data_ptr()
+        if dtype is None:
+            return
+        a = _AdamwArgs(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, self.t + 1, self.state_bits,
+                       _TYPES[self.dtype], _TYPES[dtype], 0)
+        with torch.cuda.device(here):
+            _check(_load().massive_adamw(self._list, len(self._list), ctypes.byref(a), _stream(here)))
+        self.t += 1
+
+    def states(self):
+        """(m, v), flat float32 arrays of what the states stand for (`starts`
+        says where each tensor's begin). With state_bits 32 they are the
+        states themselves."""
+        if self.state_bits == 32:
+            return self.m, self.v
+        m, v = (torch.empty(self.total, device=self.m.device) for _ in range(2))
+        _check(_load().massive_adamw_states(self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr(), self.v_scale.data_ptr(),
+                                            self.total, m.data_ptr(), v.data_ptr(), _stream(m.device)))
+        return m, v
