@@ -330,8 +330,8 @@ int massive_block_mean(const massive_block* block, const void* x, int32_t x_type
                        const massive_row_format* fmt, int32_t d, void* out, int32_t out_type, int64_t out_stride,
                        void* stream);
 
-/* Bytes of workspace of massive_block_mean_backward. */
-int massive_block_mean_workspace(const massive_block* block, int64_t* bytes);
+/* Bytes of workspace of massive_block_mean_backward on rows of d columns. */
+int massive_block_mean_workspace(const massive_block* block, int32_t d, int64_t* bytes);
 
 /* The gradient: dx[j] = sum over the entries of j, in the order of the rows
  * that list it, of dout[i] / (length of row i); plus add[j] for j < add_rows

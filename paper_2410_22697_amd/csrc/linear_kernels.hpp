@@ -124,7 +124,7 @@ struct Staged<T, true, SLOPE, BR> {  // along k: a thread takes chunk t % 8 of r
       if constexpr (SLOPE) one(o.pre + r * o.pre_stride + k, left, z[i]);
     }
   }
-  __device__ __forceinline__ void put(char* lds, const Operand<T>& o, float*) {
+  __device__ __forceinline__ void put(char* lds, const Operand<T>& o, bool, f32x4&) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int r = threadIdx.x / 8 + 32 * i;
@@ -166,8 +166,8 @@ struct Staged<bf16, false, SLOPE, BR> {  // across k: a thread takes 8 k by 4 r,
       if constexpr (SLOPE) one(o.pre + (k1 + j) * o.pre_stride + r, left, z[j]);
     }
   }
-  // sums: if not null, this thread's sums of its four rows over k
-  __device__ __forceinline__ void put(char* lds, const Operand<bf16>& o, float* sums) {
+  // sums: with `count`, this thread's sums of its four rows over k
+  __device__ __forceinline__ void put(char* lds, const Operand<bf16>& o, bool count, f32x4& sums) {
     if (!mine()) return;
     const int r = (threadIdx.x % kRB) * 4, c = threadIdx.x / kRB;
     if constexpr (SLOPE) {
@@ -176,10 +176,10 @@ struct Staged<bf16, false, SLOPE, BR> {  // across k: a thread takes 8 k by 4 r,
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const float g = act_grad<bf16>((float)v[j][q], (float)z[j][q], o.act);
-          if (sums) sums[q] += g;
+          if (count) sums[q] += g;
           v[j][q] = (bf16)g;
         }
-    } else if (sums) {
+    } else if (count) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -219,14 +219,14 @@ struct Staged<float, false, SLOPE, BR> {  // across k in fp32: LDS keeps [k][r],
       if constexpr (SLOPE) one(o.pre + k * o.pre_stride + r, left, z[i]);
     }
   }
-  __device__ __forceinline__ void put(char* lds, const Operand<float>& o, float* sums) {
+  __device__ __forceinline__ void put(char* lds, const Operand<float>& o, bool count, f32x4& sums) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       if constexpr (SLOPE) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[i][q] = act_grad<float>(v[i][q], z[i][q], o.act);
       }
-      if (sums) {
+      if (count) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) sums[q] += v[i][q];
       }
@@ -340,7 +340,7 @@ constexpr int lin_lds_bytes() {
 // is multiplied.
 template <typename T, bool A_ALONG, bool A_SLOPE, bool B_ALONG, int BM, int BN>
 __device__ __forceinline__ void product(Acc<T, BM, BN>& c, char* lds, const Operand<T>& a, int64_t ra, const Operand<T>& b,
-                                        int64_t rb, int64_t k0, int64_t k1, float* sums) {
+                                        int64_t rb, int64_t k0, int64_t k1, bool count, f32x4& sums) {
   typedef Staged<T, A_ALONG, A_SLOPE, BM> SA;
   typedef Staged<T, B_ALONG, false, BN> SB;
   char *la = lds, *lb = lds + BM * 128;
@@ -352,8 +352,8 @@ __device__ __forceinline__ void product(Acc<T, BM, BN>& c, char* lds, const Oper
   }
   for (int64_t k = k0; k < k1; k += Tile<T>::kK) {
     __syncthreads();
-    sa.put(la, a, sums);
-    sb.put(lb, b, nullptr);
+    sa.put(la, a, count, sums);
+    sb.put(lb, b, false, sums);
     __syncthreads();
     if (k + Tile<T>::kK < k1) {
       sa.load(a, ra, k + Tile<T>::kK);
@@ -381,9 +381,10 @@ __global__ __launch_bounds__(kLinNT) void k_linear(LinearForward<T> a, int tiles
   const int64_t r0 = tile / tiles_n * BM;
   const int n0 = (int)(tile % tiles_n) * BN;
   Acc<T, BM, BN> c;
+  f32x4 none = {};
 #pragma unroll 1
   for (int s = 0; s < 2; ++s)
-    product<T, true, false, true, BM, BN>(c, lds, a.x[s], r0, a.w[s], n0, 0, a.x[s].K, nullptr);
+    product<T, true, false, true, BM, BN>(c, lds, a.x[s], r0, a.w[s], n0, 0, a.x[s].K, false, none);
   __syncthreads();
   c.emit(lds, [&](int r, int col, float* z) {
     const int64_t row = r0 + r;
@@ -430,7 +431,8 @@ __global__ __launch_bounds__(kLinNT) void k_linear_dx(LinearDx<T> a, int64_t blo
   at -= s ? a.tiles[0] : 0;
   const int n0 = at * BN;
   Acc<T, BM, BN> c;
-  product<T, true, SLOPE, false, BM, BN>(c, lds, a.dz, r0, a.w[s], n0, 0, a.dz.K, nullptr);
+  f32x4 none = {};
+  product<T, true, SLOPE, false, BM, BN>(c, lds, a.dz, r0, a.w[s], n0, 0, a.dz.K, false, none);
   __syncthreads();
   T* dx = a.dx[s];
   const int64_t stride = a.dx_stride[s];
@@ -467,9 +469,9 @@ __global__ __launch_bounds__(kLinNT) void k_linear_dw(LinearDw<T> a, int64_t blo
   at -= s ? a.tiles[0] : 0;
   const int k0 = at * BN;
   Acc<T, BM, BN> c;
-  float sums[4] = {};
+  f32x4 sums = {};
   const int64_t b = part * a.part, e = min(a.rows, b + a.part);
-  product<T, false, SLOPE, false, BM, BN>(c, lds, a.dz, n0, a.x[s], k0, b, e, bias ? sums : nullptr);
+  product<T, false, SLOPE, false, BM, BN>(c, lds, a.dz, n0, a.x[s], k0, b, e, bias, sums);
   __syncthreads();
   if (bias) {
     // the threads that share four columns add up in order

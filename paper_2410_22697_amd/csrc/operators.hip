@@ -91,6 +91,12 @@ template <typename F>
 int with_type(int32_t type, F f) {
   return type == MASSIVE_F32 ? f((float*)nullptr) : f((bf16*)nullptr);
 }
+// Columns that a lane takes at a time: 16 bytes, or one where a row is shorter.
+template <typename T, typename F>
+int with_cols(T*, int64_t d, F f) {
+  constexpr int q = 16 / sizeof(T);
+  return d >= q ? f(std::integral_constant<int, q>()) : f(std::integral_constant<int, 1>());
+}
 template <typename F>
 int with_bits(int bits, F f) {
   return bits == 8 ? f(std::integral_constant<int, 8>()) : f(std::integral_constant<int, 4>());
@@ -178,7 +184,6 @@ int block_mean(const massive_block* b, const void* x, int32_t x_type, int64_t x_
   if (out_stride < d) REFUSE("out_stride is below d");
   if (!aligned(out, size_of(out_type)) || !aligned(x, x_type == MASSIVE_PACKED ? 4 : size_of(x_type)))
     REFUSE("x or out is not aligned");
-  // the lists' ends are read before their entries: without room for any, none is read
   auto go = [&](auto* s, auto* o, auto bits, auto q) {
     using S = std::remove_pointer_t<decltype(s)>;
     using O = std::remove_pointer_t<decltype(o)>;
@@ -186,47 +191,60 @@ int block_mean(const massive_block* b, const void* x, int32_t x_type, int64_t x_
     return with_team(team, [&](auto t) {
       return launch("massive_block_mean", ms::k_block_mean<S, bits(), O, q(), t()>,
                     std::min(cdiv(b->n, ms::kMeanNT / team), kMostBlocks), ms::kMeanNT, 0, stream, b->indptr, b->indices, b->n,
-                    b->edges, x, b->rows, x_stride, f, (O*)out, out_stride);
+                    (int32_t)b->edges, x, (int32_t)b->rows, x_stride, f, (O*)out, out_stride);
     });
   };
   return with_type(out_type, [&](auto* o) {
     if (x_type == MASSIVE_PACKED)
       return with_bits(fmt->bits, [&](auto bits) { return go((float*)nullptr, o, bits, std::integral_constant<int, 8>()); });
-    if (x_type == MASSIVE_F32)
-      return go((float*)nullptr, o, std::integral_constant<int, 0>(), std::integral_constant<int, 4>());
-    return go((bf16*)nullptr, o, std::integral_constant<int, 0>(), std::integral_constant<int, 8>());
+    return with_type(x_type, [&](auto* s) {
+      return with_cols(s, d, [&](auto q) { return go(s, o, std::integral_constant<int, 0>(), q); });
+    });
   });
 }
 
-// The backward pass's workspace: two lists of pairs, the chunks' counts, the
-// digits' totals, the sources' spans.
+// The backward pass's workspace: two lists of pairs, the entries' shares, the
+// chunks' counts, the digits' totals, the sources' marks, the spans' partial
+// sums.
 struct MeanPlan {
   int passes, bits;        // digits of the sort
   int chunks;
-  int64_t chunk;
-  int64_t keys[2], vals[2], counts, totals, spans, bytes;
+  int span;
+  int64_t chunk, spans;
+  int64_t keys[2], vals[2], shares, counts, totals, marks, partial, bytes;
 };
-MeanPlan mean_plan(const massive_block* b) {
+MeanPlan mean_plan(const massive_block* b, int64_t d) {
   MeanPlan p = {};
   int need = 1;
   while ((int64_t(1) << need) <= b->rows) ++need;  // keys go up to rows
   p.passes = (int)cdiv(need, ms::kDigitBits);
   p.bits = (int)cdiv(need, p.passes);
-  p.chunk = std::max<int64_t>(ms::kChunkLeast, round_up(cdiv(b->edges, ms::kChunksMost), MS_WAVE));
+  p.chunk = std::max<int64_t>(MS_WAVE, round_up(cdiv(b->edges, ms::kChunksMost), MS_WAVE));
   p.chunks = (int)cdiv(b->edges, p.chunk);
+  p.span = b->edges <= (1 << 16) ? 16 : b->edges <= (1 << 18) ? 32 : 64;
+  p.spans = cdiv(b->edges, p.span);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t here = at;
     at += round_up(bytes, 16);
     return here;
   };
-  for (int i = 0; i < 2; ++i) p.keys[i] = take(4 * b->edges);
-  for (int i = 0; i < 2; ++i) p.vals[i] = take(4 * b->edges);
+  const int64_t list = 4 * round_up(b->edges, ms::kMeanAhead);  // read in whole steps
+  for (int i = 0; i < 2; ++i) p.keys[i] = take(list);
+  for (int i = 0; i < 2; ++i) p.vals[i] = take(list);
+  p.shares = take(list);
   p.counts = take(4 * (int64_t)p.chunks << p.bits);
   p.totals = take(int64_t(4) << p.bits);
-  p.spans = take(8 * b->rows);
+  p.marks = take(b->rows);
+  p.partial = take(p.spans * 2 * d * 4);
   p.bytes = at;
   return p;
+}
+
+// Whether the gradient takes the one-launch form, which reads every index for
+// each source.
+bool few(const massive_block* b) {
+  return b->edges <= ms::kFewEdges && b->n <= ms::kFewRows && b->rows <= ms::kFewSources;
 }
 
 int block_mean_backward(const massive_block* b, const void* dout, int32_t type, int64_t dout_stride, int32_t d,
@@ -243,7 +261,18 @@ int block_mean_backward(const massive_block* b, const void* dout, int32_t type, 
   if (dx_stride < d || (b->n > 0 && dout_stride < d)) REFUSE("dout_stride or dx_stride is below d");
   const int size = size_of(type);
   if (!aligned(dout, size) || !aligned(add, size) || !aligned(dx, size)) REFUSE("dout, add or dx is not aligned");
-  const MeanPlan p = mean_plan(b);
+  if (few(b))
+    return with_type(type, [&](auto* t) {
+      using D = std::remove_pointer_t<decltype(t)>;
+      return with_cols(t, d, [&](auto q) {
+        return launch("massive_block_mean_backward",
+                      add_rows > 0 ? ms::k_block_mean_backward_few<D, q(), true> : ms::k_block_mean_backward_few<D, q(), false>,
+                      cdiv(b->rows, ms::kMeanNT / MS_WAVE), ms::kMeanNT, 0, stream, b->indptr, b->indices, (int32_t)b->n,
+                      (int32_t)(b->n > 0 ? b->edges : 0), (int32_t)b->rows, (const D*)dout, dout_stride, d, (const D*)add, add_stride,
+                      (int32_t)add_rows, (D*)dx, dx_stride);
+      });
+    });
+  const MeanPlan p = mean_plan(b, d);
   if (!workspace || workspace_bytes < p.bytes)
     return call_error(MASSIVE_ECAPACITY, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0),
                       (long long)p.bytes);
@@ -251,45 +280,53 @@ int block_mean_backward(const massive_block* b, const void* dout, int32_t type, 
   char* w = (char*)workspace;
   uint32_t* keys[2] = {(uint32_t*)(w + p.keys[0]), (uint32_t*)(w + p.keys[1])};
   int32_t* vals[2] = {(int32_t*)(w + p.vals[0]), (int32_t*)(w + p.vals[1])};
+  float *shares = (float*)(w + p.shares), *partial = (float*)(w + p.partial);
   int32_t *counts = (int32_t*)(w + p.counts), *totals = (int32_t*)(w + p.totals);
-  int2* spans = (int2*)(w + p.spans);
+  uint8_t* marks = (uint8_t*)(w + p.marks);
   const char* what = "massive_block_mean_backward";
   const int nt = ms::kSortWaves * MS_WAVE;
   // without a row no edge belongs to one
   const int chunks = b->n > 0 ? p.chunks : 0;
+  const int32_t edges = chunks > 0 ? (int32_t)b->edges : 0, rows = (int32_t)b->rows, chunk = (int32_t)p.chunk;
   const int64_t sort_blocks = cdiv(std::max(chunks, 1), ms::kSortWaves);
   const size_t digits = sizeof(int32_t) << p.bits;
-  if (int rc = launch(what, ms::k_edges, std::max(sort_blocks, std::min<int64_t>(cdiv(b->rows, nt), 512)), nt,
-                      ms::kSortWaves * digits, stream, b->indptr, b->indices, b->n, b->edges, b->rows, p.chunk, chunks, p.bits,
-                      keys[0], vals[0], counts, spans))
+  if (int rc = launch(what, ms::k_edges, std::max(sort_blocks, std::min<int64_t>(cdiv(b->rows, 4 * nt), 512)), nt,
+                      ms::kSortWaves * digits, stream, b->indptr, b->indices, (int32_t)b->n, edges, rows, chunk, chunks, p.bits,
+                      keys[0], vals[0], counts, (uint32_t*)marks))
     return rc;
   int at = 0;
   for (int pass = 0; chunks > 0 && pass < p.passes; ++pass) {
     const int shift = pass * p.bits;
     if (pass > 0)
-      if (int rc = launch(what, ms::k_digits, sort_blocks, nt, ms::kSortWaves * digits, stream, keys[at], b->edges, p.chunk, chunks,
-                          shift, p.bits, counts))
+      if (int rc = launch(what, ms::k_digits, sort_blocks, nt, ms::kSortWaves * digits, stream, keys[at], edges, chunk, chunks, shift,
+                          p.bits, counts))
         return rc;
-    if (int rc = launch(what, ms::k_places, cdiv(1 << p.bits, MS_WAVE), ms::kPlacesWaves * MS_WAVE, 0, stream, counts, chunks,
-                        p.bits, totals))
+    if (int rc = launch(what, ms::k_places, cdiv(1 << p.bits, ms::kPlacesDigits), ms::kPlacesDigits * ms::kPlacesRuns, 0, stream,
+                        counts, chunks, p.bits, totals))
       return rc;
-    if (int rc = launch(what, ms::k_move, sort_blocks, nt, (1 + ms::kSortWaves) * digits, stream, keys[at], vals[at], b->edges,
-                        p.chunk, chunks, shift, p.bits, counts, totals, keys[1 - at], vals[1 - at]))
+    const bool last = pass == p.passes - 1;
+    if (int rc = launch(what, last ? ms::k_move<true> : ms::k_move<false>, sort_blocks, nt, (1 + ms::kSortWaves) * digits, stream,
+                        keys[at], vals[at], edges, chunk, chunks, shift, p.bits, counts, totals, keys[1 - at], vals[1 - at],
+                        b->indptr, rows, shares, marks))
       return rc;
     at = 1 - at;
   }
-  if (chunks > 0)
-    if (int rc = launch(what, ms::k_spans, std::min<int64_t>(cdiv(b->edges, ms::kMeanNT), 4096), ms::kMeanNT, 0, stream, keys[at],
-                        b->edges, b->rows, spans))
-      return rc;
   return with_type(type, [&](auto* t) {
     using D = std::remove_pointer_t<decltype(t)>;
-    constexpr int q = sizeof(D) == 4 ? 4 : 8;
-    const int team = team_of(d, q);
-    return with_team(team, [&](auto lanes) {
-      return launch(what, ms::k_block_mean_backward<D, q, lanes()>, std::min(cdiv(b->rows, ms::kMeanNT / team), kMostBlocks),
-                    ms::kMeanNT, 0, stream, spans, vals[at], b->indptr, b->edges, b->rows, (const D*)dout, dout_stride, d,
-                    (const D*)add, add_stride, add_rows, (D*)dx, dx_stride);
+    return with_cols(t, d, [&](auto q) {
+      const int team = team_of(d, q());
+      return with_team(team, [&](auto lanes) {
+        const int teams = ms::kMeanNT / team;
+        const int span_blocks = edges > 0 ? (int)cdiv(p.spans, teams) : 0;
+        // rows that nobody lists: a few turns a block
+        const int64_t blocks = span_blocks + std::min<int64_t>(cdiv(b->rows, 4 * teams), 8192);
+        const int rc = launch(what, add_rows > 0 ? ms::k_block_mean_backward<D, q(), lanes(), true> : ms::k_block_mean_backward<D, q(), lanes(), false>,
+                              blocks, ms::kMeanNT, 0, stream, keys[at], vals[at], shares, marks, edges, rows, (const D*)dout, dout_stride, d,
+                              (const D*)add, add_stride, (int32_t)add_rows, (D*)dx, dx_stride, partial, p.span, span_blocks);
+        if (rc || edges <= p.span) return rc;
+        return launch(what, ms::k_block_mean_join<D, q(), lanes()>, cdiv(p.spans, teams), ms::kMeanNT, 0, stream, keys[at],
+                      edges, rows, d, p.span, partial, (D*)dx, dx_stride);
+      });
     });
   });
 }
@@ -522,10 +559,11 @@ int massive_block_mean(const massive_block* block, const void* x, int32_t x_type
   return block_mean(block, x, x_type, x_stride, fmt, d, out, out_type, out_stride, stream);
 }
 
-int massive_block_mean_workspace(const massive_block* block, int64_t* bytes) {
+int massive_block_mean_workspace(const massive_block* block, int32_t d, int64_t* bytes) {
   if (!bytes) REFUSE("bytes is NULL");
   if (int rc = check_block(block)) return rc;
-  *bytes = mean_plan(block).bytes;
+  if (d < 1) REFUSE("d must be at least 1");
+  *bytes = few(block) ? 0 : mean_plan(block, d).bytes;
   return MASSIVE_OK;
 }
 

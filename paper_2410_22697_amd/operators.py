@@ -66,7 +66,7 @@ def _load():
         lib.massive_pack_rows.argtypes = [p(_Format), _vp, _i32, _i64, _i64, _vp, _vp, _i64, _vp]
         lib.massive_unpack_rows.argtypes = [p(_Format), _vp, _i64, _vp, _i64, _vp, _i32, _i64, _vp]
         lib.massive_block_mean.argtypes = [p(_Block), _vp, _i32, _i64, p(_Format), _i32, _vp, _i32, _i64, _vp]
-        lib.massive_block_mean_workspace.argtypes = [p(_Block), p(_i64)]
+        lib.massive_block_mean_workspace.argtypes = [p(_Block), _i32, p(_i64)]
         lib.massive_block_mean_backward.argtypes = [p(_Block), _vp, _i32, _i64, _i32, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp]
         lib.massive_linear.argtypes = [p(_LinearArgs), _vp]
         lib.massive_linear_workspace.argtypes = [p(_LinearGrads), p(_i64)]
@@ -262,11 +262,11 @@ def block_mean_backward(dout, indptr, indices, rows: int, add=None):
     lib = _load()
     dx = torch.empty((int(rows), d), dtype=dout.dtype, device=dout.device)
     need = _i64()
-    _check(lib.massive_block_mean_workspace(ctypes.byref(b), ctypes.byref(need)))
-    work = torch.empty(max(need.value, 16), dtype=torch.uint8, device=dout.device)
+    _check(lib.massive_block_mean_workspace(ctypes.byref(b), d, ctypes.byref(need)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=dout.device) if need.value else None
     _check(lib.massive_block_mean_backward(ctypes.byref(b), dout.data_ptr(), _TYPES[dout.dtype], stride, d,
                                            add.data_ptr() if add_rows else None, add_stride, add_rows, dx.data_ptr(), d,
-                                           work.data_ptr(), work.numel(), _stream(dout.device)))
+                                           _ptr(work), need.value, _stream(dout.device)))
     return dx
 
 

@@ -59,7 +59,7 @@ def test_rows():
     assert call(ctypes.byref(f), None, 0, None, 0, None, 0, 16, None) == OK
 
 
-def block(indptr=P, indices=P, n=4, edges=8, rows=10):
+def block(indptr=P, indices=P, n=4, edges=5000, rows=10):
     return operators._Block(indptr, indices, n, edges, rows)
 
 
@@ -72,7 +72,7 @@ def test_block(bad, word):
     b = block(**bad)
     size = ctypes.c_int64()
     refused(lib().massive_block_mean(ctypes.byref(b), P, 0, 16, None, 16, P, 0, 16, None), word)
-    refused(lib().massive_block_mean_workspace(ctypes.byref(b), ctypes.byref(size)), word)
+    refused(lib().massive_block_mean_workspace(ctypes.byref(b), 16, ctypes.byref(size)), word)
     refused(lib().massive_block_mean_backward(ctypes.byref(b), P, 0, 16, 16, None, 0, 0, P, 16, P, 1 << 40, None), word)
 
 
@@ -91,8 +91,9 @@ def test_block_mean():
 
 def test_block_mean_backward():
     b, size = block(), ctypes.c_int64()
-    assert lib().massive_block_mean_workspace(ctypes.byref(b), ctypes.byref(size)) == OK and size.value > 0
-    refused(lib().massive_block_mean_workspace(ctypes.byref(b), None), "NULL")
+    assert lib().massive_block_mean_workspace(ctypes.byref(b), 16, ctypes.byref(size)) == OK and size.value > 0
+    refused(lib().massive_block_mean_workspace(ctypes.byref(b), 16, None), "NULL")
+    refused(lib().massive_block_mean_workspace(ctypes.byref(b), 0, ctypes.byref(size)), "d must")
     call = lib().massive_block_mean_backward
     need = size.value
     for args, word, code in (((P, 5, 16, 16, None, 0, 0, P, 16, P, need), "type", EINVAL), ((P, 0, 15, 16, None, 0, 0, P, 16, P, need), "stride", EINVAL),
