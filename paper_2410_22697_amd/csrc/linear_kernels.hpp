@@ -69,6 +69,35 @@ __device__ __forceinline__ float act_grad(float g, float z, int act) {
   return g * (q + (s > 0.0f ? z * s : 0.0f));
 }
 
+// The same for several values: the activation is the same for all of them.
+template <typename T>
+__device__ __forceinline__ void act_values(float (&z)[8], int act) {
+  if (act == kActNone) return;
+  if (act == kActRelu) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) z[q] = act_value<T>(z[q], kActRelu);
+  } else if (act == kActGelu) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) z[q] = act_value<T>(z[q], kActGelu);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) z[q] = act_value<T>(z[q], kActSilu);
+  }
+}
+template <typename T, int Q>
+__device__ __forceinline__ void act_grads(cols_t<T, Q>& g, const cols_t<T, Q>& z, int act) {
+  if (act == kActRelu) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) g[q] = (T)act_grad<T>((float)g[q], (float)z[q], kActRelu);
+  } else if (act == kActGelu) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) g[q] = (T)act_grad<T>((float)g[q], (float)z[q], kActGelu);
+  } else {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) g[q] = (T)act_grad<T>((float)g[q], (float)z[q], kActSilu);
+  }
+}
+
 // ---------------------------------------------------------------- operands
 // One operand of a product: element (r, k), r below R, k below K, is at
 // p[r * stride + k] (along k) or p[k * stride + r] (across k); with pre, the
@@ -128,10 +157,7 @@ struct Staged<T, true, SLOPE, BR> {  // along k: a thread takes chunk t % 8 of r
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int r = threadIdx.x / 8 + 32 * i;
-      if constexpr (SLOPE) {
-#pragma unroll
-        for (int q = 0; q < kV; ++q) v[i][q] = (T)act_grad<T>((float)v[i][q], (float)z[i][q], o.act);
-      }
+      if constexpr (SLOPE) act_grads<T, kV>(v[i], z[i], o.act);
       *reinterpret_cast<u32x4*>(lds + chunk_at(r, threadIdx.x % 8)) = __builtin_bit_cast(u32x4, v[i]);
     }
   }
@@ -222,10 +248,7 @@ struct Staged<float, false, SLOPE, BR> {  // across k in fp32: LDS keeps [k][r],
   __device__ __forceinline__ void put(char* lds, const Operand<float>& o, bool count, f32x4& sums) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      if constexpr (SLOPE) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[i][q] = act_grad<float>(v[i][q], z[i][q], o.act);
-      }
+      if constexpr (SLOPE) act_grads<float, 4>(v[i], z[i], o.act);
       if (count) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) sums[q] += v[i][q];
@@ -374,6 +397,27 @@ struct LinearForward {
   int n, act;
 };
 
+// The epilogue of eight neighbouring outputs of a row: z holds their products.
+template <typename T>
+__device__ __forceinline__ void linear_finish(const LinearForward<T>& a, int64_t row, int col, float (&z)[8]) {
+  const int left = a.n - col;
+  if (left <= 0) return;
+  float t[8];
+  if (a.bias) {
+    load_cols<T, 8>(a.bias + col, left, t);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) z[q] += t[q];
+  }
+  if (a.pre) store_cols<T, 8>(a.pre + row * a.pre_stride + col, left, z);
+  act_values<T>(z, a.act);
+  if (a.residual) {
+    load_cols<T, 8>(a.residual + row * a.residual_stride + col, left, t);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) z[q] += t[q];
+  }
+  store_cols<T, 8>(a.y + row * a.y_stride + col, left, z);
+}
+
 template <typename T, int BM, int BN>
 __global__ __launch_bounds__(kLinNT) void k_linear(LinearForward<T> a, int tiles_n, int64_t blocks) {
   __shared__ __align__(16) char lds[lin_lds_bytes<T, BM, BN>()];
@@ -386,27 +430,8 @@ __global__ __launch_bounds__(kLinNT) void k_linear(LinearForward<T> a, int tiles
   for (int s = 0; s < 2; ++s)
     product<T, true, false, true, BM, BN>(c, lds, a.x[s], r0, a.w[s], n0, 0, a.x[s].K, false, none);
   __syncthreads();
-  c.emit(lds, [&](int r, int col, float* z) {
-    const int64_t row = r0 + r;
-    const int left = a.n - n0 - col;
-    if (row >= a.rows || left <= 0) return;
-    float t[8];
-    if (a.bias) {
-      load_cols<T, 8>(a.bias + n0 + col, left, t);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) z[q] += t[q];
-    }
-    if (a.pre) store_cols<T, 8>(a.pre + row * a.pre_stride + n0 + col, left, z);
-    if (a.act != kActNone) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) z[q] = act_value<T>(z[q], a.act);
-    }
-    if (a.residual) {
-      load_cols<T, 8>(a.residual + row * a.residual_stride + n0 + col, left, t);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) z[q] += t[q];
-    }
-    store_cols<T, 8>(a.y + row * a.y_stride + n0 + col, left, z);
+  c.emit(lds, [&](int r, int col, float (&z)[8]) {
+    if (r0 + r < a.rows) linear_finish(a, r0 + r, n0 + col, z);
   });
 }
 

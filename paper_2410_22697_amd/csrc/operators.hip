@@ -15,6 +15,7 @@
 #include "block_kernels.hpp"
 #include "call_error.hpp"
 #include "linear_kernels.hpp"
+#include "linear_stream.hpp"
 #include "rows_kernels.hpp"
 
 namespace {
@@ -361,6 +362,40 @@ int with_tile(int64_t rows, int64_t cols, F f) {
   return f(std::integral_constant<int, 64>(), std::integral_constant<int, 64>());
 }
 
+// The streaming form's shape for n outputs from `chunks` chunks of k: blocks of
+// 32 outputs that a wave accumulates, and whether their weights stay in LDS.
+struct StreamPlan {
+  int nb;
+  bool resident;
+  int lds_weights, lds;
+};
+StreamPlan stream_plan(int64_t n, int64_t chunks) {
+  StreamPlan p;
+  auto bytes = [&](int nb) { return chunks * nb * ms::kStreamBlockBytes; };
+  p.nb = n <= 64 ? 2 : n <= 128 || bytes(8) > ms::kStreamLds ? 4 : 8;
+  p.resident = bytes(p.nb) <= ms::kStreamLds;
+  p.lds_weights = (int)(p.resident ? bytes(p.nb) : 2 * p.nb * ms::kStreamBlockBytes);
+  p.lds = p.lds_weights + ms::kStreamNT / MS_WAVE * ms::kStreamTurn + p.nb * 32 * 4;  // weights, turns, bias
+  return p;
+}
+// Blocks: every CU's share once, in whole rounds of the output groups on the
+// eight XCDs.
+int64_t stream_blocks(const StreamPlan& p, int64_t rows, int groups) {
+  const int64_t per_cu = p.lds <= (80 << 10) ? 2 : 1;
+  const int64_t most = std::max<int64_t>(1, 256 * per_cu / 8 / groups) * groups * 8;
+  return std::min(most, round_up(cdiv(rows, ms::kStreamRows), 8) * groups);
+}
+constexpr int64_t kStreamLeast = 8192;  // rows
+
+// f(blocks of 32 outputs, whether they stay), both as types.
+template <typename F>
+int with_stream(const StreamPlan& p, F f) {
+  using std::integral_constant;
+  if (p.nb == 8) return f(integral_constant<int, 8>(), std::true_type());
+  if (p.nb == 4) return p.resident ? f(integral_constant<int, 4>(), std::true_type()) : f(integral_constant<int, 4>(), std::false_type());
+  return p.resident ? f(integral_constant<int, 2>(), std::true_type()) : f(integral_constant<int, 2>(), std::false_type());
+}
+
 template <typename T>
 int linear(const massive_linear_args* a, void* stream) {
   ms::LinearForward<T> f;
@@ -379,6 +414,16 @@ int linear(const massive_linear_args* a, void* stream) {
   f.rows = a->rows;
   f.n = a->n;
   f.act = a->act;
+  // a segment of under 16 bytes cannot be read in whole vectors
+  constexpr int kV = 16 / sizeof(T);
+  if (a->rows >= kStreamLeast && a->k >= kV && (a->k_second == 0 || a->k_second >= kV)) {
+    const StreamPlan p = stream_plan(a->n, cdiv(a->k * sizeof(T), 256) + cdiv(a->k_second * sizeof(T), 256));
+    const int groups = (int)cdiv(a->n, p.nb * 32);
+    return with_stream(p, [&](auto nb, auto resident) {
+      return launch("massive_linear", ms::k_linear_stream<T, nb(), resident()>, stream_blocks(p, a->rows, groups), ms::kStreamNT, p.lds,
+                    stream, f, groups, p.lds_weights);
+    });
+  }
   return with_tile(a->rows, a->n, [&](auto bm, auto bn) {
     const int tiles_n = (int)cdiv(a->n, bn());
     const int64_t blocks = cdiv(a->rows, bm()) * tiles_n;
@@ -431,7 +476,17 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
     f.k[0] = a->k;
     f.k[1] = a->k_second;
     const int64_t cols = (a->dx ? k[0] : 0) + (a->dx_second ? k[1] : 0);
-    const int rc = with_tile(a->rows, cols, [&](auto bm, auto bn) {
+    constexpr int kV = 16 / sizeof(T);
+    const bool streams = a->rows >= kStreamLeast && a->n >= kV;
+    const StreamPlan p = stream_plan(std::max(a->dx ? k[0] : 0, a->dx_second ? k[1] : 0), cdiv(a->n * sizeof(T), 256));
+    auto go_stream = [&](auto nb, auto resident) {
+      for (int s = 0; s < 2; ++s) f.tiles[s] = f.dx[s] ? (int)cdiv(k[s], nb() * 32) : 0;
+      const int groups = f.tiles[0] + f.tiles[1];
+      const int64_t blocks = stream_blocks(p, a->rows, groups);
+      return slope ? launch("massive_linear_backward", ms::k_linear_dx_stream<T, true, nb(), resident()>, blocks, ms::kStreamNT, p.lds, stream, f, groups, p.lds_weights)
+                   : launch("massive_linear_backward", ms::k_linear_dx_stream<T, false, nb(), resident()>, blocks, ms::kStreamNT, p.lds, stream, f, groups, p.lds_weights);
+    };
+    const int rc = streams ? with_stream(p, go_stream) : with_tile(a->rows, cols, [&](auto bm, auto bn) {
       for (int s = 0; s < 2; ++s) f.tiles[s] = f.dx[s] ? (int)cdiv(k[s], bn()) : 0;
       const int64_t blocks = cdiv(a->rows, bm()) * (f.tiles[0] + f.tiles[1]);
       if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");

@@ -82,33 +82,45 @@ def _check(rc):
         raise MassiveError(rc, _lib.massive_last_error(None).decode())
 
 
-def _stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+def _stream(device: int) -> int:
+    """The current stream of a GPU, as the library takes it."""
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _on_gpu(*tensors):
-    """All tensors given lie on the current GPU: the library launches there."""
+def _on_gpu(*tensors) -> int:
+    """The GPU on which all tensors given (not None) lie, which must be the current one: the library launches there."""
+    there = None
     for t in tensors:
-        if t is not None and not t.is_cuda:
-            raise ValueError("operators take device (cuda) tensors, not one on %s" % t.device)
+        if t is not None:
+            at = t.get_device()
+            if at < 0 or not t.is_cuda:
+                raise ValueError("operators take device (cuda) tensors, not one on %s" % t.device)
+            if there is not None and at != there:
+                raise ValueError("tensors lie on cuda:%d and on cuda:%d" % (there, at))
+            there = at
     here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != here:
-            raise ValueError("a tensor lies on %s, and cuda:%d is the current device" % (t.device, here))
+    if there is not None and there != here:
+        raise ValueError("a tensor lies on cuda:%d, and cuda:%d is the current device" % (there, here))
+    return here
 
 
 def _matrix(t, name, cols=None, rows=None, dtype=None) -> int:
     """The row stride of a 2-d tensor whose rows are contiguous; checks its shape and type."""
-    if t.dim() != 2 or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be a 2-d tensor with contiguous rows" % name)
+    if t.dim() != 2:
+        raise ValueError("%s must be a 2-d tensor" % name)
     if t.dtype not in _TYPES or (dtype is not None and t.dtype != dtype):
         raise ValueError("%s is %s, and must be %s" % (name, t.dtype, dtype or "float32 or bfloat16"))
-    if (cols is not None and t.shape[1] != cols) or (rows is not None and t.shape[0] != rows):
-        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), ("any" if rows is None else rows, "any" if cols is None else cols)))
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    n, d = t.shape
+    if (cols is not None and d != cols) or (rows is not None and n != rows):
+        raise ValueError("%s has shape %s, expected %s" % (name, (n, d), ("any" if rows is None else rows, "any" if cols is None else cols)))
+    if n <= 1 and d <= 1 or not n or not d:
+        return d
+    step, one = t.stride()
+    if d > 1 and one != 1:
+        raise ValueError("%s must have contiguous rows" % name)
+    if n > 1 and step < d:
         raise ValueError("%s has rows that overlap" % name)
-    # a row count of one or none leaves the stride open
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return step if n > 1 else d  # of a single row the stride says nothing
 
 
 def _ids(t, name) -> int:
@@ -156,7 +168,7 @@ def pack_rows(x, fmt: RowFormat, out=None, slots=None):
     `out`, or to its first n rows without slots. Without out, a new table of n
     rows. Returns the table."""
     stride = _matrix(x, "x", cols=fmt.d)
-    _on_gpu(x, slots)
+    here = _on_gpu(x, slots)
     n = x.shape[0]
     if slots is not None and _ids(slots, "slots") != n:
         raise ValueError("x has %d rows, and there are %d slots" % (n, slots.numel()))
@@ -170,7 +182,7 @@ def pack_rows(x, fmt: RowFormat, out=None, slots=None):
     if slots is None and rows < n:
         raise ValueError("out has %d rows, and x %d" % (rows, n))
     _check(_load().massive_pack_rows(ctypes.byref(fmt.c), x.data_ptr(), _TYPES[x.dtype], stride, n,
-                                     None if slots is None else slots.data_ptr(), out.data_ptr(), rows, _stream(x.device)))
+                                     None if slots is None else slots.data_ptr(), out.data_ptr(), rows, _stream(here)))
     return out
 
 
@@ -179,16 +191,15 @@ def unpack_rows(table, fmt: RowFormat, index=None, dtype=torch.float32, out=None
     every row without an index, of a table on the GPU or in pinned memory, to
     a new tensor of dtype, or to `out`."""
     rows = _table(table, fmt, pinned=True)
-    _on_gpu(index, out)
+    here = _on_gpu(index, out)
     n = rows if index is None else _ids(index, "index")
     if out is None:
         if dtype not in _TYPES:
             raise ValueError("dtype must be float32 or bfloat16, not %s" % dtype)
-        device = table.device if table.is_cuda else torch.device("cuda", torch.cuda.current_device())
-        out = torch.empty((n, fmt.d), dtype=dtype, device=device)
+        out = torch.empty((n, fmt.d), dtype=dtype, device="cuda")
     stride = _matrix(out, "out", cols=fmt.d, rows=n)
     _check(_load().massive_unpack_rows(ctypes.byref(fmt.c), table.data_ptr(), rows, None if index is None else index.data_ptr(), n,
-                                       out.data_ptr(), _TYPES[out.dtype], stride, _stream(out.device)))
+                                       out.data_ptr(), _TYPES[out.dtype], stride, _stream(here)))
     return out
 
 
@@ -201,7 +212,7 @@ def _block(indptr, indices, rows) -> _Block:
 
 
 def _block_mean(x, indptr, indices, fmt, dtype):
-    _on_gpu(indptr, indices)
+    here = _on_gpu(indptr, indices)
     if fmt is not None:
         rows, d, kind, stride, c = _table(x, fmt, "x", pinned=True), fmt.d, PACKED, 0, ctypes.byref(fmt.c)
         dtype = dtype or torch.float32
@@ -213,9 +224,9 @@ def _block_mean(x, indptr, indices, fmt, dtype):
     if dtype not in _TYPES:
         raise ValueError("dtype must be float32 or bfloat16, not %s" % dtype)
     b = _block(indptr, indices, rows)
-    out = torch.empty((b.n, d), dtype=dtype, device=indptr.device)
+    out = torch.empty((b.n, d), dtype=dtype, device="cuda")
     _check(_load().massive_block_mean(ctypes.byref(b), x.data_ptr(), kind, stride, c, d, out.data_ptr(), _TYPES[dtype], d,
-                                      _stream(out.device)))
+                                      _stream(here)))
     return out
 
 
@@ -250,7 +261,7 @@ def block_mean_backward(dout, indptr, indices, rows: int, add=None):
     dout[i] / length(i) over the rows i that list j, in their order; plus
     add[j] for the first len(add) rows."""
     stride = _matrix(dout, "dout")
-    _on_gpu(dout, indptr, indices, add)
+    here = _on_gpu(dout, indptr, indices, add)
     b = _block(indptr, indices, rows)
     if dout.shape[0] != b.n:
         raise ValueError("dout has %d rows, and the block %d" % (dout.shape[0], b.n))
@@ -266,7 +277,7 @@ def block_mean_backward(dout, indptr, indices, rows: int, add=None):
     work = torch.empty(need.value, dtype=torch.uint8, device=dout.device) if need.value else None
     _check(lib.massive_block_mean_backward(ctypes.byref(b), dout.data_ptr(), _TYPES[dout.dtype], stride, d,
                                            add.data_ptr() if add_rows else None, add_stride, add_rows, dx.data_ptr(), d,
-                                           _ptr(work), need.value, _stream(dout.device)))
+                                           _ptr(work), need.value, _stream(here)))
     return dx
 
 
@@ -278,24 +289,20 @@ def _activation(act) -> int:
 
 
 def _layer(x, weight, x2):
-    """Checks the inputs and weights of a layer; (rows, n, k, k2)."""
-    _matrix(x, "x")
+    """Checks the inputs and weights of a layer; (rows, n, k, k2) and the strides of x, x2 and weight."""
+    x_stride = _matrix(x, "x")
     rows, k = x.shape
-    k2 = 0
+    k2 = x2_stride = 0
     if x2 is not None:
-        _matrix(x2, "x2", rows=rows, dtype=x.dtype)
+        x2_stride = _matrix(x2, "x2", rows=rows, dtype=x.dtype)
         k2 = x2.shape[1]
-    _matrix(weight, "weight", cols=k + k2, dtype=x.dtype)
-    return rows, weight.shape[0], k, k2
+    w_stride = _matrix(weight, "weight", cols=k + k2, dtype=x.dtype)
+    return rows, weight.shape[0], k, k2, x_stride, x2_stride, w_stride
 
 
 def _vector(t, name, n, dtype):
     if t.dim() != 1 or t.numel() != n or t.dtype != dtype or not t.is_contiguous():
         raise ValueError("%s must be a contiguous 1-d tensor of %d values of %s" % (name, n, dtype))
-
-
-def _stride(t, cols):
-    return cols if t is None or t.shape[0] <= 1 else t.stride(0)
 
 
 def _ptr(t):
@@ -304,18 +311,17 @@ def _ptr(t):
 
 def _linear(x, weight, bias, act, residual, x2, save_pre):
     code = _activation(act)
-    rows, n, k, k2 = _layer(x, weight, x2)
-    _on_gpu(x, weight, bias, residual, x2)
+    rows, n, k, k2, x_stride, x2_stride, w_stride = _layer(x, weight, x2)
+    here = _on_gpu(x, weight, bias, residual, x2)
+    dtype = x.dtype
     if bias is not None:
-        _vector(bias, "bias", n, x.dtype)
-    if residual is not None:
-        _matrix(residual, "residual", cols=n, rows=rows, dtype=x.dtype)
-    y = torch.empty((rows, n), dtype=x.dtype, device=x.device)
+        _vector(bias, "bias", n, dtype)
+    res_stride = 0 if residual is None else _matrix(residual, "residual", cols=n, rows=rows, dtype=dtype)
+    y = torch.empty((rows, n), dtype=dtype, device="cuda")
     pre = torch.empty_like(y) if save_pre else None
     a = _LinearArgs(x.data_ptr(), _ptr(x2), weight.data_ptr(), _ptr(bias), _ptr(residual), y.data_ptr(), _ptr(pre), rows,
-                    _stride(x, k), _stride(x2, k2), _stride(weight, k + k2), _stride(residual, n), n, n, n, k, k2,
-                    _TYPES[x.dtype], code)
-    _check(_load().massive_linear(ctypes.byref(a), _stream(x.device)))
+                    x_stride, x2_stride, w_stride, res_stride, n, n, n, k, k2, _TYPES[dtype], code)
+    _check(_load().massive_linear(ctypes.byref(a), _stream(here)))
     return y, pre
 
 
@@ -360,26 +366,25 @@ def linear_backward(dy, x, weight, act: str = "none", pre=None, x2=None, bias: b
     residual, y serves as well), None for act "none". The residual's gradient
     is dy."""
     code = _activation(act)
-    rows, n, k, k2 = _layer(x, weight, x2)
-    _on_gpu(dy, x, weight, x2, pre)
-    _matrix(dy, "dy", cols=n, rows=rows, dtype=x.dtype)
+    rows, n, k, k2, x_stride, x2_stride, w_stride = _layer(x, weight, x2)
+    here = _on_gpu(dy, x, weight, x2, pre)
+    dtype = x.dtype
+    dy_stride = _matrix(dy, "dy", cols=n, rows=rows, dtype=dtype)
     if (pre is None) != (code == 0):
         raise ValueError("pre goes with an activation, and only with one")
-    if pre is not None:
-        _matrix(pre, "pre", cols=n, rows=rows, dtype=x.dtype)
-    new = lambda *shape: torch.empty(shape, dtype=x.dtype, device=x.device)  # noqa: E731
+    pre_stride = 0 if pre is None else _matrix(pre, "pre", cols=n, rows=rows, dtype=dtype)
+    new = lambda *shape: torch.empty(shape, dtype=dtype, device="cuda")  # noqa: E731
     dx = new(rows, k) if need_dx else None
     dx2 = new(rows, k2) if need_dx2 and x2 is not None else None
     dw = new(n, k + k2) if need_dw else None
     db = new(n) if bias else None
     g = _LinearGrads(dy.data_ptr(), _ptr(pre), x.data_ptr(), _ptr(x2), weight.data_ptr(), _ptr(dx), _ptr(dx2), _ptr(dw), _ptr(db),
-                     rows, _stride(dy, n), _stride(pre, n), _stride(x, k), _stride(x2, k2), _stride(weight, k + k2), k, k2, k + k2,
-                     n, k, k2, _TYPES[x.dtype], code)
+                     rows, dy_stride, pre_stride, x_stride, x2_stride, w_stride, k, k2, k + k2, n, k, k2, _TYPES[dtype], code)
     lib = _load()
     need = _i64()
     _check(lib.massive_linear_workspace(ctypes.byref(g), ctypes.byref(need)))
-    work = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
-    _check(lib.massive_linear_backward(ctypes.byref(g), _ptr(work), need.value, _stream(x.device)))
+    work = torch.empty(need.value, dtype=torch.uint8, device="cuda") if need.value else None
+    _check(lib.massive_linear_backward(ctypes.byref(g), _ptr(work), need.value, _stream(here)))
     return dx, dx2, dw, db
 
 
@@ -444,13 +449,13 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ValueError("%d parameters, and %d gradients" % (len(self.params), len(grads)))
         dtype = None
-        here = self.params[0].device
+        here = _on_gpu(*self.params)
         for e, p, c, g, a in zip(self._list, self.params, self.copies, grads, self.starts):
             if g is None:
                 e.n = 0
                 continue
-            if g.numel() != p.numel() or not g.is_contiguous() or g.device != here:
-                raise ValueError("a gradient must be a contiguous tensor of its parameter's shape, on %s" % here)
+            if g.numel() != p.numel() or not g.is_contiguous() or g.get_device() != here:
+                raise ValueError("a gradient must be a contiguous tensor of its parameter's shape, on cuda:%d" % here)
             if dtype is None:
                 dtype = g.dtype
             if g.dtype != dtype or dtype not in _TYPES:
@@ -462,8 +467,7 @@ class AdamW:
             return
         a = _AdamwArgs(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, self.t + 1, self.state_bits,
                        _TYPES[self.dtype], _TYPES[dtype], 0)
-        with torch.cuda.device(here):
-            _check(_load().massive_adamw(self._list, len(self._list), ctypes.byref(a), _stream(here)))
+        _check(_load().massive_adamw(self._list, len(self._list), ctypes.byref(a), _stream(here)))
         self.t += 1
 
     def states(self):
@@ -474,5 +478,5 @@ class AdamW:
             return self.m, self.v
         m, v = (torch.empty(self.total, device=self.m.device) for _ in range(2))
         _check(_load().massive_adamw_states(self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr(), self.v_scale.data_ptr(),
-                                            self.total, m.data_ptr(), v.data_ptr(), _stream(m.device)))
+                                            self.total, m.data_ptr(), v.data_ptr(), _stream(_on_gpu(m))))
         return m, v
