@@ -4,11 +4,13 @@
 //   dx       dz w              dz = dy * act'(pre), taken as it is read
 //   dw       dz^T [x | x2], dbias = sum of dz over the rows
 //
-// All three are C = A B^T over a reduction index k, on tiles of BM x BN by a
-// block of four waves, with the matrix unit's 32x32 products (bf16: 16 k at a
-// time; fp32: 2). An operand is read along k (its rows are k-contiguous: x, w
-// in the forward pass, dz for dx) or across k (its columns are: w for dx, dz
-// and x for dw), through LDS, the next tile's loads in flight meanwhile.
+// All three are C = A B^T over a reduction index k, with the matrix unit's
+// 32x32 products (bf16: 16 k at a time; fp32: 2). Here are the forms of y and
+// dx for few rows (linear_stream.hpp has those for many, and
+// linear_weights.hpp dw): tiles of BM x BN by a block of four waves. An operand
+// is read along k (its rows are k-contiguous: x, w in the forward pass, dz for
+// dx) or across k (its columns are: w for dx), through LDS, the next tile's
+// loads in flight meanwhile.
 #pragma once
 
 #include "common.hpp"
@@ -153,7 +155,7 @@ struct Staged<T, true, SLOPE, BR> {  // along k: a thread takes chunk t % 8 of r
       if constexpr (SLOPE) one(o.pre + r * o.pre_stride + k, left, z[i]);
     }
   }
-  __device__ __forceinline__ void put(char* lds, const Operand<T>& o, bool, f32x4&) {
+  __device__ __forceinline__ void put(char* lds, const Operand<T>& o) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int r = threadIdx.x / 8 + 32 * i;
@@ -167,10 +169,10 @@ struct Staged<T, true, SLOPE, BR> {  // along k: a thread takes chunk t % 8 of r
   }
 };
 
-template <bool SLOPE, int BR>
-struct Staged<bf16, false, SLOPE, BR> {  // across k: a thread takes 8 k by 4 r, and turns them
+template <int BR>
+struct Staged<bf16, false, false, BR> {  // across k: a thread takes 8 k by 4 r, and turns them
   typedef cols_t<bf16, 4> quad;
-  quad v[8], z[SLOPE ? 8 : 1];
+  quad v[8];
   static constexpr int kRB = BR / 4;  // threads along r
 
   __device__ __forceinline__ static void one(const bf16* p, int64_t left, quad& v) {
@@ -189,28 +191,11 @@ struct Staged<bf16, false, SLOPE, BR> {  // across k: a thread takes 8 k by 4 r,
     for (int j = 0; j < 8; ++j) {
       const int64_t left = k1 + j < o.K ? o.R - r : 0;
       one(o.p + (k1 + j) * o.stride + r, left, v[j]);
-      if constexpr (SLOPE) one(o.pre + (k1 + j) * o.pre_stride + r, left, z[j]);
     }
   }
-  // sums: with `count`, this thread's sums of its four rows over k
-  __device__ __forceinline__ void put(char* lds, const Operand<bf16>& o, bool count, f32x4& sums) {
+  __device__ __forceinline__ void put(char* lds, const Operand<bf16>&) {
     if (!mine()) return;
     const int r = (threadIdx.x % kRB) * 4, c = threadIdx.x / kRB;
-    if constexpr (SLOPE) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float g = act_grad<bf16>((float)v[j][q], (float)z[j][q], o.act);
-          if (count) sums[q] += g;
-          v[j][q] = (bf16)g;
-        }
-    } else if (count) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) sums[q] += (float)v[j][q];
-    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       bf16x8 w;
@@ -221,11 +206,11 @@ struct Staged<bf16, false, SLOPE, BR> {  // across k: a thread takes 8 k by 4 r,
   }
 };
 
-template <bool SLOPE, int BR>
-struct Staged<float, false, SLOPE, BR> {  // across k in fp32: LDS keeps [k][r], a thread takes 4 r of every 8th k
+template <int BR>
+struct Staged<float, false, false, BR> {  // across k in fp32: LDS keeps [k][r], a thread takes 4 r of every 8th k
   static constexpr int kRB = BR / 4, kKT = kLinNT / kRB, kN = 32 / kKT;
   typedef cols_t<float, 4> quad;
-  quad v[kN], z[SLOPE ? kN : 1];
+  quad v[kN];
 
   __device__ __forceinline__ static void one(const float* p, int64_t left, quad& v) {
     if (left >= 4) {
@@ -242,17 +227,11 @@ struct Staged<float, false, SLOPE, BR> {  // across k in fp32: LDS keeps [k][r],
       const int64_t k = k0 + threadIdx.x / kRB + kKT * i;
       const int64_t left = k < o.K ? o.R - r : 0;
       one(o.p + k * o.stride + r, left, v[i]);
-      if constexpr (SLOPE) one(o.pre + k * o.pre_stride + r, left, z[i]);
     }
   }
-  __device__ __forceinline__ void put(char* lds, const Operand<float>& o, bool count, f32x4& sums) {
+  __device__ __forceinline__ void put(char* lds, const Operand<float>&) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      if constexpr (SLOPE) act_grads<float, 4>(v[i], z[i], o.act);
-      if (count) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) sums[q] += v[i][q];
-      }
       const int k = threadIdx.x / kRB + kKT * i, r = (threadIdx.x % kRB) * 4;
       *reinterpret_cast<f32x4*>(lds + (k * BR + r) * 4) = v[i];
     }
@@ -363,7 +342,7 @@ constexpr int lin_lds_bytes() {
 // is multiplied.
 template <typename T, bool A_ALONG, bool A_SLOPE, bool B_ALONG, int BM, int BN>
 __device__ __forceinline__ void product(Acc<T, BM, BN>& c, char* lds, const Operand<T>& a, int64_t ra, const Operand<T>& b,
-                                        int64_t rb, int64_t k0, int64_t k1, bool count, f32x4& sums) {
+                                        int64_t rb, int64_t k0, int64_t k1) {
   typedef Staged<T, A_ALONG, A_SLOPE, BM> SA;
   typedef Staged<T, B_ALONG, false, BN> SB;
   char *la = lds, *lb = lds + BM * 128;
@@ -375,8 +354,8 @@ __device__ __forceinline__ void product(Acc<T, BM, BN>& c, char* lds, const Oper
   }
   for (int64_t k = k0; k < k1; k += Tile<T>::kK) {
     __syncthreads();
-    sa.put(la, a, count, sums);
-    sb.put(lb, b, false, sums);
+    sa.put(la, a);
+    sb.put(lb, b);
     __syncthreads();
     if (k + Tile<T>::kK < k1) {
       sa.load(a, ra, k + Tile<T>::kK);
@@ -425,10 +404,9 @@ __global__ __launch_bounds__(kLinNT) void k_linear(LinearForward<T> a, int tiles
   const int64_t r0 = tile / tiles_n * BM;
   const int n0 = (int)(tile % tiles_n) * BN;
   Acc<T, BM, BN> c;
-  f32x4 none = {};
 #pragma unroll 1
   for (int s = 0; s < 2; ++s)
-    product<T, true, false, true, BM, BN>(c, lds, a.x[s], r0, a.w[s], n0, 0, a.x[s].K, false, none);
+    product<T, true, false, true, BM, BN>(c, lds, a.x[s], r0, a.w[s], n0, 0, a.x[s].K);
   __syncthreads();
   c.emit(lds, [&](int r, int col, float (&z)[8]) {
     if (r0 + r < a.rows) linear_finish(a, r0 + r, n0 + col, z);
@@ -456,8 +434,7 @@ __global__ __launch_bounds__(kLinNT) void k_linear_dx(LinearDx<T> a, int64_t blo
   at -= s ? a.tiles[0] : 0;
   const int n0 = at * BN;
   Acc<T, BM, BN> c;
-  f32x4 none = {};
-  product<T, true, SLOPE, false, BM, BN>(c, lds, a.dz, r0, a.w[s], n0, 0, a.dz.K, false, none);
+  product<T, true, SLOPE, false, BM, BN>(c, lds, a.dz, r0, a.w[s], n0, 0, a.dz.K);
   __syncthreads();
   T* dx = a.dx[s];
   const int64_t stride = a.dx_stride[s];
@@ -466,62 +443,6 @@ __global__ __launch_bounds__(kLinNT) void k_linear_dx(LinearDx<T> a, int64_t blo
     const int64_t row = r0 + r;
     const int left = k - n0 - col;
     if (row < a.rows && left > 0) store_cols<T, 8>(dx + row * stride + n0 + col, left, v);
-  });
-}
-
-// ---------------------------------------------------------------------- dw
-// The rows are split into parts; a block sums one tile of dw over one part and
-// writes it as fp32, and k_linear_join adds the parts in order.
-template <typename T>
-struct LinearDw {
-  Operand<T> dz, x[2];     // both across k, which is the row here
-  float *dw, *dbias;       // [parts][n][k0 + k1] and [parts][n], null where not asked for
-  int64_t rows, part;      // rows of a part, a multiple of the tile's k
-  int n, k[2], tiles[2], tiles_n;
-};
-
-template <typename T, bool SLOPE, int BM, int BN>
-__global__ __launch_bounds__(kLinNT) void k_linear_dw(LinearDw<T> a, int64_t blocks) {
-  __shared__ __align__(16) char lds[lin_lds_bytes<T, BM, BN>()];
-  const int tiles = a.tiles[0] + a.tiles[1];
-  const int64_t tile = tile_of_block(blockIdx.x, blocks);
-  const int64_t part = tile / (tiles * a.tiles_n);
-  const int in = (int)(tile % (tiles * a.tiles_n));
-  const int n0 = in / tiles * BM;
-  int at = in % tiles;
-  const bool bias = a.dbias && at == 0;
-  const int s = at >= a.tiles[0] ? 1 : 0;
-  at -= s ? a.tiles[0] : 0;
-  const int k0 = at * BN;
-  Acc<T, BM, BN> c;
-  f32x4 sums = {};
-  const int64_t b = part * a.part, e = min(a.rows, b + a.part);
-  product<T, false, SLOPE, false, BM, BN>(c, lds, a.dz, n0, a.x[s], k0, b, e, bias, sums);
-  __syncthreads();
-  if (bias) {
-    // the threads that share four columns add up in order
-    constexpr int kRB = BM / 4;
-    float* turn = reinterpret_cast<float*>(lds);
-    constexpr int kGroups = sizeof(T) == 2 ? 8 : kLinNT / kRB;
-    if ((int)threadIdx.x < kRB * kGroups) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) turn[(threadIdx.x / kRB) * BM + (threadIdx.x % kRB) * 4 + q] = sums[q];
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < BM && n0 + (int)threadIdx.x < a.n) {
-      float t = 0.0f;
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g) t += turn[g * BM + threadIdx.x];
-      a.dbias[part * a.n + n0 + threadIdx.x] = t;
-    }
-    __syncthreads();
-  }
-  if (!a.dw) return;
-  const int k = a.k[s], all = a.k[0] + a.k[1], off = s ? a.k[0] : 0;
-  float* dw = a.dw + part * a.n * (int64_t)all + off;
-  c.emit(lds, [&](int r, int col, float* v) {
-    const int left = k - k0 - col;
-    if (n0 + r < a.n && left > 0) store_cols<float, 8>(dw + (int64_t)(n0 + r) * all + k0 + col, left, v);
   });
 }
 

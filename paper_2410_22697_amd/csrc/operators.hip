@@ -16,6 +16,7 @@
 #include "call_error.hpp"
 #include "linear_kernels.hpp"
 #include "linear_stream.hpp"
+#include "linear_weights.hpp"
 #include "rows_kernels.hpp"
 
 namespace {
@@ -432,23 +433,24 @@ int linear(const massive_linear_args* a, void* stream) {
   });
 }
 
-// How dw's rows are split: enough parts for the chip, none shorter than 512
-// rows.
+// dw's tiles, and the parts into which its rows are split: enough blocks for
+// the chip, and parts of no less than eight steps of rows where there are.
 struct DwPlan {
-  int bm, bn, tiles_n, tiles[2];
+  bool narrow;  // tiles of 64 outputs by 256 columns, else of 256 by 128
+  int tiles_n, tiles[2];
   int64_t part, parts, dw_floats, bytes;
 };
 DwPlan dw_plan(const massive_linear_grads* a) {
   DwPlan p = {};
-  p.bm = a->n <= 64 ? 64 : 128;
-  p.bn = a->k <= 64 && a->k_second <= 64 ? 64 : 128;
-  if (p.bm != p.bn) p.bm = p.bn = 64;
-  p.tiles_n = (int)cdiv(a->n, p.bm);
-  p.tiles[0] = (int)cdiv(a->k, p.bn);
-  p.tiles[1] = (int)cdiv(a->k_second, p.bn);
+  p.narrow = a->n <= 64;
+  const int bn = p.narrow ? 64 : 256, bk = p.narrow ? 256 : 128;
+  const int step = 64 / size_of(a->type);
+  p.tiles_n = (int)cdiv(a->n, bn);
+  p.tiles[0] = (int)cdiv(a->k, bk);
+  p.tiles[1] = (int)cdiv(a->k_second, bk);
   const int64_t tiles = (int64_t)p.tiles_n * (p.tiles[0] + p.tiles[1]);
-  const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 512));
-  p.part = round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, 768 / tiles))), 64);
+  const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 8 * step));
+  p.part = round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, (p.narrow ? 512 : 256) / tiles))), step);
   p.parts = cdiv(a->rows, p.part);
   p.dw_floats = a->dw ? p.parts * a->n * ((int64_t)a->k + a->k_second) : 0;
   p.bytes = 4 * (round_up(p.dw_floats, 4) + (a->dbias ? p.parts * a->n : 0));
@@ -498,9 +500,9 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
   if (!a->dw && !a->dbias) return MASSIVE_OK;
   const DwPlan p = dw_plan(a);
   ms::LinearDw<T> f;
-  f.dz = operand<T>(a->dy, a->dy_stride, a->n, a->rows, a->pre, a->pre_stride, a->act);
-  f.x[0] = operand<T>(a->x, a->x_stride, k[0], a->rows);
-  f.x[1] = operand<T>(a->x_second, a->x_second_stride, k[1], a->rows);
+  f.dz = operand<T>(a->dy, a->dy_stride, a->rows, a->n, a->pre, a->pre_stride, a->act);
+  f.x[0] = operand<T>(a->x, a->x_stride, a->rows, k[0]);
+  f.x[1] = operand<T>(a->x_second, a->x_second_stride, a->rows, k[1]);
   f.dw = a->dw ? (float*)workspace : nullptr;
   f.dbias = a->dbias ? (float*)workspace + round_up(p.dw_floats, 4) : nullptr;
   f.rows = a->rows;
@@ -513,11 +515,11 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
   f.tiles_n = p.tiles_n;
   const int64_t blocks = p.parts * p.tiles_n * (p.tiles[0] + p.tiles[1]);
   if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
-  auto go = [&](auto b) {
-    return slope ? launch("massive_linear_backward", ms::k_linear_dw<T, true, b(), b()>, blocks, ms::kLinNT, 0, stream, f, blocks)
-                 : launch("massive_linear_backward", ms::k_linear_dw<T, false, b(), b()>, blocks, ms::kLinNT, 0, stream, f, blocks);
-  };
-  const int rc = p.bm == 128 ? go(std::integral_constant<int, 128>()) : go(std::integral_constant<int, 64>());
+  const char* what = "massive_linear_backward";
+  const int rc = p.narrow ? (slope ? launch(what, ms::k_linear_dw<T, true, 64, 256>, blocks, ms::kDwNT, 0, stream, f, blocks)
+                                   : launch(what, ms::k_linear_dw<T, false, 64, 256>, blocks, ms::kDwNT, 0, stream, f, blocks))
+                          : (slope ? launch(what, ms::k_linear_dw<T, true, 256, 128>, blocks, ms::kDwNT, 0, stream, f, blocks)
+                                   : launch(what, ms::k_linear_dw<T, false, 256, 128>, blocks, ms::kDwNT, 0, stream, f, blocks));
   if (rc) return rc;
   const int64_t values = (int64_t)a->n * ((a->dw ? k[0] + k[1] : 0) + (a->dbias ? 1 : 0));
   return launch("massive_linear_backward", ms::k_linear_join<T>, std::min<int64_t>(cdiv(values, ms::kLinNT), 4096), ms::kLinNT, 0,
