@@ -27,29 +27,9 @@ constexpr int kStreamBlockBytes = 32 * 256; // weights of 32 outputs and a chunk
 template <typename T>
 struct StreamSegment {
   Operand<T> x;  // R rows, K columns, along k
-  const T* w;    // along: w[n * w_stride + k]; across: w[k * w_stride + n]
-  int64_t w_stride;
+  Weights<T> w;
   int chunks;    // of K
 };
-
-// The 16 bytes of k that a lane holds for (segment, k): those from k on where
-// they are all there; the row's last 16 bytes, of which only those from k on
-// count, at its end; none behind it. `skip` counts the elements left out.
-template <typename T>
-__device__ __forceinline__ int skipped(int64_t k, int64_t K) {
-  constexpr int kV = 16 / sizeof(T);
-  return k + kV <= K ? 0 : k < K ? (int)(k + kV - K) : kV;
-}
-template <typename T>
-__device__ __forceinline__ u32x4 without(u32x4 v, int skip) {
-  constexpr int kPer = 4 / sizeof(T);  // elements per word
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int left = skip - q * kPer;  // elements of this word to clear
-    v[q] = left >= kPer ? 0u : left == 1 && kPer == 2 ? v[q] & 0xFFFF0000u : v[q];
-  }
-  return v;
-}
 
 // The units of 16 bytes of k by kV outputs in which a thread moves weights.
 template <typename T, bool ACROSS, int NB>
@@ -66,7 +46,7 @@ struct StreamWeights {
       const int unit = threadIdx.x + p * kStreamNT;
       const int r = n0 + (unit % (NB * 32 / kV)) * kV, at = unit / (NB * 32 / kV);
       const int64_t k = (int64_t)chunk * kStreamSteps * 2 * kV + at * kV;
-      const int skip = skipped<T>(k, s.x.K);
+      const int skip = s.x.K < kV ? (k ? kV : 0) : skipped<T>(k, s.x.K);
 #pragma unroll
       for (int q = 0; q < kV; ++q) v[p][q] = (u32x4)0u;
       if (unit >= kUnits || skip == kV) continue;
@@ -75,8 +55,8 @@ struct StreamWeights {
         // kV rows of k, kV outputs of each, turned by store()
 #pragma unroll
         for (int q = 0; q < kV; ++q) {
-          if (q < skip) continue;
-          const T* p0 = s.w + (from + q) * s.w_stride + r;
+          if (q < skip || from + q >= s.x.K) continue;
+          const T* p0 = s.w.p + (from + q) * s.w.stride + r;
           if (r + kV <= n) {
             v[p][q] = __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(p0));
           } else {
@@ -89,8 +69,10 @@ struct StreamWeights {
       } else {
 #pragma unroll
         for (int q = 0; q < kV; ++q)
-          if (r + q < n)
-            v[p][q] = without<T>(__builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(s.w + (int64_t)(r + q) * s.w_stride + from)), skip);
+          if (r + q < n && s.x.K < kV)
+            v[p][q] = k_along(s.w.p + (int64_t)(r + q) * s.w.stride, k, s.x.K);
+          else if (r + q < n)
+            v[p][q] = without<T>(__builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(s.w.p + (int64_t)(r + q) * s.w.stride + from)), skip);
       }
     }
   }
@@ -150,6 +132,15 @@ __device__ __forceinline__ void stream_product(const StreamSegment<T> (&segs)[2]
   // one step of (tile, chunk) to its registers
   auto fetch = [&](int s, const StreamSegment<T>& g, int c, int64_t row) {
     const int64_t k = ((int64_t)c * kStreamSteps + s) * 2 * kV + half * kV;
+    if (g.x.K < kV) {  // one step has it all
+      x[s] = (u32x4)0u;
+      if constexpr (SLOPE) z[s] = (u32x4)0u;
+      if (s == 0) {
+        x[s] = k_along(g.x.p + row * g.x.stride, k, g.x.K);
+        if constexpr (SLOPE) z[s] = k_along(g.x.pre + row * g.x.pre_stride, k, g.x.K);
+      }
+      return;
+    }
     const int64_t from = min(k, g.x.K - kV);  // masked when it is used
     x[s] = __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(g.x.p + row * g.x.stride + from));
     if constexpr (SLOPE)
@@ -174,7 +165,7 @@ __device__ __forceinline__ void stream_product(const StreamSegment<T> (&segs)[2]
       const char* wl = lds + (RESIDENT ? c : buffer) * kChunkBytes + lane * 16;
       const bool more = !RESIDENT && (!wrap || tile + tile_step < tiles);
       if (more) w.load(next, in_seg(next_c), n0, n);
-      if (((int64_t)cs + 1) * kStreamSteps * 2 * kV > g.x.K) {  // the segment's end lies in this chunk
+      if (((int64_t)cs + 1) * kStreamSteps * 2 * kV > g.x.K && g.x.K >= kV) {  // the segment's end lies in this chunk
 #pragma unroll
         for (int q = 0; q < kStreamSteps; ++q) {
           const int skip = skipped<T>(((int64_t)cs * kStreamSteps + q) * 2 * kV + half * kV, g.x.K);
@@ -286,8 +277,8 @@ __global__ __launch_bounds__(kStreamNT) void k_linear_stream(LinearForward<T> a,
   int64_t tile, step;
   int group;
   stream_place(groups, tile, step, group);
-  const StreamSegment<T> segs[2] = {{a.x[0], a.w[0].p, a.w[0].stride, (int)((a.x[0].K * sizeof(T) + 255) / 256)},
-                                    {a.x[1], a.w[1].p, a.w[1].stride, (int)((a.x[1].K * sizeof(T) + 255) / 256)}};
+  const StreamSegment<T> segs[2] = {{a.x[0], a.w[0], (int)((a.x[0].K * sizeof(T) + 255) / 256)},
+                                    {a.x[1], a.w[1], (int)((a.x[1].K * sizeof(T) + 255) / 256)}};
   // the group's bias as fp32, beside the turns: read with LDS's own waits, not behind the rows on their way
   float* bias = reinterpret_cast<float*>(stream_lds + lds_weights + kStreamNT / MS_WAVE * kStreamTurn);
   const int n0 = group * NB * 32;
@@ -313,12 +304,7 @@ __global__ __launch_bounds__(kStreamNT) void k_linear_stream(LinearForward<T> a,
               store_cols<T, 8>(a.y + row * a.y_stride + c0 + c, 8, z);
             },
             [&](int r, int c, float z) {
-              const int64_t row = r0 + r;
-              z += bias[c0 - n0 + c];
-              if (a.pre) a.pre[row * a.pre_stride + c0 + c] = (T)z;
-              z = act_value<T>(z, a.act);
-              if (a.residual) z += (float)a.residual[row * a.residual_stride + c0 + c];
-              a.y[row * a.y_stride + c0 + c] = (T)z;
+              linear_finish(a, r0 + r, c0 + c, z + bias[c0 - n0 + c]);
             });
       });
 }
@@ -331,7 +317,7 @@ __global__ __launch_bounds__(kStreamNT) void k_linear_dx_stream(LinearDx<T> a, i
   stream_place(groups, tile, step, group);
   const int s = group >= a.tiles[0] ? 1 : 0;
   const int n0 = (group - (s ? a.tiles[0] : 0)) * NB * 32;
-  const StreamSegment<T> segs[2] = {{a.dz, a.w[s].p, a.w[s].stride, (int)((a.dz.K * sizeof(T) + 255) / 256)}, {a.dz, nullptr, 0, 0}};
+  const StreamSegment<T> segs[2] = {{a.dz, a.w[s], (int)((a.dz.K * sizeof(T) + 255) / 256)}, {a.dz, a.w[s], 0}};
   T* dx = a.dx[s];
   const int64_t stride = a.dx_stride[s];
   const int k = a.k[s];

@@ -14,6 +14,7 @@
 #include "adamw_kernels.hpp"
 #include "block_kernels.hpp"
 #include "call_error.hpp"
+#include "linear_few.hpp"
 #include "linear_kernels.hpp"
 #include "linear_stream.hpp"
 #include "linear_weights.hpp"
@@ -334,7 +335,7 @@ int block_mean_backward(const massive_block* b, const void* dout, int32_t type, 
 }
 
 // ------------------------------------------------------------------- linear
-constexpr int64_t kMostRows = int64_t(1) << 29;  // tiles of 64 rows stay within a launch
+constexpr int64_t kMostRows = int64_t(1) << 29;
 
 template <typename T>
 ms::Operand<T> operand(const void* p, int64_t stride, int64_t R, int64_t K, const void* pre = nullptr, int64_t pre_stride = 0,
@@ -352,28 +353,20 @@ int check_layer(int64_t rows, int32_t n, int32_t k, int32_t k_second, int32_t ty
   return MASSIVE_OK;
 }
 
-// Squares of 128 where they give the chip enough blocks, else of 64; 64 columns
-// where no more are asked for.
-template <typename F>
-int with_tile(int64_t rows, int64_t cols, F f) {
-  if (cols <= 64 && cdiv(rows, 128) >= 256)
-    return f(std::integral_constant<int, 128>(), std::integral_constant<int, 64>());
-  if (cols > 64 && cdiv(rows, 128) * cdiv(cols, 128) >= 256)
-    return f(std::integral_constant<int, 128>(), std::integral_constant<int, 128>());
-  return f(std::integral_constant<int, 64>(), std::integral_constant<int, 64>());
-}
-
-// The streaming form's shape for n outputs from `chunks` chunks of k: blocks of
-// 32 outputs that a wave accumulates, and whether their weights stay in LDS.
+// The streaming form's shape for n outputs (of each of `parts` groups that have
+// no block in common) from `chunks` chunks of k: blocks of 32 outputs that a
+// wave accumulates, and whether their weights stay in LDS. As many as there
+// are outputs, unless fewer give more of the chip's 256 CUs work.
 struct StreamPlan {
   int nb;
   bool resident;
   int lds_weights, lds;
 };
-StreamPlan stream_plan(int64_t n, int64_t chunks) {
+StreamPlan stream_plan(int64_t rows, int64_t n, int parts, int64_t chunks) {
   StreamPlan p;
   auto bytes = [&](int nb) { return chunks * nb * ms::kStreamBlockBytes; };
-  p.nb = n <= 64 ? 2 : n <= 128 || bytes(8) > ms::kStreamLds ? 4 : 8;
+  p.nb = n <= 32 ? 1 : n <= 64 ? 2 : n <= 128 || bytes(8) > ms::kStreamLds ? 4 : 8;
+  while (p.nb > 2 && cdiv(rows, ms::kStreamRows) * cdiv(n, p.nb * 32) * parts < 256) p.nb /= 2;
   p.resident = bytes(p.nb) <= ms::kStreamLds;
   p.lds_weights = (int)(p.resident ? bytes(p.nb) : 2 * p.nb * ms::kStreamBlockBytes);
   p.lds = p.lds_weights + ms::kStreamNT / MS_WAVE * ms::kStreamTurn + p.nb * 32 * 4;  // weights, turns, bias
@@ -386,7 +379,6 @@ int64_t stream_blocks(const StreamPlan& p, int64_t rows, int groups) {
   const int64_t most = std::max<int64_t>(1, 256 * per_cu / 8 / groups) * groups * 8;
   return std::min(most, round_up(cdiv(rows, ms::kStreamRows), 8) * groups);
 }
-constexpr int64_t kStreamLeast = 8192;  // rows
 
 // f(blocks of 32 outputs, whether they stay), both as types.
 template <typename F>
@@ -394,8 +386,17 @@ int with_stream(const StreamPlan& p, F f) {
   using std::integral_constant;
   if (p.nb == 8) return f(integral_constant<int, 8>(), std::true_type());
   if (p.nb == 4) return p.resident ? f(integral_constant<int, 4>(), std::true_type()) : f(integral_constant<int, 4>(), std::false_type());
-  return p.resident ? f(integral_constant<int, 2>(), std::true_type()) : f(integral_constant<int, 2>(), std::false_type());
+  if (p.nb == 2) return p.resident ? f(integral_constant<int, 2>(), std::true_type()) : f(integral_constant<int, 2>(), std::false_type());
+  return p.resident ? f(integral_constant<int, 1>(), std::true_type()) : f(integral_constant<int, 1>(), std::false_type());
 }
+
+// Whether a product of rows x cols results streams its rows: from about 2^21
+// results on (dx in bf16: 2^20). Below, both forms take about as long as a
+// launch, and the form for few rows has more blocks; above, it reads its
+// operands too often. Measured, us, few rows' form / streaming, 256 -> 256: bf16
+// 4000 rows 11 / 20, 8000 21 / 20, 16000 41 / 21; fp32 8000 39 / 44, 16000
+// 75 / 46.
+bool streams(int64_t rows, int64_t cols, int log2_least) { return rows * round_up(cols, 32) >= int64_t(1) << log2_least; }
 
 template <typename T>
 int linear(const massive_linear_args* a, void* stream) {
@@ -403,8 +404,8 @@ int linear(const massive_linear_args* a, void* stream) {
   const int64_t k = a->k;
   f.x[0] = operand<T>(a->x, a->x_stride, a->rows, k);
   f.x[1] = operand<T>(a->x_second, a->x_second_stride, a->rows, a->k_second);
-  f.w[0] = operand<T>(a->w, a->w_stride, a->n, k);
-  f.w[1] = operand<T>((const T*)a->w + k, a->w_stride, a->n, a->k_second);
+  f.w[0] = {(const T*)a->w, a->w_stride};
+  f.w[1] = {(const T*)a->w + k, a->w_stride};
   f.bias = (const T*)a->bias;
   f.residual = (const T*)a->residual;
   f.y = (T*)a->y;
@@ -415,22 +416,18 @@ int linear(const massive_linear_args* a, void* stream) {
   f.rows = a->rows;
   f.n = a->n;
   f.act = a->act;
-  // a segment of under 16 bytes cannot be read in whole vectors
-  constexpr int kV = 16 / sizeof(T);
-  if (a->rows >= kStreamLeast && a->k >= kV && (a->k_second == 0 || a->k_second >= kV)) {
-    const StreamPlan p = stream_plan(a->n, cdiv(a->k * sizeof(T), 256) + cdiv(a->k_second * sizeof(T), 256));
+  if (streams(a->rows, a->n, 21)) {
+    const StreamPlan p = stream_plan(a->rows, a->n, 1, cdiv(a->k * sizeof(T), 256) + cdiv(a->k_second * sizeof(T), 256));
     const int groups = (int)cdiv(a->n, p.nb * 32);
     return with_stream(p, [&](auto nb, auto resident) {
       return launch("massive_linear", ms::k_linear_stream<T, nb(), resident()>, stream_blocks(p, a->rows, groups), ms::kStreamNT, p.lds,
                     stream, f, groups, p.lds_weights);
     });
   }
-  return with_tile(a->rows, a->n, [&](auto bm, auto bn) {
-    const int tiles_n = (int)cdiv(a->n, bn());
-    const int64_t blocks = cdiv(a->rows, bm()) * tiles_n;
-    if (blocks > kMostBlocks) REFUSE("too many rows and outputs for one call");
-    return launch("massive_linear", ms::k_linear<T, bm(), bn()>, blocks, ms::kLinNT, 0, stream, f, tiles_n, blocks);
-  });
+  const int tiles_n = (int)cdiv(a->n, 32);
+  const int64_t blocks = cdiv(a->rows, 32) * tiles_n;
+  if (blocks > kMostBlocks / 2) REFUSE("too many outputs for so many rows");
+  return launch("massive_linear", ms::k_linear_few<T>, blocks, ms::kFewNT, 0, stream, f, tiles_n);
 }
 
 // dw's tiles, and the parts into which its rows are split: enough blocks for
@@ -469,7 +466,7 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
   if (a->dx || a->dx_second) {
     ms::LinearDx<T> f;
     f.dz = operand<T>(a->dy, a->dy_stride, a->rows, a->n, a->pre, a->pre_stride, a->act);
-    for (int s = 0; s < 2; ++s) f.w[s] = operand<T>((const T*)a->w + (s ? k[0] : 0), a->w_stride, k[s], a->n);
+    for (int s = 0; s < 2; ++s) f.w[s] = {(const T*)a->w + (s ? k[0] : 0), a->w_stride};
     f.dx[0] = (T*)a->dx;
     f.dx[1] = (T*)a->dx_second;
     f.dx_stride[0] = a->dx_stride;
@@ -477,10 +474,9 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
     f.rows = a->rows;
     f.k[0] = a->k;
     f.k[1] = a->k_second;
-    const int64_t cols = (a->dx ? k[0] : 0) + (a->dx_second ? k[1] : 0);
-    constexpr int kV = 16 / sizeof(T);
-    const bool streams = a->rows >= kStreamLeast && a->n >= kV;
-    const StreamPlan p = stream_plan(std::max(a->dx ? k[0] : 0, a->dx_second ? k[1] : 0), cdiv(a->n * sizeof(T), 256));
+    const int64_t k0 = a->dx ? k[0] : 0, k1 = a->dx_second ? k[1] : 0;
+    const bool stream_it = streams(a->rows, round_up(k0, 32) + k1, sizeof(T) == 2 ? 20 : 21);
+    const StreamPlan p = stream_plan(a->rows, std::max(k0, k1), k0 && k1 ? 2 : 1, cdiv(a->n * sizeof(T), 256));
     auto go_stream = [&](auto nb, auto resident) {
       for (int s = 0; s < 2; ++s) f.tiles[s] = f.dx[s] ? (int)cdiv(k[s], nb() * 32) : 0;
       const int groups = f.tiles[0] + f.tiles[1];
@@ -488,13 +484,13 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
       return slope ? launch("massive_linear_backward", ms::k_linear_dx_stream<T, true, nb(), resident()>, blocks, ms::kStreamNT, p.lds, stream, f, groups, p.lds_weights)
                    : launch("massive_linear_backward", ms::k_linear_dx_stream<T, false, nb(), resident()>, blocks, ms::kStreamNT, p.lds, stream, f, groups, p.lds_weights);
     };
-    const int rc = streams ? with_stream(p, go_stream) : with_tile(a->rows, cols, [&](auto bm, auto bn) {
-      for (int s = 0; s < 2; ++s) f.tiles[s] = f.dx[s] ? (int)cdiv(k[s], bn()) : 0;
-      const int64_t blocks = cdiv(a->rows, bm()) * (f.tiles[0] + f.tiles[1]);
-      if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
-      return slope ? launch("massive_linear_backward", ms::k_linear_dx<T, true, bm(), bn()>, blocks, ms::kLinNT, 0, stream, f, blocks)
-                   : launch("massive_linear_backward", ms::k_linear_dx<T, false, bm(), bn()>, blocks, ms::kLinNT, 0, stream, f, blocks);
-    });
+    auto go_few = [&] {
+      for (int s = 0; s < 2; ++s) f.tiles[s] = f.dx[s] ? (int)cdiv(k[s], 32) : 0;
+      const int64_t blocks = cdiv(a->rows, 32) * (f.tiles[0] + f.tiles[1]);
+      if (blocks > kMostBlocks / 2) REFUSE("too many columns for so many rows");
+      return launch("massive_linear_backward", slope ? ms::k_linear_dx_few<T, true> : ms::k_linear_dx_few<T, false>, blocks, ms::kFewNT, 0, stream, f);
+    };
+    const int rc = stream_it ? with_stream(p, go_stream) : go_few();
     if (rc) return rc;
   }
   if (!a->dw && !a->dbias) return MASSIVE_OK;
