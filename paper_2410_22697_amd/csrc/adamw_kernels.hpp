@@ -38,16 +38,21 @@ static_assert(sizeof(AdamwLaunch) <= 4000, "the launch's arguments hold the list
 // 8-bit codes of a value of m (a signed square law) and of v (a fourth power),
 // and back. The products are taken in exactly this order, without fused
 // multiply-adds, so that a state is the nearest code of its 32-bit value as
-// the formula's own roundings give it.
+// the formula's own roundings give it. The roots of `fast` are the hardware's,
+// a unit or two in the last place off: enough unless they lie so near the
+// middle between two codes (unsure()) that the rounding could go the other way.
 #pragma clang fp contract(off)
-__device__ __forceinline__ int code_m(float m, float inv) {
-  const float c = fminf(rintf(sqrtf(fabsf(m) * inv)), 127.0f);
+__device__ __forceinline__ float root_m(float t, bool fast) { return fast ? __builtin_amdgcn_sqrtf(t) : sqrtf(t); }
+__device__ __forceinline__ float root_v(float t, bool fast) {
+  return fast ? __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(t)) : sqrtf(sqrtf(t));
+}
+__device__ __forceinline__ bool unsure(float root) { return fabsf(root - (floorf(root) + 0.5f)) < 0x1p-12f; }
+__device__ __forceinline__ int code_m(float m, float root) {
+  const float c = fminf(rintf(root), 127.0f);
   return m < 0.0f ? -(int)c : (int)c;
 }
-__device__ __forceinline__ uint32_t code_v(float v, float inv) {
-  const float t = v * inv;
-  const float c = fminf(fmaxf(rintf(sqrtf(sqrtf(t))), 1.0f), 255.0f);
-  return t > 0.0f ? (uint32_t)c : 0u;
+__device__ __forceinline__ uint32_t code_v(float t, float root) {
+  return t > 0.0f ? (uint32_t)fminf(fmaxf(rintf(root), 1.0f), 255.0f) : 0u;
 }
 __device__ __forceinline__ float value_m(int c, float scale) { return (float)(c * (c < 0 ? -c : c)) * scale; }
 __device__ __forceinline__ float value_v(uint32_t c, float scale) {
@@ -121,7 +126,8 @@ __global__ __launch_bounds__(kAdamwNT) void k_adamw(AdamwLaunch a) {
       m[q] = m[q] * a.b1 + g[q] * a.b1c;
       v[q] = v[q] * a.b2 + (g[q] * g[q]) * a.b2c;
       p[q] = p[q] * a.decay;
-      p[q] = p[q] - (m[q] * a.lr) / (sqrtf(v[q]) * a.v_factor + a.eps);
+      // (the quotient to a few units in its last place: it is small beside p)
+      p[q] = p[q] - (m[q] * a.lr) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[q]) * a.v_factor + a.eps);
       mag_m = max(mag_m, __float_as_uint(m[q]) & 0x7FFFFFFFu);
       mag_v = max(mag_v, __float_as_uint(v[q]) & 0x7FFFFFFFu);
     }
@@ -143,12 +149,28 @@ __global__ __launch_bounds__(kAdamwNT) void k_adamw(AdamwLaunch a) {
         t.v_scale[at / kAdamwShare] = sv;
       }
       if (valid > 0) {
+        float tv[kAdamwQ], rm[kAdamwQ], rv[kAdamwQ];
+        bool again = false;
+#pragma unroll
+        for (int q = 0; q < kAdamwQ; ++q) {
+          tv[q] = v[q] * iv;
+          rm[q] = root_m(fabsf(m[q]) * im, true);
+          rv[q] = root_v(tv[q], true);
+          again |= unsure(rm[q]) || unsure(rv[q]);
+        }
+        if (again) {
+#pragma unroll
+          for (int q = 0; q < kAdamwQ; ++q) {
+            rm[q] = root_m(fabsf(m[q]) * im, false);
+            rv[q] = root_v(tv[q], false);
+          }
+        }
         cols_t<int8_t, kAdamwQ> wm;
         cols_t<uint8_t, kAdamwQ> wv;
 #pragma unroll
         for (int q = 0; q < kAdamwQ; ++q) {
-          wm[q] = (int8_t)(im != 0.0f ? code_m(m[q], im) : 0);
-          wv[q] = (uint8_t)(iv != 0.0f ? code_v(v[q], iv) : 0u);
+          wm[q] = (int8_t)(im != 0.0f ? code_m(m[q], rm[q]) : 0);
+          wv[q] = (uint8_t)(iv != 0.0f ? code_v(tv[q], rv[q]) : 0u);
         }
         int8_t* cm = (int8_t*)t.m + i;
         uint8_t* cv = (uint8_t*)t.v + i;

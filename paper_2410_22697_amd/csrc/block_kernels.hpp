@@ -26,25 +26,11 @@ __device__ __forceinline__ int last_cols(int c, int d) {
 // there stays zero.
 template <typename S, int BITS, int Q>
 struct Source {
-  typedef uint32_t raw __attribute__((ext_vector_type(Q * BITS / 32), aligned(4)));
-  raw w = (raw)0;
-  float step = 0.0f, lo = 0.0f;
-  // a packed row's floats follow its codes, so Q codes can be read from any column on
+  PackedCols<BITS, Q> p;
   __device__ __forceinline__ void load(const void* x, int64_t j, int64_t, const PackedRows& f, int c) {
-    const uint8_t* row = (const uint8_t*)x + j * f.row_bytes;
-    w = *reinterpret_cast<const raw*>(row + c * BITS / 8);
-    const float* s = reinterpret_cast<const float*>(row + f.floats_at) + (c >> f.group_log2) * (BITS == 8 ? 1 : 2);
-    if constexpr (BITS == 8) {
-      step = s[0];
-    } else {
-      lo = s[0];
-      step = s[1];
-    }
+    p.load((const uint8_t*)x + j * f.row_bytes, f, c);
   }
-  __device__ __forceinline__ float value(int q) const {
-    if constexpr (BITS == 8) return (float)(int8_t)(w[q / 4] >> (8 * (q % 4))) * step;
-    else return lo + (float)((w[q / 8] >> (4 * (q % 8))) & 15u) * step;
-  }
+  __device__ __forceinline__ float value(int q) const { return p.value(q); }
 };
 template <typename S, int Q>
 struct Source<S, 0, Q> {

@@ -117,7 +117,7 @@ int pack_rows(const massive_row_format* fmt, const void* src, int32_t src_type, 
   if (src_stride < f.d) REFUSE("src_stride is below d");
   if (!aligned(src, size_of(src_type)) || !aligned(slots, 4) || !aligned(table, 4)) REFUSE("src, slots or table is not aligned");
   const int team = team_of(f.d, ms::kRowsQ);
-  const int64_t blocks = std::min(cdiv(n, ms::kRowsNT / team), kMostBlocks);
+  const int64_t blocks = std::min(cdiv(n, ms::kRowsAhead * (ms::kRowsNT / team)), kMostBlocks);
   return with_type(src_type, [&](auto* s) {
     using S = std::remove_pointer_t<decltype(s)>;
     return with_bits(fmt->bits, [&](auto bits) {
@@ -140,8 +140,8 @@ int unpack_rows(const massive_row_format* fmt, const void* table, int64_t table_
   if (!out || (table_rows > 0 && !table)) REFUSE("table / out are NULL");
   if (out_stride < f.d) REFUSE("out_stride is below d");
   if (!aligned(out, size_of(out_type)) || !aligned(index, 4) || !aligned(table, 4)) REFUSE("table, index or out is not aligned");
-  const int team = team_of(f.d, ms::kRowsQ);
-  const int64_t blocks = std::min(cdiv(n, ms::kRowsNT / team), kMostBlocks);
+  const int team = team_of(f.d, 16 / size_of(out_type));
+  const int64_t blocks = std::min(cdiv(n, ms::kRowsAhead * (ms::kRowsNT / team)), kMostBlocks);
   return with_type(out_type, [&](auto* o) {
     using O = std::remove_pointer_t<decltype(o)>;
     return with_bits(fmt->bits, [&](auto bits) {

@@ -1,9 +1,10 @@
 // rows_kernels.hpp - rows written to a table in 8 or 4 bits, and read back.
 //
 // Both kernels give a row to a team of T lanes, T the power of two that covers
-// it at eight columns a lane (64 lanes take a longer row in turns), so rows of
-// a frontier's width share a wave. They move each value once and are bound by
-// memory: a value costs ~6 instructions.
+// it (64 lanes take a longer row in turns), so rows of a frontier's width share
+// a wave. They move each value once and are bound by memory: a value costs ~6
+// instructions. Both read what a row's address hangs on and, where it does not,
+// the row itself at once, and take two rows at a time.
 #pragma once
 
 #include "common.hpp"
@@ -12,12 +13,28 @@
 namespace ms {
 
 constexpr int kRowsNT = 256;
-constexpr int kRowsQ = 8;  // columns per lane: 8 bytes of 8-bit codes, 4 of 4-bit ones
+constexpr int kRowsQ = 8;  // columns per lane of a written row: 8 bytes of 8-bit codes, 4 of 4-bit ones
+constexpr int kRowsAhead = 2;  // rows of a team that are on their way together
 
-// Largest (or least) over aligned runs of `width` lanes, a power of two.
+// Largest (or least) over aligned runs of `width` lanes, a power of two. Within
+// 16 lanes the partners come by data-parallel moves: the neighbour, the other
+// pair, and, since equal groups hold equal values by then, the mirror images.
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false));
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
+}
 template <typename F, typename V>
 __device__ __forceinline__ V team_reduce(V x, int width, F pick) {
-  for (int o = width >> 1; o > 0; o >>= 1) x = pick(x, __shfl_xor(x, o, MS_WAVE));
+  if (width > 1) x = pick(x, moved<0xB1>(x));   // quad_perm 1 0 3 2
+  if (width > 2) x = pick(x, moved<0x4E>(x));   // quad_perm 2 3 0 1
+  if (width > 4) x = pick(x, moved<0x141>(x));  // row_half_mirror
+  if (width > 8) x = pick(x, moved<0x140>(x));  // row_mirror
+  if (width > 16) x = pick(x, __shfl_xor(x, 16, MS_WAVE));
+  if (width > 32) x = pick(x, __shfl_xor(x, 32, MS_WAVE));
   return x;
 }
 
@@ -86,69 +103,101 @@ __global__ __launch_bounds__(kRowsNT) void k_pack_rows(const S* __restrict__ src
   const int d = f.d;
   const bool whole = f.group_log2 == 31;
   const int width = whole ? T : 1 << (f.group_log2 - 3);  // lanes that share a group
-  for (int64_t i = (int64_t)blockIdx.x * (kRowsNT / T) + threadIdx.x / T; i < n; i += (int64_t)gridDim.x * (kRowsNT / T)) {
-    const int64_t slot = slots ? (int64_t)slots[i] : i;
-    if (slot < 0 || slot >= rows) continue;  // the same for the whole team
-    const S* x = src + i * stride;
-    uint8_t* row = table + slot * f.row_bytes;
-    float* floats = reinterpret_cast<float*>(row + f.floats_at);
-    float v[kRowsQ], step, inv;
-    if (whole && d > T * kRowsQ) {
-      // one group longer than the team: a sweep for its ends, one for the codes
-      GroupEnds<BITS> e;
-      for (int c = lane * kRowsQ; c < d; c += T * kRowsQ) {
-        load_cols<S, kRowsQ>(x + c, d - c, v);
-        e.add(v, d - c);
+  const int64_t step = (int64_t)gridDim.x * (kRowsNT / T);
+  for (int64_t i0 = (int64_t)blockIdx.x * (kRowsNT / T) + threadIdx.x / T; i0 < n; i0 += kRowsAhead * step) {
+    const int c1 = lane * kRowsQ;
+    int64_t slot[kRowsAhead];
+    float head[kRowsAhead][kRowsQ];  // the lane's first columns
+#pragma unroll
+    for (int u = 0; u < kRowsAhead; ++u) {
+      const int64_t i = i0 + u * step;
+      slot[u] = -1;
+      if (i < n) {
+        slot[u] = slots ? (int64_t)slots[i] : i;
+        if (c1 < d) load_cols<S, kRowsQ>(src + i * stride + c1, d - c1, head[u]);
       }
-      e.join(T);
-      e.scale(step, inv);
-      for (int c = lane * kRowsQ; c < d; c += T * kRowsQ) {
-        load_cols<S, kRowsQ>(x + c, d - c, v);
-        store_codes<BITS>(row, c, d, v, d - c, e.lo, inv);
-      }
-      if (lane == 0) {
-        if (BITS == 4) floats[0] = e.lo;
-        floats[BITS == 4 ? 1 : 0] = step;
-      }
-      continue;
     }
-    for (int c0 = 0; c0 < d; c0 += T * kRowsQ) {  // groups end with the team's turn or inside it
-      const int c = c0 + lane * kRowsQ;
-      GroupEnds<BITS> e;
-      if (c < d) {
-        load_cols<S, kRowsQ>(x + c, d - c, v);
-        e.add(v, d - c);
+#pragma unroll
+    for (int u = 0; u < kRowsAhead; ++u) {
+      if (slot[u] < 0 || slot[u] >= rows) continue;  // the same for the whole team
+      const S* x = src + (i0 + u * step) * stride;
+      uint8_t* row = table + slot[u] * f.row_bytes;
+      float* floats = reinterpret_cast<float*>(row + f.floats_at);
+      float step_size, inv;
+      if (whole && d > T * kRowsQ) {
+        // one group longer than the team: a sweep for its ends, one for the codes
+        GroupEnds<BITS> e;
+        float v[kRowsQ];
+        e.add(head[u], d - c1);
+        for (int c = c1 + T * kRowsQ; c < d; c += T * kRowsQ) {
+          load_cols<S, kRowsQ>(x + c, d - c, v);
+          e.add(v, d - c);
+        }
+        e.join(T);
+        e.scale(step_size, inv);
+        for (int c = c1; c < d; c += T * kRowsQ) {
+          load_cols<S, kRowsQ>(x + c, d - c, v);
+          store_codes<BITS>(row, c, d, v, d - c, e.lo, inv);
+        }
+        if (lane == 0) {
+          if (BITS == 4) floats[0] = e.lo;
+          floats[BITS == 4 ? 1 : 0] = step_size;
+        }
+        continue;
       }
-      e.join(width);
-      e.scale(step, inv);
-      if (c < d) {
-        store_codes<BITS>(row, c, d, v, d - c, e.lo, inv);
-        if (lane % width == 0) {
-          const int g = c >> f.group_log2;
-          if (BITS == 4) floats[2 * g] = e.lo;
-          floats[BITS == 4 ? 2 * g + 1 : g] = step;
+      for (int c0 = 0; c0 < d; c0 += T * kRowsQ) {  // groups end with the team's turn or inside it
+        const int c = c0 + c1;
+        GroupEnds<BITS> e;
+        float v[kRowsQ];
+        if (c0 == 0) {
+#pragma unroll
+          for (int q = 0; q < kRowsQ; ++q) v[q] = head[u][q];
+        } else if (c < d) {
+          load_cols<S, kRowsQ>(x + c, d - c, v);
+        }
+        if (c < d) e.add(v, d - c);
+        e.join(width);
+        e.scale(step_size, inv);
+        if (c < d) {
+          store_codes<BITS>(row, c, d, v, d - c, e.lo, inv);
+          if (lane % width == 0) {
+            const int g = c >> f.group_log2;
+            if (BITS == 4) floats[2 * g] = e.lo;
+            floats[BITS == 4 ? 2 * g + 1 : g] = step_size;
+          }
         }
       }
     }
   }
 }
 
+// Q columns a lane: 16 bytes of output.
 template <typename O, int BITS, int T>
 __global__ __launch_bounds__(kRowsNT) void k_unpack_rows(const uint8_t* __restrict__ table, int64_t rows,
                                                          const int32_t* __restrict__ index, int64_t n, O* __restrict__ out,
                                                          int64_t stride, PackedRows f) {
+  constexpr int Q = 16 / sizeof(O);
   const int lane = threadIdx.x % T;
-  for (int64_t i = (int64_t)blockIdx.x * (kRowsNT / T) + threadIdx.x / T; i < n; i += (int64_t)gridDim.x * (kRowsNT / T)) {
-    const uint8_t* row = packed_row(table, rows, index ? (int64_t)index[i] : i, f.row_bytes);
-    for (int c = lane * kRowsQ; c < f.d; c += T * kRowsQ) {
-      PackedCols<BITS, kRowsQ> p;
-      if (row)
-        p.load(row, f, c);
-      else
-        p.none();
-      float v[kRowsQ];
-      p.values(v);
-      store_cols<O, kRowsQ>(out + i * stride + c, f.d - c, v);
+  const int64_t step = (int64_t)gridDim.x * (kRowsNT / T);
+  for (int64_t i0 = (int64_t)blockIdx.x * (kRowsNT / T) + threadIdx.x / T; i0 < n; i0 += kRowsAhead * step) {
+    int64_t at[kRowsAhead];
+#pragma unroll
+    for (int u = 0; u < kRowsAhead; ++u) {
+      const int64_t i = i0 + u * step;
+      at[u] = i < n ? (index ? (int64_t)index[i] : i) : -1;
+    }
+    for (int c = lane * Q; c < f.d; c += T * Q) {
+      PackedCols<BITS, Q> p[kRowsAhead];
+#pragma unroll
+      for (int u = 0; u < kRowsAhead; ++u)
+        if (at[u] >= 0 && at[u] < rows) p[u].load(table + at[u] * f.row_bytes, f, c);
+#pragma unroll
+      for (int u = 0; u < kRowsAhead; ++u) {
+        const int64_t i = i0 + u * step;
+        float v[Q];
+        p[u].values(v);
+        if (i < n) store_cols<O, Q>(out + i * stride + c, f.d - c, v);
+      }
     }
   }
 }

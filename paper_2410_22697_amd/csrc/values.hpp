@@ -55,51 +55,36 @@ struct PackedRows {
   int64_t row_bytes;
 };
 
-// Where a row lies in a table, null for an index outside it.
-__device__ __forceinline__ const uint8_t* packed_row(const uint8_t* table, int64_t rows, int64_t i, int64_t row_bytes) {
-  return i >= 0 && i < rows ? table + i * row_bytes : nullptr;
-}
-
 // Q columns of a packed row from column c on (c a multiple of Q): codes and
-// their group's floats, one load each, and the values that they stand for.
+// their group's floats, and the values that they stand for; zeros until they
+// are loaded. A row's floats follow its codes, so that Q codes can be read from
+// any column on.
 template <int BITS, int Q>
 struct PackedCols {
   static constexpr int kBytes = Q * BITS / 8;  // 2, 4 or 8
-  uint32_t w[kBytes > 4 ? 2 : 1];
-  float step, lo;
+  typedef uint32_t raw __attribute__((ext_vector_type(kBytes > 4 ? 2 : 1), aligned(4)));
+  raw w = (raw)0;
+  float step = 0.0f, lo = 0.0f;
 
   __device__ __forceinline__ void load(const uint8_t* row, const PackedRows& f, int c) {
     const uint8_t* p = row + (int64_t)c * BITS / 8;
-    if constexpr (kBytes == 2) {
-      w[0] = *reinterpret_cast<const uint16_t*>(p);
-    } else {
-      w[0] = *reinterpret_cast<const uint32_t*>(p);
-      // a row's codes end on four bytes, not on eight
-      if constexpr (kBytes == 8) w[1] = c + 4 < f.d ? *reinterpret_cast<const uint32_t*>(p + 4) : 0u;
-    }
-    const int g = c >> f.group_log2;
-    const float* s = reinterpret_cast<const float*>(row + f.floats_at);
+    if constexpr (kBytes == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
+    else w = *reinterpret_cast<const raw*>(p);
+    const float* s = reinterpret_cast<const float*>(row + f.floats_at) + (c >> f.group_log2) * (BITS == 8 ? 1 : 2);
     if constexpr (BITS == 8) {
-      step = s[g];
-      lo = 0.0f;
+      step = s[0];
     } else {
-      lo = s[2 * g];
-      step = s[2 * g + 1];
+      lo = s[0];
+      step = s[1];
     }
   }
-  __device__ __forceinline__ void none() {
-    w[0] = 0;
-    if constexpr (kBytes == 8) w[1] = 0;
-    step = lo = 0.0f;
+  __device__ __forceinline__ float value(int q) const {
+    if constexpr (BITS == 8) return (float)(int8_t)(w[q / 4] >> (8 * (q % 4))) * step;
+    else return lo + (float)((w[q / 8] >> (4 * (q % 8))) & 15u) * step;
   }
   __device__ __forceinline__ void values(float* x) const {
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      if constexpr (BITS == 8)
-        x[q] = (float)(int8_t)(w[q / 4] >> (8 * (q % 4))) * step;
-      else
-        x[q] = lo + (float)((w[q / 8] >> (4 * (q % 8))) & 15u) * step;
-    }
+    for (int q = 0; q < Q; ++q) x[q] = value(q);
   }
 };
 
