@@ -10,8 +10,10 @@ gradients are also there as calls of their own. Wrong arguments raise
 ValueError here, or MassiveError where the library refuses them.
 """
 import ctypes
+import operator
 from typing import List, Optional, Sequence, Tuple
 
+import numpy as np
 import torch
 
 from . import massive
@@ -47,6 +49,9 @@ class _LinearGrads(ctypes.Structure):
 
 class _AdamwTensor(ctypes.Structure):
     _fields_ = [(f, _vp) for f in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", _i64)]
+
+
+_ADAMW_ROW = np.dtype([(f, np.uint64) for f in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", np.int64)])
 
 
 class _AdamwArgs(ctypes.Structure):
@@ -389,6 +394,13 @@ def linear_backward(dy, x, weight, act: str = "none", pre=None, x2=None, bias: b
 
 
 # ------------------------------------------------------------------------ AdamW
+_dtype_of = operator.attrgetter("dtype")
+
+
+def _pointers(tensors):
+    return np.fromiter(map(torch.Tensor.data_ptr, tensors), np.uint64, len(tensors))
+
+
 class AdamW:
     """AdamW over a list of tensors, contiguous and of one type (float32 or
     bfloat16), updated in place by `step`. state_bits 32 keeps the two moments
@@ -435,11 +447,29 @@ class AdamW:
             self.v = torch.zeros(total, dtype=torch.uint8, device=device)
             self.m_scale, self.v_scale = (torch.zeros(total // 256, device=device) for _ in range(2))
         self._list = (_AdamwTensor * len(self.params))()
+        self._table = np.frombuffer(self._list, dtype=_ADAMW_ROW)  # the same memory, by columns
         size = self.m.element_size()
-        for e, p, c, a in zip(self._list, self.params, self.copies, self.starts):
-            e.m, e.v, e.n = self.m.data_ptr() + a * size, self.v.data_ptr() + a * size, p.numel()
-            if state_bits == 8:
-                e.m_scale, e.v_scale = (s.data_ptr() + a // 256 * 4 for s in (self.m_scale, self.v_scale))
+        starts = np.array(self.starts, np.uint64)
+        self._table["m"], self._table["v"] = self.m.data_ptr() + starts * size, self.v.data_ptr() + starts * size
+        if state_bits == 8:
+            self._table["m_scale"] = self.m_scale.data_ptr() + starts // 256 * 4
+            self._table["v_scale"] = self.v_scale.data_ptr() + starts // 256 * 4
+        self._sizes = np.array([p.numel() for p in self.params], np.int64)
+        self._table["param"] = _pointers(self.params)
+        self._table["copy"] = [0 if c is None else c.data_ptr() for c in self.copies]
+
+    def _own_memory(self):
+        """The parameters' and copies' memory may have been replaced since it was last seen."""
+        now = _pointers(self.params)
+        for i in np.flatnonzero(now != self._table["param"]):
+            p = self.params[i]
+            if p.dtype != self.dtype or p.numel() != self._sizes[i] or not p.is_contiguous():
+                raise ValueError("a parameter's memory was replaced by another type, size or layout")
+            _on_gpu(p)
+        self._table["param"] = now
+        for i, c in enumerate(self.copies):
+            if c is not None and c.data_ptr() != self._table["copy"][i]:
+                raise ValueError("a copy's memory was replaced")
 
     def step(self, grads: Optional[Sequence] = None):
         """One step. grads: a contiguous tensor of each parameter's shape, all
@@ -448,25 +478,25 @@ class AdamW:
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params):
             raise ValueError("%d parameters, and %d gradients" % (len(self.params), len(grads)))
-        dtype = None
-        here = _on_gpu(*self.params)
-        for e, p, c, g, a in zip(self._list, self.params, self.copies, grads, self.starts):
-            if g is None:
-                e.n = 0
-                continue
-            if g.numel() != p.numel() or not g.is_contiguous() or g.get_device() != here:
-                raise ValueError("a gradient must be a contiguous tensor of its parameter's shape, on cuda:%d" % here)
-            if dtype is None:
-                dtype = g.dtype
-            if g.dtype != dtype or dtype not in _TYPES:
-                raise ValueError("gradients must be of one type, float32 or bfloat16")
-            # (a parameter's memory may have been replaced since the last step)
-            e.param, e.grad, e.n = p.data_ptr(), g.data_ptr(), p.numel()
-            e.copy = None if c is None else c.data_ptr()
-        if dtype is None:
-            return
+        there = slice(None)
+        if any(g is None for g in grads):
+            there = np.array([i for i, g in enumerate(grads) if g is not None], np.int64)
+            grads = [grads[i] for i in there]
+            if not grads:
+                return
+        here = _on_gpu(self.params[0])
+        types = set(map(_dtype_of, grads))
+        if len(types) != 1 or not types <= _TYPES.keys():
+            raise ValueError("gradients must be of one type, float32 or bfloat16")
+        if set(map(torch.Tensor.get_device, grads)) != {here} or not all(map(torch.Tensor.is_contiguous, grads)) or \
+                not np.array_equal(np.fromiter(map(torch.Tensor.numel, grads), np.int64, len(grads)), self._sizes[there]):
+            raise ValueError("a gradient must be a contiguous tensor of its parameter's shape, on cuda:%d" % here)
+        self._own_memory()
+        self._table["n"] = 0
+        self._table["n"][there] = self._sizes[there]
+        self._table["grad"][there] = _pointers(grads)
         a = _AdamwArgs(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, self.t + 1, self.state_bits,
-                       _TYPES[self.dtype], _TYPES[dtype], 0)
+                       _TYPES[self.dtype], _TYPES[types.pop()], 0)
         _check(_load().massive_adamw(self._list, len(self._list), ctypes.byref(a), _stream(here)))
         self.t += 1
 
