@@ -94,17 +94,11 @@ __global__ __launch_bounds__(kFewNT) void k_linear_few(LinearForward<T> a, int t
 }
 
 template <typename T, bool SLOPE>
-__global__ __launch_bounds__(kFewNT) void k_linear_dx_few(LinearDx<T> a) {
-  const int tiles = a.tiles[0] + a.tiles[1];
-  int at = (int)(blockIdx.x % tiles);
-  const int s = at >= a.tiles[0] ? 1 : 0;
-  at -= s ? a.tiles[0] : 0;
+__global__ __launch_bounds__(kFewNT) void k_linear_dx_few(LinearDx<T> a, int tiles_n) {
   const Operand<T> dz[1] = {a.dz};
-  const Weights<T> w[1] = {a.w[s]};
-  T* dx = a.dx[s];
-  const int64_t stride = a.dx_stride[s];
-  few_product<T, SLOPE, true, 1>(dz, w, (int64_t)(blockIdx.x / tiles) * 32, a.rows, at * 32, a.k[s],
-                              [&](int64_t row, int col, float v) { dx[row * stride + col] = (T)v; });
+  const Weights<T> w[1] = {a.w};
+  few_product<T, SLOPE, true, 1>(dz, w, (int64_t)(blockIdx.x / tiles_n) * 32, a.rows, (int)(blockIdx.x % tiles_n) * 32, a.cols,
+                                 [&](int64_t row, int col, float v) { linear_dx_store(a, row, col, v); });
 }
 
 }  // namespace ms

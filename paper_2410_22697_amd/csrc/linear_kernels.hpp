@@ -198,15 +198,33 @@ __device__ __forceinline__ void linear_finish(const LinearForward<T>& a, int64_t
 }
 
 // ---------------------------------------------------------------------- dx
+// The columns asked for, of the first input and then of the second, as one row.
 template <typename T>
 struct LinearDx {
   Operand<T> dz;
-  Weights<T> w[2];  // of each input's columns, across k
+  Weights<T> w;  // of those columns, across k
   T* dx[2];
   int64_t dx_stride[2];
   int64_t rows;
-  int k[2], tiles[2];  // columns of each input, and their tiles (0 where its gradient is not asked for)
+  int cols, split;  // column split is the second input's first
 };
+
+template <typename T>
+__device__ __forceinline__ void linear_dx_store(const LinearDx<T>& a, int64_t row, int col, float v) {
+  const int s = col >= a.split ? 1 : 0;
+  a.dx[s][row * a.dx_stride[s] + col - (s ? a.split : 0)] = (T)v;
+}
+// Eight of them, all there.
+template <typename T>
+__device__ __forceinline__ void linear_dx_store(const LinearDx<T>& a, int64_t row, int col, const float (&v)[8]) {
+  if (col < a.split && col + 8 > a.split) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) linear_dx_store(a, row, col + q, v[q]);
+    return;
+  }
+  const int s = col >= a.split ? 1 : 0;
+  store_cols<T, 8>(a.dx[s] + row * a.dx_stride[s] + col - (s ? a.split : 0), 8, v);
+}
 
 // -------------------------------------------------------------------- join
 // Adds the parts, of dw (rows of `cols` values) and of dbias.

@@ -315,19 +315,14 @@ __global__ __launch_bounds__(kStreamNT) void k_linear_dx_stream(LinearDx<T> a, i
   int64_t tile, step;
   int group;
   stream_place(groups, tile, step, group);
-  const int s = group >= a.tiles[0] ? 1 : 0;
-  const int n0 = (group - (s ? a.tiles[0] : 0)) * NB * 32;
-  const StreamSegment<T> segs[2] = {{a.dz, a.w[s], (int)((a.dz.K * sizeof(T) + 255) / 256)}, {a.dz, a.w[s], 0}};
-  T* dx = a.dx[s];
-  const int64_t stride = a.dx_stride[s];
-  const int k = a.k[s];
+  const StreamSegment<T> segs[2] = {{a.dz, a.w, (int)((a.dz.K * sizeof(T) + 255) / 256)}, {a.dz, a.w, 0}};
   stream_product<T, SLOPE, true, NB, RESIDENT>(
-      segs, a.rows, n0, k, tile, (a.rows + kStreamRows - 1) / kStreamRows, step, stream_lds, lds_weights,
+      segs, a.rows, group * NB * 32, a.cols, tile, (a.rows + kStreamRows - 1) / kStreamRows, step, stream_lds, lds_weights,
       [&](int64_t r0, int c0, const float* turn) {
         stream_out(
-            turn, (int)min(a.rows - r0, (int64_t)16), k - c0,
-            [&](int r, int c, float* v) { store_cols<T, 8>(dx + (r0 + r) * stride + c0 + c, 8, v); },
-            [&](int r, int c, float v) { dx[(r0 + r) * stride + c0 + c] = (T)v; });
+            turn, (int)min(a.rows - r0, (int64_t)16), a.cols - c0,
+            [&](int r, int c, const float (&v)[8]) { linear_dx_store(a, r0 + r, c0 + c, v); },
+            [&](int r, int c, float v) { linear_dx_store(a, r0 + r, c0 + c, v); });
       });
 }
 

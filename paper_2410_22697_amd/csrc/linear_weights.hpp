@@ -22,12 +22,14 @@ struct LinearDw {
   Operand<T> dz, x[2];  // R rows (the reduction), K columns
   float *dw, *dbias;    // [parts][n][k0 + k1] and [parts][n], null where not asked for
   int64_t rows, part;   // rows of a part, a multiple of a step's
-  int n, k[2], tiles[2], tiles_n;
+  int n, k[2], second;  // second: the position of the second input's first column
+  int tiles_n, tiles_k;
 };
 
-// Columns are read in vectors of 16 bytes, the last one of a row ending with
-// the row: position `at` of a tile that begins at column 0 holds column
-// dw_column(at), or nothing (-1; also the columns that the last vector repeats).
+// Columns are read in vectors of 16 bytes, the last one of an input ending with
+// its row: position `at` holds column dw_column(at), or nothing (-1; also the
+// columns that the last vector repeats). The second input's positions begin at
+// a whole vector behind the first one's.
 template <typename T>
 __device__ __forceinline__ int dw_column(int at, int columns) {
   constexpr int kV = 16 / sizeof(T);
@@ -83,23 +85,16 @@ __global__ __launch_bounds__(kDwNT) void k_linear_dw(LinearDw<T> a, int64_t bloc
   constexpr int kWn = TN / 64, kWk = 8 / kWn, kI = 2, kJ = TK / kWk / 32;  // waves, and 32x32 squares of a wave
   constexpr int kTileN = kRows * dw_pitch<T, TN>(), kTileK = kRows * dw_pitch<T, TK>();
   __shared__ __align__(16) char lds[2 * (kTileN + kTileK)];
-  const int tiles = a.tiles[0] + a.tiles[1];
   const int64_t tile = tile_of_block(blockIdx.x, blocks);
-  const int64_t part = tile / (tiles * a.tiles_n);
-  const int in = (int)(tile % (tiles * a.tiles_n));
-  const int n0 = in / tiles * TN;
-  int at = in % tiles;
-  const bool bias = a.dbias && at == 0;
-  const int seg = at >= a.tiles[0] ? 1 : 0;
-  at -= seg ? a.tiles[0] : 0;
-  const int k0 = at * TK;
-  const Operand<T>& x = a.x[seg];
+  const int64_t part = tile / (a.tiles_k * a.tiles_n);
+  const int in = (int)(tile % (a.tiles_k * a.tiles_n));
+  const int n0 = in / a.tiles_k * TN, k0 = in % a.tiles_k * TK;
+  const bool bias = a.dbias && k0 == 0;
   const int64_t first = part * a.part, end = min(a.rows, first + a.part);
   const int steps = (int)((end - first + kRows - 1) / kRows);
   const int lane = lane_id();
   const int wave = wave_uniform((int32_t)wave_id());
   const int wn = wave % kWn * 64, wk = wave / kWn * (kJ * 32);
-  const int cols_n = a.n - n0, cols_k = a.k[seg] - k0;
 
   u32x4 dy[2][kPn], z[2][SLOPE ? kPn : 1], xs[2][kPk];
   float sums[kV] = {};
@@ -109,21 +104,23 @@ __global__ __launch_bounds__(kDwNT) void k_linear_dw(LinearDw<T> a, int64_t bloc
     for (int i = 0; i < kPn; ++i) {
       const int id = threadIdx.x + i * kDwNT;
       const int64_t r = first + (int64_t)step * kRows + id / kVn;
-      const int c = id % kVn * kV;
+      const int c = n0 + id % kVn * kV;
       dy[S][i] = (u32x4)0u;
       if constexpr (SLOPE) z[S][i] = (u32x4)0u;
-      if (id < kRows * kVn && r < end && c < cols_n) {
-        dy[S][i] = dw_load(a.dz.p + r * a.dz.stride + n0, c, cols_n);
-        if constexpr (SLOPE) z[S][i] = dw_load(a.dz.pre + r * a.dz.pre_stride + n0, c, cols_n);
+      if (id < kRows * kVn && r < end && c < a.n) {
+        dy[S][i] = dw_load(a.dz.p + r * a.dz.stride, c, a.n);
+        if constexpr (SLOPE) z[S][i] = dw_load(a.dz.pre + r * a.dz.pre_stride, c, a.n);
       }
     }
 #pragma unroll
     for (int i = 0; i < kPk; ++i) {
       const int id = threadIdx.x + i * kDwNT;
       const int64_t r = first + (int64_t)step * kRows + id / kVk;
-      const int c = id % kVk * kV;
+      const int at = k0 + id % kVk * kV, seg = at >= a.second ? 1 : 0, c = at - (seg ? a.second : 0);
+      const T* x = seg ? a.x[1].p + r * a.x[1].stride : a.x[0].p + r * a.x[0].stride;
+      const int columns = seg ? a.k[1] : a.k[0];
       xs[S][i] = (u32x4)0u;
-      if (id < kRows * kVk && r < end && c < cols_k) xs[S][i] = dw_load(x.p + r * x.stride + k0, c, cols_k);
+      if (id < kRows * kVk && r < end && c < columns) xs[S][i] = dw_load(x, c, columns);
     }
   };
   auto put = [&](auto set) {
@@ -195,27 +192,29 @@ __global__ __launch_bounds__(kDwNT) void k_linear_dw(LinearDw<T> a, int64_t bloc
       for (int q = 0; q < kV; ++q) turn[threadIdx.x / kVn * TN + threadIdx.x % kVn * kV + q] = sums[q];
     }
     __syncthreads();
-    const int col = (int)threadIdx.x < TN ? dw_column<T>(threadIdx.x, cols_n) : -1;
+    const int col = (int)threadIdx.x < TN ? dw_column<T>(n0 + threadIdx.x, a.n) : -1;
     if (col >= 0) {
       float t = 0.0f;
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) t += turn[g * TN + threadIdx.x];
-      a.dbias[part * a.n + n0 + col] = t;
+      a.dbias[part * a.n + col] = t;
     }
   }
   if (!a.dw) return;
   const int all = a.k[0] + a.k[1];
-  float* dw = a.dw + part * a.n * (int64_t)all + (seg ? a.k[0] : 0) + k0;
+  float* dw = a.dw + part * a.n * (int64_t)all;
 #pragma unroll
   for (int j = 0; j < kJ; ++j) {
-    const int ck = dw_column<T>(wk + 32 * j + lane % 32, cols_k);
+    const int at = k0 + wk + 32 * j + lane % 32, seg = at >= a.second ? 1 : 0;
+    int ck = dw_column<T>(at - (seg ? a.second : 0), a.k[seg]);
     if (ck < 0) continue;
+    ck += seg ? a.k[0] : 0;
 #pragma unroll
     for (int i = 0; i < kI; ++i)
 #pragma unroll
       for (int g = 0; g < 16; ++g) {
-        const int cn = dw_column<T>(wn + 32 * i + 8 * (g / 4) + 4 * (lane / 32) + g % 4, cols_n);
-        if (cn >= 0) dw[(int64_t)(n0 + cn) * all + ck] = acc[i][j][g];
+        const int cn = dw_column<T>(n0 + wn + 32 * i + 8 * (g / 4) + 4 * (lane / 32) + g % 4, a.n);
+        if (cn >= 0) dw[(int64_t)cn * all + ck] = acc[i][j][g];
       }
   }
 }

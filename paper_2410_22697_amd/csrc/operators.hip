@@ -9,6 +9,7 @@
 #include <cstdint>
 #include <tuple>
 #include <type_traits>
+#include <utility>
 
 #include "../../include/massive.h"
 #include "adamw_kernels.hpp"
@@ -353,20 +354,19 @@ int check_layer(int64_t rows, int32_t n, int32_t k, int32_t k_second, int32_t ty
   return MASSIVE_OK;
 }
 
-// The streaming form's shape for n outputs (of each of `parts` groups that have
-// no block in common) from `chunks` chunks of k: blocks of 32 outputs that a
-// wave accumulates, and whether their weights stay in LDS. As many as there
-// are outputs, unless fewer give more of the chip's 256 CUs work.
+// The streaming form's shape for n outputs from `chunks` chunks of k: blocks of
+// 32 outputs that a wave accumulates, and whether their weights stay in LDS. As
+// many as there are outputs, unless fewer give more of the chip's 256 CUs work.
 struct StreamPlan {
   int nb;
   bool resident;
   int lds_weights, lds;
 };
-StreamPlan stream_plan(int64_t rows, int64_t n, int parts, int64_t chunks) {
+StreamPlan stream_plan(int64_t rows, int64_t n, int64_t chunks) {
   StreamPlan p;
   auto bytes = [&](int nb) { return chunks * nb * ms::kStreamBlockBytes; };
   p.nb = n <= 32 ? 1 : n <= 64 ? 2 : n <= 128 || bytes(8) > ms::kStreamLds ? 4 : 8;
-  while (p.nb > 2 && cdiv(rows, ms::kStreamRows) * cdiv(n, p.nb * 32) * parts < 256) p.nb /= 2;
+  while (p.nb > 2 && cdiv(rows, ms::kStreamRows) * cdiv(n, p.nb * 32) < 256) p.nb /= 2;
   p.resident = bytes(p.nb) <= ms::kStreamLds;
   p.lds_weights = (int)(p.resident ? bytes(p.nb) : 2 * p.nb * ms::kStreamBlockBytes);
   p.lds = p.lds_weights + ms::kStreamNT / MS_WAVE * ms::kStreamTurn + p.nb * 32 * 4;  // weights, turns, bias
@@ -417,7 +417,7 @@ int linear(const massive_linear_args* a, void* stream) {
   f.n = a->n;
   f.act = a->act;
   if (streams(a->rows, a->n, 21)) {
-    const StreamPlan p = stream_plan(a->rows, a->n, 1, cdiv(a->k * sizeof(T), 256) + cdiv(a->k_second * sizeof(T), 256));
+    const StreamPlan p = stream_plan(a->rows, a->n, cdiv(a->k * sizeof(T), 256) + cdiv(a->k_second * sizeof(T), 256));
     const int groups = (int)cdiv(a->n, p.nb * 32);
     return with_stream(p, [&](auto nb, auto resident) {
       return launch("massive_linear", ms::k_linear_stream<T, nb(), resident()>, stream_blocks(p, a->rows, groups), ms::kStreamNT, p.lds,
@@ -430,24 +430,33 @@ int linear(const massive_linear_args* a, void* stream) {
   return launch("massive_linear", ms::k_linear_few<T>, blocks, ms::kFewNT, 0, stream, f, tiles_n);
 }
 
-// dw's tiles, and the parts into which its rows are split: enough blocks for
-// the chip, and parts of no less than eight steps of rows where there are.
+// dw's tiles, outputs by columns of both inputs (each input's in whole vectors),
+// and the parts into which its rows are split. The tile is the one that
+// multiplies the fewest zeros; of equal ones the tallest, which reads x the
+// fewest times. Enough parts for the chip, none of less than eight steps of rows
+// where there are more.
 struct DwPlan {
-  bool narrow;  // tiles of 64 outputs by 256 columns, else of 256 by 128
-  int tiles_n, tiles[2];
-  int64_t part, parts, dw_floats, bytes;
+  int bn, bk, second;
+  int64_t tiles_n, tiles_k, part, parts, dw_floats, bytes;
 };
 DwPlan dw_plan(const massive_linear_grads* a) {
   DwPlan p = {};
-  p.narrow = a->n <= 64;
-  const int bn = p.narrow ? 64 : 256, bk = p.narrow ? 256 : 128;
-  const int step = 64 / size_of(a->type);
-  p.tiles_n = (int)cdiv(a->n, bn);
-  p.tiles[0] = (int)cdiv(a->k, bk);
-  p.tiles[1] = (int)cdiv(a->k_second, bk);
-  const int64_t tiles = (int64_t)p.tiles_n * (p.tiles[0] + p.tiles[1]);
+  const int vector = 16 / size_of(a->type), step = 64 / size_of(a->type);
+  p.second = (int)round_up(a->k, vector);
+  const int64_t cols = p.second + a->k_second;
+  int64_t least = 0;
+  for (const auto& t : {std::pair<int, int>(256, 128), std::pair<int, int>(128, 128), std::pair<int, int>(64, 256)}) {
+    const int64_t area = round_up(a->n, t.first) * round_up(cols, t.second);
+    if (!p.bn || area < least) {
+      least = area;
+      p.bn = t.first;
+      p.bk = t.second;
+    }
+  }
+  p.tiles_n = cdiv(a->n, p.bn);
+  p.tiles_k = cdiv(cols, p.bk);
   const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 8 * step));
-  p.part = round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, (p.narrow ? 512 : 256) / tiles))), step);
+  p.part = round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, (p.bn == 256 ? 256 : 512) / (p.tiles_n * p.tiles_k)))), step);
   p.parts = cdiv(a->rows, p.part);
   p.dw_floats = a->dw ? p.parts * a->n * ((int64_t)a->k + a->k_second) : 0;
   p.bytes = 4 * (round_up(p.dw_floats, 4) + (a->dbias ? p.parts * a->n : 0));
@@ -466,31 +475,29 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
   if (a->dx || a->dx_second) {
     ms::LinearDx<T> f;
     f.dz = operand<T>(a->dy, a->dy_stride, a->rows, a->n, a->pre, a->pre_stride, a->act);
-    for (int s = 0; s < 2; ++s) f.w[s] = {(const T*)a->w + (s ? k[0] : 0), a->w_stride};
+    const int k0 = a->dx ? a->k : 0, k1 = a->dx_second ? a->k_second : 0;
+    f.w = {(const T*)a->w + (a->dx ? 0 : k[0]), a->w_stride};
     f.dx[0] = (T*)a->dx;
     f.dx[1] = (T*)a->dx_second;
     f.dx_stride[0] = a->dx_stride;
     f.dx_stride[1] = a->dx_second_stride;
     f.rows = a->rows;
-    f.k[0] = a->k;
-    f.k[1] = a->k_second;
-    const int64_t k0 = a->dx ? k[0] : 0, k1 = a->dx_second ? k[1] : 0;
-    const bool stream_it = streams(a->rows, round_up(k0, 32) + k1, sizeof(T) == 2 ? 20 : 21);
-    const StreamPlan p = stream_plan(a->rows, std::max(k0, k1), k0 && k1 ? 2 : 1, cdiv(a->n * sizeof(T), 256));
-    auto go_stream = [&](auto nb, auto resident) {
-      for (int s = 0; s < 2; ++s) f.tiles[s] = f.dx[s] ? (int)cdiv(k[s], nb() * 32) : 0;
-      const int groups = f.tiles[0] + f.tiles[1];
-      const int64_t blocks = stream_blocks(p, a->rows, groups);
-      return slope ? launch("massive_linear_backward", ms::k_linear_dx_stream<T, true, nb(), resident()>, blocks, ms::kStreamNT, p.lds, stream, f, groups, p.lds_weights)
-                   : launch("massive_linear_backward", ms::k_linear_dx_stream<T, false, nb(), resident()>, blocks, ms::kStreamNT, p.lds, stream, f, groups, p.lds_weights);
-    };
-    auto go_few = [&] {
-      for (int s = 0; s < 2; ++s) f.tiles[s] = f.dx[s] ? (int)cdiv(k[s], 32) : 0;
-      const int64_t blocks = cdiv(a->rows, 32) * (f.tiles[0] + f.tiles[1]);
+    f.cols = k0 + k1;
+    f.split = k0;
+    int rc;
+    if (streams(a->rows, f.cols, sizeof(T) == 2 ? 20 : 21)) {
+      const StreamPlan p = stream_plan(a->rows, f.cols, cdiv(a->n * sizeof(T), 256));
+      const int groups = (int)cdiv(f.cols, p.nb * 32);
+      rc = with_stream(p, [&](auto nb, auto resident) {
+        return launch("massive_linear_backward", slope ? ms::k_linear_dx_stream<T, true, nb(), resident()> : ms::k_linear_dx_stream<T, false, nb(), resident()>,
+                      stream_blocks(p, a->rows, groups), ms::kStreamNT, p.lds, stream, f, groups, p.lds_weights);
+      });
+    } else {
+      const int tiles_n = (int)cdiv(f.cols, 32);
+      const int64_t blocks = cdiv(a->rows, 32) * tiles_n;
       if (blocks > kMostBlocks / 2) REFUSE("too many columns for so many rows");
-      return launch("massive_linear_backward", slope ? ms::k_linear_dx_few<T, true> : ms::k_linear_dx_few<T, false>, blocks, ms::kFewNT, 0, stream, f);
-    };
-    const int rc = stream_it ? with_stream(p, go_stream) : go_few();
+      rc = launch("massive_linear_backward", slope ? ms::k_linear_dx_few<T, true> : ms::k_linear_dx_few<T, false>, blocks, ms::kFewNT, 0, stream, f, tiles_n);
+    }
     if (rc) return rc;
   }
   if (!a->dw && !a->dbias) return MASSIVE_OK;
@@ -504,18 +511,21 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
   f.rows = a->rows;
   f.part = p.part;
   f.n = a->n;
-  for (int s = 0; s < 2; ++s) {
-    f.k[s] = (int)k[s];
-    f.tiles[s] = p.tiles[s];
-  }
-  f.tiles_n = p.tiles_n;
-  const int64_t blocks = p.parts * p.tiles_n * (p.tiles[0] + p.tiles[1]);
-  if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
-  const char* what = "massive_linear_backward";
-  const int rc = p.narrow ? (slope ? launch(what, ms::k_linear_dw<T, true, 64, 256>, blocks, ms::kDwNT, 0, stream, f, blocks)
-                                   : launch(what, ms::k_linear_dw<T, false, 64, 256>, blocks, ms::kDwNT, 0, stream, f, blocks))
-                          : (slope ? launch(what, ms::k_linear_dw<T, true, 256, 128>, blocks, ms::kDwNT, 0, stream, f, blocks)
-                                   : launch(what, ms::k_linear_dw<T, false, 256, 128>, blocks, ms::kDwNT, 0, stream, f, blocks));
+  f.k[0] = a->k;
+  f.k[1] = a->k_second;
+  f.second = p.second;
+  f.tiles_n = (int)p.tiles_n;
+  f.tiles_k = (int)p.tiles_k;
+  const int64_t blocks = p.parts * p.tiles_n * p.tiles_k;
+  if (blocks > kMostBlocks / 2) REFUSE("too many rows and columns for one call");
+  auto go = [&](auto bn, auto bk) {
+    return launch("massive_linear_backward", slope ? ms::k_linear_dw<T, true, bn(), bk()> : ms::k_linear_dw<T, false, bn(), bk()>, blocks, ms::kDwNT, 0,
+                  stream, f, blocks);
+  };
+  using std::integral_constant;
+  const int rc = p.bn == 256   ? go(integral_constant<int, 256>(), integral_constant<int, 128>())
+                 : p.bn == 128 ? go(integral_constant<int, 128>(), integral_constant<int, 128>())
+                               : go(integral_constant<int, 64>(), integral_constant<int, 256>());
   if (rc) return rc;
   const int64_t values = (int64_t)a->n * ((a->dw ? k[0] + k[1] : 0) + (a->dbias ? 1 : 0));
   return launch("massive_linear_backward", ms::k_linear_join<T>, std::min<int64_t>(cdiv(values, ms::kLinNT), 4096), ms::kLinNT, 0,
