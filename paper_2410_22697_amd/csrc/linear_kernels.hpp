@@ -23,89 +23,73 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 enum { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
 
 // ------------------------------------------------------------- activations
-// Results in bf16 take Phi from Abramowitz and Stegun's 7.1.26: for s = |z|,
+// Phi is Abramowitz and Stegun's 7.1.26: for s = |z|,
 //   1 - Phi(s) = (a1 t + .. + a5 t^5) exp(-s^2 / 2) / 2, t = 1 / (1 + p s / sqrt(2)),
-// with an error of 1.5e-7 at most, which shares its exponential with the slope.
-// Results in fp32 take the compiler's erfcf and expf.
+// which is off by 0.75e-7 at most and shares its exponential with the slope:
+// gelu's slope is ~20 instructions, where the compiler's erfcf and expf made a
+// wide layer's gradients in fp32 half as slow again as the matrix unit is.
+// Exponentials and reciprocals are the hardware's, one unit in the last place.
 constexpr float kErfP = 0.3275911f * 0.70710678f;
+constexpr float kLog2e = 1.44269504f;
 
 // (a1 + a2 t + .. + a5 t^4) / 2
 __device__ __forceinline__ float tail_poly(float t) {
   return 0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f)));
 }
-constexpr float kLog2e = 1.44269504f;
+// exp(-z^2 / 2) and 1 / (1 + exp(-z))
+__device__ __forceinline__ float bell(float z) { return __builtin_amdgcn_exp2f(z * (z * (-0.5f * kLog2e))); }
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * z)); }
 
-template <typename T>
 __device__ __forceinline__ float act_value(float z, int act) {
   if (act == kActRelu) return z <= 0.0f ? 0.0f : z;  // a NaN stays one
   if (act == kActGelu) {
-    if constexpr (sizeof(T) == 2) {
-      const float t = __builtin_amdgcn_rcpf(1.0f + kErfP * fabsf(z));
-      const float e = __builtin_amdgcn_exp2f(z * (z * (-0.5f * kLog2e)));
-      return z * (0.5f + copysignf(0.5f - e * (t * tail_poly(t)), z));
-    } else {
-      return z * (0.5f * erfcf(-z * 0.70710678f));
-    }
+    const float t = __builtin_amdgcn_rcpf(1.0f + kErfP * fabsf(z));
+    return z * (0.5f + copysignf(0.5f - bell(z) * (t * tail_poly(t)), z));
   }
-  if (act == kActSilu) {
-    if constexpr (sizeof(T) == 2) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * z));
-    else return z / (1.0f + expf(-z));
-  }
-  return z;
+  return act == kActSilu ? z * logistic(z) : z;
 }
 
 // g * act'(z). A slope's products with z are taken with z held within bounds
 // beyond which the other factor is 0, so that infinities have their limits'
 // slopes; a NaN stays one by the exponential.
-template <typename T>
 __device__ __forceinline__ float act_grad(float g, float z, int act) {
   if (act == kActRelu) return z > 0.0f ? g : 0.0f;
   if (act == kActGelu) {
     // Phi(z) + z phi(z) is r below 0 and 1 - r above, r = (1 - Phi(s)) - s phi(s)
-    if constexpr (sizeof(T) == 2) {
-      const float s = fminf(fabsf(z), 40.0f);
-      const float t = __builtin_amdgcn_rcpf(1.0f + kErfP * s);
-      const float e = __builtin_amdgcn_exp2f(z * (z * (-0.5f * kLog2e)));
-      const float half_less_r = 0.5f - e * (t * tail_poly(t) - 0.39894228f * s);
-      return g * (0.5f + copysignf(half_less_r, z));
-    } else {
-      const float s = fminf(fmaxf(z, -40.0f), 40.0f);
-      return g * (0.5f * erfcf(-z * 0.70710678f) + s * (expf(-0.5f * z * z) * 0.39894228f));
-    }
+    const float s = fminf(fabsf(z), 40.0f);
+    const float t = __builtin_amdgcn_rcpf(1.0f + kErfP * s);
+    const float half_less_r = 0.5f - bell(z) * (t * tail_poly(t) - 0.39894228f * s);
+    return g * (0.5f + copysignf(half_less_r, z));
   }
-  const float s = fminf(fmaxf(z, -100.0f), 100.0f);
-  float q;
-  if constexpr (sizeof(T) == 2) q = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * z));
-  else q = 1.0f / (1.0f + expf(-z));
+  const float s = fminf(fmaxf(z, -100.0f), 100.0f), q = logistic(z);
   return g * (q + q * (s - s * q));
 }
 
 // The same for several values: the activation is the same for all of them.
-template <typename T>
 __device__ __forceinline__ void act_values(float (&z)[8], int act) {
   if (act == kActNone) return;
   if (act == kActRelu) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) z[q] = act_value<T>(z[q], kActRelu);
+    for (int q = 0; q < 8; ++q) z[q] = act_value(z[q], kActRelu);
   } else if (act == kActGelu) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) z[q] = act_value<T>(z[q], kActGelu);
+    for (int q = 0; q < 8; ++q) z[q] = act_value(z[q], kActGelu);
   } else {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) z[q] = act_value<T>(z[q], kActSilu);
+    for (int q = 0; q < 8; ++q) z[q] = act_value(z[q], kActSilu);
   }
 }
 template <typename T, int Q>
 __device__ __forceinline__ void act_grads(cols_t<T, Q>& g, const cols_t<T, Q>& z, int act) {
   if (act == kActRelu) {
 #pragma unroll
-    for (int q = 0; q < Q; ++q) g[q] = (T)act_grad<T>((float)g[q], (float)z[q], kActRelu);
+    for (int q = 0; q < Q; ++q) g[q] = (T)act_grad((float)g[q], (float)z[q], kActRelu);
   } else if (act == kActGelu) {
 #pragma unroll
-    for (int q = 0; q < Q; ++q) g[q] = (T)act_grad<T>((float)g[q], (float)z[q], kActGelu);
+    for (int q = 0; q < Q; ++q) g[q] = (T)act_grad((float)g[q], (float)z[q], kActGelu);
   } else {
 #pragma unroll
-    for (int q = 0; q < Q; ++q) g[q] = (T)act_grad<T>((float)g[q], (float)z[q], kActSilu);
+    for (int q = 0; q < Q; ++q) g[q] = (T)act_grad((float)g[q], (float)z[q], kActSilu);
   }
 }
 
@@ -192,7 +176,7 @@ struct LinearForward {
 template <typename T>
 __device__ __forceinline__ void linear_finish(const LinearForward<T>& a, int64_t row, int col, float z) {
   if (a.pre) a.pre[row * a.pre_stride + col] = (T)z;
-  z = act_value<T>(z, a.act);
+  z = act_value(z, a.act);
   if (a.residual) z += (float)a.residual[row * a.residual_stride + col];
   a.y[row * a.y_stride + col] = (T)z;
 }

@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kStreamNT) void k_linear_stream(LinearForward<T> a,
 #pragma unroll
               for (int q = 0; q < 8; ++q) z[q] += q < 4 ? lo[q % 4] : hi[q % 4];
               if (a.pre) store_cols<T, 8>(a.pre + row * a.pre_stride + c0 + c, 8, z);
-              act_values<T>(z, a.act);
+              act_values(z, a.act);
               if (a.residual) {
                 float t[8];
                 load_cols<T, 8>(a.residual + row * a.residual_stride + c0 + c, 8, t);

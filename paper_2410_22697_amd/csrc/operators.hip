@@ -356,16 +356,20 @@ int check_layer(int64_t rows, int32_t n, int32_t k, int32_t k_second, int32_t ty
 
 // The streaming form's shape for n outputs from `chunks` chunks of k: blocks of
 // 32 outputs that a wave accumulates, and whether their weights stay in LDS. As
-// many as there are outputs, unless fewer give more of the chip's 256 CUs work.
+// many as there are outputs, unless fewer give more of the chip's 256 CUs work;
+// eight (WIDE) only in bf16 without a slope, where the accumulators and the rows
+// on their way fit the registers and the matrix unit does not set the pace (240K
+// rows, 64 + 64 -> 256 in bf16: 64 us with eight, 72 with four).
 struct StreamPlan {
   int nb;
   bool resident;
   int lds_weights, lds;
 };
+template <bool WIDE>
 StreamPlan stream_plan(int64_t rows, int64_t n, int64_t chunks) {
   StreamPlan p;
   auto bytes = [&](int nb) { return chunks * nb * ms::kStreamBlockBytes; };
-  p.nb = n <= 32 ? 1 : n <= 64 ? 2 : n <= 128 || bytes(8) > ms::kStreamLds ? 4 : 8;
+  p.nb = n <= 32 ? 1 : n <= 64 ? 2 : n <= 128 || !WIDE || bytes(8) > ms::kStreamLds ? 4 : 8;
   while (p.nb > 2 && cdiv(rows, ms::kStreamRows) * cdiv(n, p.nb * 32) < 256) p.nb /= 2;
   p.resident = bytes(p.nb) <= ms::kStreamLds;
   p.lds_weights = (int)(p.resident ? bytes(p.nb) : 2 * p.nb * ms::kStreamBlockBytes);
@@ -381,10 +385,11 @@ int64_t stream_blocks(const StreamPlan& p, int64_t rows, int groups) {
 }
 
 // f(blocks of 32 outputs, whether they stay), both as types.
-template <typename F>
+template <bool WIDE, typename F>
 int with_stream(const StreamPlan& p, F f) {
   using std::integral_constant;
-  if (p.nb == 8) return f(integral_constant<int, 8>(), std::true_type());
+  if constexpr (WIDE)
+    if (p.nb == 8) return f(integral_constant<int, 8>(), std::true_type());
   if (p.nb == 4) return p.resident ? f(integral_constant<int, 4>(), std::true_type()) : f(integral_constant<int, 4>(), std::false_type());
   if (p.nb == 2) return p.resident ? f(integral_constant<int, 2>(), std::true_type()) : f(integral_constant<int, 2>(), std::false_type());
   return p.resident ? f(integral_constant<int, 1>(), std::true_type()) : f(integral_constant<int, 1>(), std::false_type());
@@ -417,9 +422,10 @@ int linear(const massive_linear_args* a, void* stream) {
   f.n = a->n;
   f.act = a->act;
   if (streams(a->rows, a->n, 21)) {
-    const StreamPlan p = stream_plan(a->rows, a->n, cdiv(a->k * sizeof(T), 256) + cdiv(a->k_second * sizeof(T), 256));
+    constexpr bool kWide = sizeof(T) == 2;
+    const StreamPlan p = stream_plan<kWide>(a->rows, a->n, cdiv(a->k * sizeof(T), 256) + cdiv(a->k_second * sizeof(T), 256));
     const int groups = (int)cdiv(a->n, p.nb * 32);
-    return with_stream(p, [&](auto nb, auto resident) {
+    return with_stream<kWide>(p, [&](auto nb, auto resident) {
       return launch("massive_linear", ms::k_linear_stream<T, nb(), resident()>, stream_blocks(p, a->rows, groups), ms::kStreamNT, p.lds,
                     stream, f, groups, p.lds_weights);
     });
@@ -486,12 +492,16 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
     f.split = k0;
     int rc;
     if (streams(a->rows, f.cols, sizeof(T) == 2 ? 20 : 21)) {
-      const StreamPlan p = stream_plan(a->rows, f.cols, cdiv(a->n * sizeof(T), 256));
-      const int groups = (int)cdiv(f.cols, p.nb * 32);
-      rc = with_stream(p, [&](auto nb, auto resident) {
-        return launch("massive_linear_backward", slope ? ms::k_linear_dx_stream<T, true, nb(), resident()> : ms::k_linear_dx_stream<T, false, nb(), resident()>,
-                      stream_blocks(p, a->rows, groups), ms::kStreamNT, p.lds, stream, f, groups, p.lds_weights);
-      });
+      auto stream_with = [&](auto with_slope) {
+        constexpr bool kWide = sizeof(T) == 2 && !with_slope();
+        const StreamPlan p = stream_plan<kWide>(a->rows, f.cols, cdiv(a->n * sizeof(T), 256));
+        const int groups = (int)cdiv(f.cols, p.nb * 32);
+        return with_stream<kWide>(p, [&](auto nb, auto resident) {
+          return launch("massive_linear_backward", ms::k_linear_dx_stream<T, with_slope(), nb(), resident()>, stream_blocks(p, a->rows, groups),
+                        ms::kStreamNT, p.lds, stream, f, groups, p.lds_weights);
+        });
+      };
+      rc = slope ? stream_with(std::true_type()) : stream_with(std::false_type());
     } else {
       const int tiles_n = (int)cdiv(f.cols, 32);
       const int64_t blocks = cdiv(a->rows, 32) * tiles_n;
