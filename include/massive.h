@@ -320,7 +320,7 @@ int massive_unpack_rows(const massive_row_format* fmt, const void* table, int64_
 typedef struct {
   const int32_t* indptr;  /* [n + 1] */
   const int32_t* indices; /* [edges] */
-  int64_t n, edges, rows;
+  int64_t n, edges, rows; /* each at most 2^30 */
 } massive_block;
 
 /* out[i] = mean of x[j] over row i's list, d columns; zeros for an empty list.

@@ -347,15 +347,16 @@ __global__ __launch_bounds__(kMeanNT) void k_block_mean_backward(const uint32_t*
     const uint32_t before = b > 0 ? keys[b - 1] : none, after = e < edges ? keys[e] : none;
     for (int c0 = lane * Q; c0 < d; c0 += T * Q) {
       const int c = last_cols<Q>(c0, d);
+      const bool streamed = whole_aligned<D, Q>(dx + c) && dx_stride * sizeof(D) % 16 == 0;
       uint32_t cur = none;
       bool left = false;  // the run came in from the span before
       float sum[Q] = {};
       auto close = [&](bool right) {
         if (cur >= (uint32_t)rows) return;
         if (!left && !right) {
-          store_cols<D, Q>(dx + (int64_t)cur * dx_stride + c, Q, sum);
+          store_whole<D, Q>(dx + (int64_t)cur * dx_stride + c, sum, streamed);
         } else {
-          store_cols<float, Q>(partial + (2 * s + (left ? 0 : 1)) * d + c, Q, sum);
+          store_whole<float, Q>(partial + (2 * s + (left ? 0 : 1)) * d + c, sum, false);
         }
       };
       for (int32_t at = b; at < e; at += kMeanAhead) {

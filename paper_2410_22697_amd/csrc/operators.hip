@@ -155,12 +155,12 @@ int unpack_rows(const massive_row_format* fmt, const void* table, int64_t table_
 }
 
 // --------------------------------------------------------------- block mean
-constexpr int64_t kMostIds = (int64_t(1) << 31) - 1;  // rows and edges are counted in int32
+constexpr int64_t kMostIds = int64_t(1) << 30;  // rows and edges are counted in int32, some of them a step ahead
 
 int check_block(const massive_block* b) {
   if (!b) REFUSE("the block is NULL");
   if (b->n < 0 || b->edges < 0 || b->rows < 0) REFUSE("n, edges and rows must not be negative");
-  if (b->n > kMostIds - 1 || b->edges > kMostIds - 1 || b->rows > kMostIds - 1) REFUSE("n, edges and rows must be below 2^31 - 1");
+  if (b->n > kMostIds || b->edges > kMostIds || b->rows > kMostIds) REFUSE("n, edges and rows must be at most 2^30");
   if (b->n > 0 && !b->indptr) REFUSE("indptr is NULL");
   if (b->edges > 0 && !b->indices) REFUSE("indices is NULL");
   if (!aligned(b->indptr, 4) || !aligned(b->indices, 4)) REFUSE("indptr or indices is not aligned");

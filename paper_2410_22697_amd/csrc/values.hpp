@@ -31,27 +31,37 @@ __device__ __forceinline__ void load_cols(const T* p, int valid, float* x, float
   }
 }
 
-// Stores columns [0, valid) of x, rounded to nearest even. Whole vectors go past
-// the caches' own lines: results are larger than the L2 wherever their time
-// counts, and rows that do not fill their lines would be read back for the rest
-// of them (854K rows of 100 floats unpacked: 160 us kept, 90 us streamed; of 256
-// bf16 73 and 58). Vectors that straddle lines (rows of odd strides) are better
-// put together in the cache: dx of 40K x 323 in bf16 103 us streamed, 90 kept.
+// Stores Q columns of x, rounded to nearest even: past the caches' own lines
+// where `streamed`. Results are larger than the L2 wherever their time counts,
+// and rows that do not fill their lines would be read back for the rest of them
+// (854K rows of 100 floats unpacked: 160 us kept, 90 us streamed; of 256 bf16
+// 73 and 58). Vectors that straddle lines (rows of odd strides) are better put
+// together in the cache: dx of 40K x 323 in bf16 103 us streamed, 90 kept.
+template <typename T, int Q>
+__device__ __forceinline__ void store_whole(T* p, const float* x, bool streamed) {
+  cols_t<T, Q> v;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) v[q] = (T)x[q];
+  if constexpr (sizeof(v) % 4 == 0) {
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(v) / 4)));
+    if (streamed) {
+      // (as words: two stores of one type would be made one, and lose their kind)
+      __builtin_nontemporal_store(__builtin_bit_cast(words, v), reinterpret_cast<words*>(p));
+      return;
+    }
+  }
+  *reinterpret_cast<cols_t<T, Q>*>(p) = v;
+}
+template <typename T, int Q>
+__device__ __forceinline__ bool whole_aligned(const T* p) {
+  return reinterpret_cast<uintptr_t>(p) % (Q * sizeof(T) < 16 ? Q * sizeof(T) : 16) == 0;
+}
+
+// Stores columns [0, valid) of x.
 template <typename T, int Q>
 __device__ __forceinline__ void store_cols(T* p, int valid, const float* x) {
   if (valid >= Q) {
-    cols_t<T, Q> v;
-#pragma unroll
-    for (int q = 0; q < Q; ++q) v[q] = (T)x[q];
-    if constexpr (sizeof(v) % 4 == 0) {
-      typedef uint32_t words __attribute__((ext_vector_type(sizeof(v) / 4)));
-      if (reinterpret_cast<uintptr_t>(p) % (sizeof(v) < 16 ? sizeof(v) : 16) == 0) {
-        // (as words: two stores of one type would be made one, and lose their kind)
-        __builtin_nontemporal_store(__builtin_bit_cast(words, v), reinterpret_cast<words*>(p));
-        return;
-      }
-    }
-    *reinterpret_cast<cols_t<T, Q>*>(p) = v;
+    store_whole<T, Q>(p, x, whole_aligned<T, Q>(p));
   } else {
 #pragma unroll
     for (int q = 0; q < Q; ++q)

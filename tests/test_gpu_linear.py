@@ -68,6 +68,50 @@ def test_forward_on_many_rows(dtype):
         check_forward(linear(a["x"], a["weight"], a["bias"], act="relu", residual=a["residual"], x2=a["x2"]), None, a, "relu", TYPES[dtype])
 
 
+# enough results for rows to be streamed: weights that stay in LDS and that pass through it, one to many groups of
+# outputs, segments that end inside a vector, a step or a chunk, inputs of a few columns, a last tile of one row
+STREAMED = [(70_001, 5, 0, 30), (70_001, 3, 2, 33), (33_000, 64, 64, 64), (9_001, 100, 28, 256), (9_001, 129, 67, 257), (8_193, 700, 130, 256),
+            (8_200, 1030, 0, 300), (33_025, 300, 300, 70), (2_300, 16, 0, 1000)]
+
+
+@pytest.mark.parametrize("size", STREAMED)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_forward_streamed(size, dtype):
+    rows, k, k2, n = size
+    for act, residual in (("gelu", False), ("relu", True)):
+        a = make(rows, k, k2, n, TYPES[dtype], bias=residual, residual=residual)
+        y, pre = linear(a["x"], a["weight"], a["bias"], act=act, residual=a["residual"], x2=a["x2"], save_pre=True)
+        check_forward(y, pre, a, act, TYPES[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_streamed_rows_of_any_stride(dtype):
+    """As below, where rows are streamed: NaN around the operands reaches no result, and a row's own stays in it."""
+    t = TYPES[dtype]
+    rows, k, k2, n = 9_003, 133, 21, 270
+
+    def inside(x, left, right):
+        big = torch.full((x.shape[0] + 2, x.shape[1] + left + right), float("nan"), dtype=t, device="cuda")
+        big[1:1 + x.shape[0], left:left + x.shape[1]] = x
+        return big[1:1 + x.shape[0], left:left + x.shape[1]]
+
+    a = make(rows, k, k2, n, t)
+    b = dict(a, x=inside(a["x"], 1, 2), x2=inside(a["x2"], 3, 0), weight=inside(a["weight"], 1, 1), residual=inside(a["residual"], 5, 2))
+    y, pre = linear(b["x"], b["weight"], b["bias"], act="silu", residual=b["residual"], x2=b["x2"], save_pre=True)
+    check_forward(y, pre, a, "silu", t)
+    dy = torch.randn(rows, n, device="cuda").to(t)
+    got = linear_backward(inside(dy, 3, 2), b["x"], b["weight"], "silu", inside(pre, 2, 1), b["x2"])
+    check_backward(got, dy, a, "silu", pre, t)
+    a["x"][77, 132] = float("nan")
+    a["x"][8_000, 0] = float("inf")
+    y2 = linear(a["x"], a["weight"], a["bias"], act="silu", residual=a["residual"], x2=a["x2"])
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[[77, 8_000]] = False
+    assert torch.equal(y2[keep], y[keep]) and torch.isnan(y2[77]).all()
+    want = torch.isnan((a["x"][8_000:8_001].float() @ a["weight"][:, :k].float().t()))[0]
+    assert not want.any() and not torch.isfinite(y2[8_000]).any()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_of_any_stride_and_what_lies_around_them(dtype):
     """Columns and rows around the operands hold NaN: none of it may reach a result."""
@@ -156,6 +200,24 @@ def test_backward_on_many_rows(dtype):
         check_backward(got, dy, a, act, pre, t)
         again = linear_backward(dy, a["x"], a["weight"], act, pre, a["x2"])
         assert all(u is None and v is None or torch.equal(u, v) for u, v in zip(got, again))
+
+
+@pytest.mark.parametrize("size", [(70_001, 30, 0, 5), (70_001, 33, 2, 3), (33_000, 64, 64, 64), (9_001, 128, 128, 256), (9_001, 257, 3, 129),
+                                  (8_193, 256, 0, 700), (8_200, 70, 300, 1030), (2_300, 1000, 0, 16), (5_000, 9, 250, 300)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_backward_streamed(size, dtype):
+    """dx's forms and dw's tiles: one and several of each, columns that both inputs share a vector or a tile over."""
+    rows, k, k2, n = size
+    t = TYPES[dtype]
+    for act in ("none", "gelu", "relu"):
+        a = make(rows, k, k2, n, t)
+        dy = torch.randn(rows, n, device="cuda").to(t)
+        pre = None if act == "none" else (2 * torch.randn(rows, n, device="cuda")).to(t)
+        check_backward(linear_backward(dy, a["x"], a["weight"], act, pre, a["x2"]), dy, a, act, pre, t)
+    if k2:
+        for ask in (dict(need_dx=False), dict(need_dx2=False)):
+            got = linear_backward(dy, a["x"], a["weight"], act, pre, a["x2"], need_dw=False, bias=False, **ask)
+            check_backward(got, dy, a, act, pre, t)
 
 
 def test_each_gradient_alone():

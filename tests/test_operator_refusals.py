@@ -63,8 +63,8 @@ def block(indptr=P, indices=P, n=4, edges=5000, rows=10):
     return operators._Block(indptr, indices, n, edges, rows)
 
 
-BLOCKS = [(dict(n=-1), "negative"), (dict(edges=-1), "negative"), (dict(rows=-1), "negative"), (dict(edges=1 << 31), "2^31"),
-          (dict(rows=(1 << 31) - 1), "2^31"), (dict(indptr=None), "indptr"), (dict(indices=None), "indices"), (dict(indptr=P + 2), "aligned")]
+BLOCKS = [(dict(n=-1), "negative"), (dict(edges=-1), "negative"), (dict(rows=-1), "negative"), (dict(edges=(1 << 30) + 1), "2^30"),
+          (dict(rows=(1 << 30) + 1), "2^30"), (dict(n=(1 << 30) + 1), "2^30"), (dict(indptr=None), "indptr"), (dict(indices=None), "indices"), (dict(indptr=P + 2), "aligned")]
 
 
 @pytest.mark.parametrize("bad,word", BLOCKS)
@@ -185,6 +185,42 @@ def test_adamw_states():
     refused(call(P, None, P, P, 1, P, P, None), "NULL")
     refused(call(P, P, P + 2, P, 1, P, P, None), "aligned")
     assert call(None, None, None, None, 0, None, None, None) == OK
+
+
+def test_struct_layouts_match_the_binding(tmp_path):
+    """Every field of the operators' structs, as a C99 compiler sees the header."""
+    import shutil
+    import subprocess
+    if shutil.which("gcc") is None:
+        pytest.skip("needs gcc")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    structs = {"massive_row_format": operators._Format, "massive_block": operators._Block, "massive_linear_args": operators._LinearArgs,
+               "massive_linear_grads": operators._LinearGrads, "massive_adamw_tensor": operators._AdamwTensor,
+               "massive_adamw_args": operators._AdamwArgs}
+    lines = ["#include <stddef.h>", "#include <stdio.h>", '#include "massive.h"', "int main(void) {"]
+    want = []
+    for name, s in structs.items():
+        for f, t in s._fields_:
+            lines.append('printf("%%zu %%zu\\n", offsetof(%s, %s), sizeof(((%s*)0)->%s));' % (name, f, name, f))
+            want.append((getattr(s, f).offset, ctypes.sizeof(t)))
+        lines.append('printf("%%zu 0\\n", sizeof(%s));' % name)
+        want.append((ctypes.sizeof(s), 0))
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text("\n".join(lines + ["return 0; }"]))
+    subprocess.check_call(["gcc", "-std=c99", "-pedantic", "-Wall", "-Wextra", "-Werror", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)])
+    out = subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout
+    assert [tuple(int(v) for v in line.split()) for line in out.splitlines()] == want
+    assert operators._ADAMW_ROW.itemsize == ctypes.sizeof(operators._AdamwTensor)
+    assert all(operators._ADAMW_ROW.fields[f][1] == getattr(operators._AdamwTensor, f).offset for f in operators._ADAMW_ROW.names)
+
+
+def test_constants_match_the_header():
+    import re
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "include", "massive.h")).read()
+    defs = dict(re.findall(r"#define (MASSIVE_\w+) (\d+)", text))
+    assert [int(defs["MASSIVE_" + n]) for n in ("F32", "BF16", "PACKED")] == [operators.F32, operators.BF16, operators.PACKED]
+    assert {k: int(defs["MASSIVE_ACT_" + k.upper()]) for k in operators.ACTIVATIONS} == operators.ACTIVATIONS
 
 
 def test_tensors_on_the_cpu_are_refused():
