@@ -211,23 +211,33 @@ __device__ __forceinline__ void linear_dx_store(const LinearDx<T>& a, int64_t ro
 }
 
 // -------------------------------------------------------------------- join
-// Adds the parts, of dw (rows of `cols` values) and of dbias.
+// Adds the parts, of dw (rows of `cols` values) and of dbias: four threads a
+// value, each over a quarter of the parts.
+constexpr int kJoinWays = 4;
 template <typename T>
 __global__ __launch_bounds__(kLinNT) void k_linear_join(const float* __restrict__ dw_parts, const float* __restrict__ bias_parts,
                                                         int64_t parts, int n, int cols, T* __restrict__ dw, int64_t dw_stride,
                                                         T* __restrict__ dbias) {
-  const int64_t all = (dw_parts ? (int64_t)n * cols : 0) + (bias_parts ? n : 0);
-  for (int64_t i = (int64_t)blockIdx.x * kLinNT + threadIdx.x; i < all; i += (int64_t)gridDim.x * kLinNT) {
-    const int64_t in_dw = dw_parts ? (int64_t)n * cols : 0;
-    const bool bias = i >= in_dw;
-    const float* p = bias ? bias_parts + (i - in_dw) : dw_parts + i;
-    const int64_t step = bias ? n : (int64_t)n * cols;
-    float t = 0.0f;
+  constexpr int kValues = kLinNT / kJoinWays;
+  __shared__ float sums[kJoinWays][kValues];
+  const int way = threadIdx.x / kValues;
+  const int64_t in_dw = dw_parts ? (int64_t)n * cols : 0, all = in_dw + (bias_parts ? n : 0);
+  const int64_t i = (int64_t)blockIdx.x * kValues + threadIdx.x % kValues;
+  const bool bias = i >= in_dw;
+  const float* p = bias ? bias_parts + (i - in_dw) : dw_parts + i;
+  const int64_t step = bias ? n : in_dw, per = (parts + kJoinWays - 1) / kJoinWays;
+  float t = 0.0f;
+  if (i < all) {
 #pragma unroll 8
-    for (int64_t q = 0; q < parts; ++q) t += p[q * step];
-    if (bias) dbias[i - in_dw] = (T)t;
-    else dw[i / cols * dw_stride + i % cols] = (T)t;
+    for (int64_t q = way * per; q < min(parts, (way + 1) * per); ++q) t += p[q * step];
   }
+  sums[way][threadIdx.x % kValues] = t;
+  __syncthreads();
+  if (way || i >= all) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWays; ++w) t += sums[w][threadIdx.x];
+  if (bias) dbias[i - in_dw] = (T)t;
+  else dw[i / cols * dw_stride + i % cols] = (T)t;
 }
 
 }  // namespace ms

@@ -113,21 +113,6 @@ __device__ __forceinline__ void stream_product(const StreamSegment<T> (&segs)[2]
   const int chunks = segs[0].chunks + segs[1].chunks;
   auto seg_of = [&](int c) -> const StreamSegment<T>& { return segs[c < segs[0].chunks ? 0 : 1]; };
   auto in_seg = [&](int c) { return c < segs[0].chunks ? c : c - segs[0].chunks; };
-  StreamWeights<T, ACROSS, NB> w;
-  constexpr int kChunkBytes = NB * kStreamBlockBytes;
-  if constexpr (RESIDENT) {
-    for (int c = 0; c < chunks; ++c) {
-      w.load(seg_of(c), in_seg(c), n0, n);
-      w.store(lds + c * kChunkBytes);
-    }
-    __syncthreads();
-  } else if (tile < tiles) {
-    w.load(seg_of(0), 0, n0, n);
-    w.store(lds);
-    __syncthreads();
-  }
-  if (tile >= tiles) return;
-
   u32x4 x[kStreamSteps], z[SLOPE ? kStreamSteps : 1];
   // one step of (tile, chunk) to its registers
   auto fetch = [&](int s, const StreamSegment<T>& g, int c, int64_t row) {
@@ -147,8 +132,24 @@ __device__ __forceinline__ void stream_product(const StreamSegment<T> (&segs)[2]
       z[s] = __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(g.x.pre + row * g.x.pre_stride + from));
   };
   auto row_of = [&](int64_t t) { return min(t * kStreamRows + wave * 32 + lane % 32, rows - 1); };
+  // the first rows are on their way while the weights are laid out
+  if (tile < tiles) {
 #pragma unroll
-  for (int s = 0; s < kStreamSteps; ++s) fetch(s, segs[0], 0, row_of(tile));
+    for (int s = 0; s < kStreamSteps; ++s) fetch(s, segs[0], 0, row_of(tile));
+  }
+  StreamWeights<T, ACROSS, NB> w;
+  constexpr int kChunkBytes = NB * kStreamBlockBytes;
+  if constexpr (RESIDENT) {
+    for (int c = 0; c < chunks; ++c) {
+      w.load(seg_of(c), in_seg(c), n0, n);
+      w.store(lds + c * kChunkBytes);
+    }
+    __syncthreads();
+  } else if (tile < tiles) {
+    w.load(seg_of(0), 0, n0, n);
+    w.store(lds);
+    __syncthreads();
+  }
 
   int buffer = 0;
   for (; tile < tiles; tile += tile_step) {
@@ -183,14 +184,19 @@ __device__ __forceinline__ void stream_product(const StreamSegment<T> (&segs)[2]
         for (int i = 0; i < kGroup; ++i) v[at % 2][i] = *reinterpret_cast<const u32x4*>(wl + (b0 + i) * kStreamBlockBytes + s * 1024);
       };
       weights(0);
+      // fp32 leaves out the steps behind a segment's end (100 + 100 -> 256: 158 to
+      // 141 us); in bf16 they cost less than asking
+      const int live = sizeof(T) == 2 ? kStreamSteps
+                                      : (int)min((int64_t)kStreamSteps, (g.x.K - (int64_t)cs * kStreamSteps * 2 * kV + 2 * kV - 1) / (2 * kV));
       u32x4 a;
 #pragma unroll
       for (int at = 0; at < kGroups; ++at) {
         const int s = at * kGroup / NB, b0 = at * kGroup % NB;
+        const bool counts = sizeof(T) == 2 || s < live;
         if (b0 == 0) {
           a = x[s];
-          if constexpr (SLOPE) {
-            cols_t<T, kV> d = __builtin_bit_cast(cols_t<T, kV>, a), p = __builtin_bit_cast(cols_t<T, kV>, z[s]);
+          if (SLOPE && counts) {
+            cols_t<T, kV> d = __builtin_bit_cast(cols_t<T, kV>, a), p = __builtin_bit_cast(cols_t<T, kV>, z[SLOPE ? s : 0]);
             act_grads<T, kV>(d, p, g.x.act);
             a = __builtin_bit_cast(u32x4, d);
           }
@@ -198,6 +204,7 @@ __device__ __forceinline__ void stream_product(const StreamSegment<T> (&segs)[2]
         }
         if (at + 1 < kGroups) weights(at + 1);
         __builtin_amdgcn_sched_barrier(0);  // loads stay ahead of the products that they run beside
+        if (!counts) continue;
 #pragma unroll
         for (int i = 0; i < kGroup; ++i) {
           f32x16& c16 = acc[b0 + i];

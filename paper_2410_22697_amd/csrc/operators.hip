@@ -438,9 +438,11 @@ int linear(const massive_linear_args* a, void* stream) {
 
 // dw's tiles, outputs by columns of both inputs (each input's in whole vectors),
 // and the parts into which its rows are split. The tile is the one that
-// multiplies the fewest zeros; of equal ones the tallest, which reads x the
-// fewest times. Enough parts for the chip, none of less than eight steps of rows
-// where there are more.
+// multiplies the fewest zeros; of equal ones the square one, which reads least.
+// (256 by 128 read x fewer times and left room for half the waves: the dw of
+// 110K x 1024 by 128 with gelu's slope 155 us with it, 130 with 128 by 128.)
+// Enough parts for the chip, none of less than four steps of rows where there
+// are more.
 struct DwPlan {
   int bn, bk, second;
   int64_t tiles_n, tiles_k, part, parts, dw_floats, bytes;
@@ -451,7 +453,7 @@ DwPlan dw_plan(const massive_linear_grads* a) {
   p.second = (int)round_up(a->k, vector);
   const int64_t cols = p.second + a->k_second;
   int64_t least = 0;
-  for (const auto& t : {std::pair<int, int>(256, 128), std::pair<int, int>(128, 128), std::pair<int, int>(64, 256)}) {
+  for (const auto& t : {std::pair<int, int>(128, 128), std::pair<int, int>(64, 256)}) {
     const int64_t area = round_up(a->n, t.first) * round_up(cols, t.second);
     if (!p.bn || area < least) {
       least = area;
@@ -461,8 +463,8 @@ DwPlan dw_plan(const massive_linear_grads* a) {
   }
   p.tiles_n = cdiv(a->n, p.bn);
   p.tiles_k = cdiv(cols, p.bk);
-  const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 8 * step));
-  p.part = round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, (p.bn == 256 ? 256 : 512) / (p.tiles_n * p.tiles_k)))), step);
+  const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 4 * step));
+  p.part = round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, 512 / (p.tiles_n * p.tiles_k)))), step);
   p.parts = cdiv(a->rows, p.part);
   p.dw_floats = a->dw ? p.parts * a->n * ((int64_t)a->k + a->k_second) : 0;
   p.bytes = 4 * (round_up(p.dw_floats, 4) + (a->dbias ? p.parts * a->n : 0));
@@ -527,18 +529,18 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
   f.tiles_n = (int)p.tiles_n;
   f.tiles_k = (int)p.tiles_k;
   const int64_t blocks = p.parts * p.tiles_n * p.tiles_k;
-  if (blocks > kMostBlocks / 2) REFUSE("too many rows and columns for one call");
+  const int64_t values = (int64_t)a->n * ((a->dw ? k[0] + k[1] : 0) + (a->dbias ? 1 : 0));
+  const int64_t join_blocks = cdiv(values, ms::kLinNT / ms::kJoinWays);
+  if (blocks > kMostBlocks / 2 || join_blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
   auto go = [&](auto bn, auto bk) {
     return launch("massive_linear_backward", slope ? ms::k_linear_dw<T, true, bn(), bk()> : ms::k_linear_dw<T, false, bn(), bk()>, blocks, ms::kDwNT, 0,
                   stream, f, blocks);
   };
   using std::integral_constant;
-  const int rc = p.bn == 256   ? go(integral_constant<int, 256>(), integral_constant<int, 128>())
-                 : p.bn == 128 ? go(integral_constant<int, 128>(), integral_constant<int, 128>())
-                               : go(integral_constant<int, 64>(), integral_constant<int, 256>());
+  const int rc = p.bn == 128 ? go(integral_constant<int, 128>(), integral_constant<int, 128>())
+                             : go(integral_constant<int, 64>(), integral_constant<int, 256>());
   if (rc) return rc;
-  const int64_t values = (int64_t)a->n * ((a->dw ? k[0] + k[1] : 0) + (a->dbias ? 1 : 0));
-  return launch("massive_linear_backward", ms::k_linear_join<T>, std::min<int64_t>(cdiv(values, ms::kLinNT), 4096), ms::kLinNT, 0,
+  return launch("massive_linear_backward", ms::k_linear_join<T>, join_blocks, ms::kLinNT, 0,
                 stream, (const float*)f.dw, (const float*)f.dbias, p.parts, a->n, (int)(k[0] + k[1]), (T*)a->dw, a->dw_stride,
                 (T*)a->dbias);
 }
@@ -692,7 +694,8 @@ int massive_linear_backward(const massive_linear_grads* a, void* workspace, int6
   if (a->rows == 0) {  // sums over no rows
     const int64_t values = (int64_t)a->n * ((a->dw ? k : 0) + (a->dbias ? 1 : 0));
     if (values == 0) return MASSIVE_OK;
-    const int64_t blocks = std::min<int64_t>(cdiv(values, ms::kLinNT), 4096);
+    const int64_t blocks = cdiv(values, ms::kLinNT / ms::kJoinWays);
+    if (blocks > kMostBlocks) REFUSE("too many columns for one call");
     // the pointers only say which of the two are asked for: with no parts nothing is read
     const float *dw = (const float*)a->dw, *db = (const float*)a->dbias;
     return a->type == MASSIVE_F32
