@@ -207,7 +207,7 @@ __device__ __forceinline__ void linear_dx_store(const LinearDx<T>& a, int64_t ro
     return;
   }
   const int s = col >= a.split ? 1 : 0;
-  store_cols<T, 8>(a.dx[s] + row * a.dx_stride[s] + col - (s ? a.split : 0), 8, v);
+  store_cols<T, 8, false>(a.dx[s] + row * a.dx_stride[s] + col - (s ? a.split : 0), 8, v);
 }
 
 // -------------------------------------------------------------------- join

@@ -300,7 +300,8 @@ __global__ __launch_bounds__(kStreamNT) void k_linear_stream(LinearForward<T> a,
               const f32x4 lo = *reinterpret_cast<const f32x4*>(bias + c0 - n0 + c), hi = *reinterpret_cast<const f32x4*>(bias + c0 - n0 + c + 4);
 #pragma unroll
               for (int q = 0; q < 8; ++q) z[q] += q < 4 ? lo[q % 4] : hi[q % 4];
-              if (a.pre) store_cols<T, 8>(a.pre + row * a.pre_stride + c0 + c, 8, z);
+              // (64 bytes of a row at a time: the cache puts its lines together)
+              if (a.pre) store_cols<T, 8, false>(a.pre + row * a.pre_stride + c0 + c, 8, z);
               act_values(z, a.act);
               if (a.residual) {
                 float t[8];
@@ -308,7 +309,7 @@ __global__ __launch_bounds__(kStreamNT) void k_linear_stream(LinearForward<T> a,
 #pragma unroll
                 for (int q = 0; q < 8; ++q) z[q] += t[q];
               }
-              store_cols<T, 8>(a.y + row * a.y_stride + c0 + c, 8, z);
+              store_cols<T, 8, false>(a.y + row * a.y_stride + c0 + c, 8, z);
             },
             [&](int r, int c, float z) {
               linear_finish(a, r0 + r, c0 + c, z + bias[c0 - n0 + c]);

@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kRowsNT) void k_pack_rows(const S* __restrict__ src
   }
 }
 
-// Q columns a lane: 16 bytes of output.
+// 16 bytes of output a lane.
 template <typename O, int BITS, int T>
 __global__ __launch_bounds__(kRowsNT) void k_unpack_rows(const uint8_t* __restrict__ table, int64_t rows,
                                                          const int32_t* __restrict__ index, int64_t n, O* __restrict__ out,

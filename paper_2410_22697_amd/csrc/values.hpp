@@ -58,10 +58,10 @@ __device__ __forceinline__ bool whole_aligned(const T* p) {
 }
 
 // Stores columns [0, valid) of x.
-template <typename T, int Q>
+template <typename T, int Q, bool STREAMED = true>
 __device__ __forceinline__ void store_cols(T* p, int valid, const float* x) {
   if (valid >= Q) {
-    store_whole<T, Q>(p, x, whole_aligned<T, Q>(p));
+    store_whole<T, Q>(p, x, STREAMED && whole_aligned<T, Q>(p));
   } else {
 #pragma unroll
     for (int q = 0; q < Q; ++q)
