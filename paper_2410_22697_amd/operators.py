@@ -5,9 +5,10 @@ block, a layer and the step on its weights.
 As in the rest of the binding, Python only checks and marshals arguments: every
 operator runs in the library's HIP kernels, on the current stream of the
 tensors' device, and returns without waiting. Outputs and workspaces come from
-torch's allocator. `linear` and `block_mean` take part in autograd; their
-gradients are also there as calls of their own. Wrong arguments raise
-ValueError here, or MassiveError where the library refuses them.
+torch's allocator. `linear` and `block_mean` take part in autograd (once: their
+gradients are not differentiated again), and their gradients are also there as
+calls of their own. Wrong arguments raise ValueError here, or MassiveError where
+the library refuses them.
 """
 import ctypes
 import operator
@@ -15,6 +16,7 @@ from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import massive
 from .massive import OK, MassiveError
@@ -243,6 +245,7 @@ class _BlockMean(torch.autograd.Function):
         return _block_mean(x, indptr, indices, None, dtype)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         indptr, indices = ctx.saved_tensors
         # summed in the gradient's type, and given in the input's
@@ -341,6 +344,7 @@ class _Linear(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, x2, pre = ctx.saved_tensors
         need = ctx.needs_input_grad
