@@ -193,21 +193,22 @@ __global__ __launch_bounds__(kSortWaves* MS_WAVE) void k_digits(const uint32_t* 
 
 // counts[chunk][digit] to the number of equal digits in the chunks before, and
 // totals[digit]. A block takes 16 digits (64 bytes of a chunk's counts), its 64
-// groups of 16 threads take the chunks in 64 runs.
-constexpr int kPlacesDigits = 16, kPlacesRuns = 64;
+// groups of 16 threads take the chunks in 64 runs, whose counts they keep in
+// registers until the places of the runs are known.
+constexpr int kPlacesDigits = 16, kPlacesRuns = 64, kPlacesRun = kChunksMost / kPlacesRuns;
 __global__ __launch_bounds__(kPlacesDigits* kPlacesRuns) void k_places(int32_t* __restrict__ counts, int chunks, int bits,
                                                                        int32_t* __restrict__ totals) {
   __shared__ int32_t part[kPlacesRuns][kPlacesDigits];
   const int g0 = threadIdx.x % kPlacesDigits, run = threadIdx.x / kPlacesDigits;
   const int digits = 1 << bits;
   const int g = blockIdx.x * kPlacesDigits + g0;
-  const int per = (chunks + kPlacesRuns - 1) / kPlacesRuns;
-  const int b = min(chunks, run * per), e = min(chunks, b + per);
-  int32_t sum = 0;
-  if (g < digits) {
-#pragma unroll 8
-    for (int w = b; w < e; ++w) sum += counts[(int64_t)w * digits + g];
-  }
+  const int per = (chunks + kPlacesRuns - 1) / kPlacesRuns;  // at most kPlacesRun
+  const int b = run * per;
+  int32_t v[kPlacesRun], sum = 0;
+#pragma unroll
+  for (int u = 0; u < kPlacesRun; ++u) v[u] = u < per && b + u < chunks && g < digits ? counts[(int64_t)(b + u) * digits + g] : 0;
+#pragma unroll
+  for (int u = 0; u < kPlacesRun; ++u) sum += v[u];
   part[run][g0] = sum;
   __syncthreads();
   if (run == 0) {
@@ -221,18 +222,11 @@ __global__ __launch_bounds__(kPlacesDigits* kPlacesRuns) void k_places(int32_t* 
     if (g < digits) totals[g] = before;
   }
   __syncthreads();
-  if (g >= digits) return;
   int32_t before = part[run][g0];
-  for (int w0 = b; w0 < e; w0 += 8) {
-    int32_t v[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = w0 + u < e ? counts[(int64_t)(w0 + u) * digits + g] : 0;
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (w0 + u < e) {
-        counts[(int64_t)(w0 + u) * digits + g] = before;
-        before += v[u];
-      }
+  for (int u = 0; u < kPlacesRun; ++u) {
+    if (u < per && b + u < chunks && g < digits) counts[(int64_t)(b + u) * digits + g] = before;
+    before += v[u];
   }
 }
 
@@ -407,7 +401,8 @@ __global__ __launch_bounds__(kMeanNT, ADD ? 3 : 4) void k_block_mean_backward(co
 }
 
 // The rows whose runs cross from span to span: the team of a run's first
-// crossing adds its partial sums in order.
+// crossing adds its partial sums in order, kJoinAhead of them on their way.
+constexpr int kJoinAhead = 8;
 template <typename D, int Q, int T>
 __global__ __launch_bounds__(kMeanNT) void k_block_mean_join(const uint32_t* __restrict__ keys, int32_t edges, int32_t rows, int d, int span,
                                                              const float* __restrict__ partial, D* __restrict__ dx,
@@ -424,23 +419,26 @@ __global__ __launch_bounds__(kMeanNT) void k_block_mean_join(const uint32_t* __r
       float sum[Q];
       load_cols<float, Q>(partial + (2 * (s - 1) + 1) * d + c, Q, sum);
       bool on = true;
-      for (int64_t t = s; on; t += kMeanAhead) {
-        float v[kMeanAhead][Q];
-        bool in[kMeanAhead];
+      for (int64_t t = s; on; t += kJoinAhead) {
+        float v[kJoinAhead][Q];
+        uint32_t at_end[kJoinAhead];
+        // (read whether they belong to the row or not: a sum's load need not wait for its key's)
 #pragma unroll
-        for (int u = 0; u < kMeanAhead; ++u) {
-          in[u] = t + u < spans && keys[(t + u) * span] == k;
-          // (whether it belongs to the row or not: its load need not wait for the key's)
-          if (t + u < spans) load_cols<float, Q>(partial + 2 * (t + u) * d + c, Q, v[u]);
+        for (int u = 0; u < kJoinAhead; ++u) {
+          const int64_t to = min(t + u, spans - 1);
+          at_end[u] = keys[to * span];
+          load_cols<float, Q>(partial + 2 * to * d + c, Q, v[u]);
         }
+        bool in[kJoinAhead];
 #pragma unroll
-        for (int u = 0; u < kMeanAhead; ++u) {
+        for (int u = 0; u < kJoinAhead; ++u) {
+          in[u] = t + u < spans && at_end[u] == k;
           if (in[u]) {
 #pragma unroll
             for (int q = 0; q < Q; ++q) sum[q] += v[u][q];
           }
         }
-        on = in[kMeanAhead - 1];
+        on = in[kJoinAhead - 1];
       }
       store_cols<D, Q>(dx + (int64_t)k * dx_stride + c, Q, sum);
     }
