@@ -60,7 +60,7 @@ __device__ __forceinline__ void few_product(const Operand<T> (&x)[SEGMENTS], con
       for (int u = 0; u < kFewAhead; ++u) {
         if constexpr (SLOPE) {
           cols_t<T, kV> d = __builtin_bit_cast(cols_t<T, kV>, a[u]);
-          act_grads<T, kV>(d, __builtin_bit_cast(cols_t<T, kV>, z[u]), o.act);
+          act_grads<T, kV>(d, __builtin_bit_cast(cols_t<T, kV>, z[u]), o.act, [](int, float) {});
           a[u] = __builtin_bit_cast(u32x4, d);
         }
         if constexpr (sizeof(T) == 2) {

@@ -197,7 +197,7 @@ __device__ __forceinline__ void stream_product(const StreamSegment<T> (&segs)[2]
           a = x[s];
           if (SLOPE && counts) {
             cols_t<T, kV> d = __builtin_bit_cast(cols_t<T, kV>, a), p = __builtin_bit_cast(cols_t<T, kV>, z[SLOPE ? s : 0]);
-            act_grads<T, kV>(d, p, g.x.act);
+            act_grads<T, kV>(d, p, g.x.act, [](int, float) {});
             a = __builtin_bit_cast(u32x4, d);
           }
           fetch(s, next, in_seg(next_c), next_row);

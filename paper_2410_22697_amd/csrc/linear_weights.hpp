@@ -130,8 +130,9 @@ __global__ __launch_bounds__(kDwNT) void k_linear_dw(LinearDw<T> a, int64_t bloc
     for (int i = 0; i < kPn; ++i) {
       const int id = threadIdx.x + i * kDwNT;
       cols_t<T, kV> g = __builtin_bit_cast(cols_t<T, kV>, dy[S][i]);
-      if constexpr (SLOPE) act_grads<T, kV>(g, __builtin_bit_cast(cols_t<T, kV>, z[S][i]), a.dz.act);
-      if (bias) {
+      if constexpr (SLOPE) {
+        act_grads<T, kV>(g, __builtin_bit_cast(cols_t<T, kV>, z[S][i]), a.dz.act, [&](int q, float v) { sums[q] += v; });
+      } else if (bias) {
 #pragma unroll
         for (int q = 0; q < kV; ++q) sums[q] += (float)g[q];
       }
