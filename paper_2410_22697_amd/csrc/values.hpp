@@ -34,9 +34,11 @@ __device__ __forceinline__ void load_cols(const T* p, int valid, float* x, float
 // Stores Q columns of x, rounded to nearest even: past the caches' own lines
 // where `streamed`. Results are larger than the L2 wherever their time counts,
 // and rows that do not fill their lines would be read back for the rest of them
-// (854K rows of 100 floats unpacked: 160 us kept, 90 us streamed; of 256 bf16
-// 73 and 58). Vectors that straddle lines (rows of odd strides) are better put
+// (854K rows of 100 floats in 4 bits read back: 169 us kept, 156 streamed; the
+// mean's gradient of 242K x 256 floats 186 and 180). Vectors that straddle lines (rows of odd strides) are better put
 // together in the cache: dx of 40K x 323 in bf16 103 us streamed, 90 kept.
+// So are the layer's, of which a wave has 64 bytes of a row at a time: 242K x
+// 256 in bf16 86 us streamed, 77 kept.
 template <typename T, int Q>
 __device__ __forceinline__ void store_whole(T* p, const float* x, bool streamed) {
   cols_t<T, Q> v;
