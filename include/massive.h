@@ -263,7 +263,8 @@ int massive_get_timing(massive_ctx* ctx, double* out_ms, int64_t* out_calls);
  * documented as updated in place. Arrays hold 32-bit or bf16 values
  * (MASSIVE_F32, MASSIVE_BF16) at their natural alignment; strides are in
  * elements. Sums, products' accumulators and statistics are fp32; a result is
- * rounded once, to nearest even, where it is stored. Results do not depend on
+ * rounded to nearest even where it is stored, and nothing before it is rounded
+ * to fewer bits, but for dz in massive_linear_grads. Results do not depend on
  * the order in which the device runs a call's blocks: the same call on the
  * same inputs gives the same bits. An empty extent (no rows, no tensors) is
  * MASSIVE_OK and does nothing. On failure the message is in
@@ -373,7 +374,11 @@ int massive_linear(const massive_linear_args* args, void* stream);
  * apart), dw = dz^T [x | x2], dbias = sum of dz over the rows. dx, dx_second,
  * dw and dbias may each be NULL; the residual's gradient is dy. pre is z as
  * massive_linear wrote it (for relu, y without a residual serves as well), and
- * NULL for MASSIVE_ACT_NONE. */
+ * NULL for MASSIVE_ACT_NONE. With MASSIVE_BF16, dz is rounded to bf16 before
+ * the products dx and dw, whose factors are bf16 (dz is one already for the
+ * identity and relu; for gelu and silu a gradient of normal values is 0.0023
+ * of its size off, where its own rounding leaves 0.0017). dbias sums it
+ * unrounded. */
 typedef struct {
   const void *dy, *pre, *x, *x_second, *w;
   void *dx, *dx_second, *dw, *dbias;

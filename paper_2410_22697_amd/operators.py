@@ -373,7 +373,9 @@ def linear_backward(dy, x, weight, act: str = "none", pre=None, x2=None, bias: b
     """(dx, dx2, dweight, dbias) of `linear`, None for those not asked for or
     not there. pre is what linear returned with save_pre (for relu without a
     residual, y serves as well), None for act "none". The residual's gradient
-    is dy."""
+    is dy. In bfloat16, dy times the activation's slope is rounded to bfloat16
+    before it is multiplied by the weights and by the inputs; dbias sums it
+    unrounded."""
     code = _activation(act)
     rows, n, k, k2, x_stride, x2_stride, w_stride = _layer(x, weight, x2)
     here = _on_gpu(dy, x, weight, x2, pre)
