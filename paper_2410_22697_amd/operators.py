@@ -7,8 +7,9 @@ operator runs in the library's HIP kernels, on the current stream of the
 tensors' device, and returns without waiting. Outputs and workspaces come from
 torch's allocator. `linear` and `block_mean` take part in autograd (once: their
 gradients are not differentiated again), and their gradients are also there as
-calls of their own. Wrong arguments raise ValueError here, or MassiveError where
-the library refuses them.
+calls of their own. What a call changes in place counts as changed there: a
+backward pass that would read it raises. Wrong arguments raise ValueError here,
+or MassiveError where the library refuses them.
 """
 import ctypes
 import operator
@@ -17,6 +18,7 @@ from typing import List, Optional, Sequence, Tuple
 import numpy as np
 import torch
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
 
 from . import massive
 from .massive import OK, MassiveError
@@ -190,6 +192,7 @@ def pack_rows(x, fmt: RowFormat, out=None, slots=None):
         raise ValueError("out has %d rows, and x %d" % (rows, n))
     _check(_load().massive_pack_rows(ctypes.byref(fmt.c), x.data_ptr(), _TYPES[x.dtype], stride, n,
                                      None if slots is None else slots.data_ptr(), out.data_ptr(), rows, _stream(here)))
+    increment_version(out)
     return out
 
 
@@ -204,9 +207,12 @@ def unpack_rows(table, fmt: RowFormat, index=None, dtype=torch.float32, out=None
         if dtype not in _TYPES:
             raise ValueError("dtype must be float32 or bfloat16, not %s" % dtype)
         out = torch.empty((n, fmt.d), dtype=dtype, device="cuda")
+    elif out.requires_grad and torch.is_grad_enabled():
+        raise ValueError("out requires a gradient, which rows read from a table have not")
     stride = _matrix(out, "out", cols=fmt.d, rows=n)
     _check(_load().massive_unpack_rows(ctypes.byref(fmt.c), table.data_ptr(), rows, None if index is None else index.data_ptr(), n,
                                        out.data_ptr(), _TYPES[out.dtype], stride, _stream(here)))
+    increment_version(out)
     return out
 
 
@@ -463,6 +469,12 @@ class AdamW:
         self._sizes = np.array([p.numel() for p in self.params], np.int64)
         self._table["param"] = _pointers(self.params)
         self._table["copy"] = [0 if c is None else c.data_ptr() for c in self.copies]
+        self._changed = self._written(range(len(self.params)))
+
+    def _written(self, at):
+        """The tensors that a step of the parameters `at` writes."""
+        states = [s for s in (self.m, self.v, self.m_scale, self.v_scale) if s is not None]
+        return [self.params[i] for i in at] + [self.copies[i] for i in at if self.copies[i] is not None] + states
 
     def _own_memory(self):
         """The parameters' and copies' memory may have been replaced since it was last seen."""
@@ -484,12 +496,13 @@ class AdamW:
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params):
             raise ValueError("%d parameters, and %d gradients" % (len(self.params), len(grads)))
-        there = slice(None)
+        there, changed = slice(None), self._changed
         if any(g is None for g in grads):
             there = np.array([i for i, g in enumerate(grads) if g is not None], np.int64)
             grads = [grads[i] for i in there]
             if not grads:
                 return
+            changed = self._written(there)
         here = _on_gpu(self.params[0])
         types = set(map(_dtype_of, grads))
         if len(types) != 1 or not types <= _TYPES.keys():
@@ -504,6 +517,7 @@ class AdamW:
         a = _AdamwArgs(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, self.t + 1, self.state_bits,
                        _TYPES[self.dtype], _TYPES[types.pop()], 0)
         _check(_load().massive_adamw(self._list, len(self._list), ctypes.byref(a), _stream(here)))
+        increment_version(changed)
         self.t += 1
 
     def states(self):
