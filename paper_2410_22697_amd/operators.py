@@ -5,9 +5,10 @@ block, a layer and the step on its weights.
 As in the rest of the binding, Python only checks and marshals arguments: every
 operator runs in the library's HIP kernels, on the current stream of the
 tensors' device, and returns without waiting. Outputs and workspaces come from
-torch's allocator. `linear` and `block_mean` take part in autograd (once: their
-gradients are not differentiated again), and their gradients are also there as
-calls of their own. What a call changes in place counts as changed there: a
+torch's allocator. `linear` and `block_mean` take part in autograd (once, in
+reverse: their gradients are not differentiated again, and tensors with
+forward-mode tangents are refused), and their gradients are also there as calls
+of their own. What a call changes in place counts as changed there: a
 backward pass that would read it raises. Wrong arguments raise ValueError here,
 or MassiveError where the library refuses them.
 """
@@ -17,6 +18,7 @@ from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 from torch.autograd.graph import increment_version
 
@@ -111,6 +113,12 @@ def _on_gpu(*tensors) -> int:
     if there is not None and there != here:
         raise ValueError("a tensor lies on cuda:%d, and cuda:%d is the current device" % (there, here))
     return here
+
+
+def _no_tangent(*tensors):
+    """Forward-mode derivatives are not there: a tensor that carries a tangent is refused, rather than the tangent lost."""
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise ValueError("operators have no forward-mode derivatives, and a tensor carries a tangent")
 
 
 def _matrix(t, name, cols=None, rows=None, dtype=None) -> int:
@@ -265,6 +273,7 @@ def block_mean(x, indptr, indices, fmt: Optional[RowFormat] = None, dtype=None):
     next frontier. x is float32 or bfloat16, or with fmt a table of packed
     rows. The result has x's type (float32 for packed rows) unless dtype says
     otherwise. An index outside x stands for a row of zeros."""
+    _no_tangent(x)
     if fmt is None and x.requires_grad and torch.is_grad_enabled():
         return _BlockMean.apply(x, indptr, indices, dtype)
     return _block_mean(x, indptr, indices, fmt, dtype)
@@ -274,6 +283,7 @@ def block_mean_backward(dout, indptr, indices, rows: int, add=None):
     """The gradient [rows, d] of block_mean's x, in dout's type: row j sums
     dout[i] / length(i) over the rows i that list j, in their order; plus
     add[j] for the first len(add) rows."""
+    _no_tangent(dout, add)
     stride = _matrix(dout, "dout")
     here = _on_gpu(dout, indptr, indices, add)
     b = _block(indptr, indices, rows)
@@ -366,6 +376,7 @@ def linear(x, weight, bias=None, act: str = "none", residual=None, x2=None, save
     x2 [rows, k2], weight [n, k + k2], bias [n], residual [rows, n]; all of one
     type, float32 or bfloat16, rows of any stride. With save_pre, returns the
     activation's argument too, for linear_backward."""
+    _no_tangent(x, weight, bias, residual, x2)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, residual, x2)):
         if save_pre:
             raise ValueError("save_pre is for calls outside autograd")
@@ -382,6 +393,7 @@ def linear_backward(dy, x, weight, act: str = "none", pre=None, x2=None, bias: b
     is dy. In bfloat16, dy times the activation's slope is rounded to bfloat16
     before it is multiplied by the weights and by the inputs; dbias sums it
     unrounded."""
+    _no_tangent(dy, x, weight, pre, x2)
     code = _activation(act)
     rows, n, k, k2, x_stride, x2_stride, w_stride = _layer(x, weight, x2)
     here = _on_gpu(dy, x, weight, x2, pre)
@@ -503,6 +515,7 @@ class AdamW:
             if not grads:
                 return
             changed = self._written(there)
+        _no_tangent(*self.params, *grads)
         here = _on_gpu(self.params[0])
         types = set(map(_dtype_of, grads))
         if len(types) != 1 or not types <= _TYPES.keys():
