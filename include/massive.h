@@ -426,8 +426,10 @@ typedef struct {
  *   p *= 1 - lr * weight_decay
  *   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
  *   p -= lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
- * with the new m and v in 32 bits, before they are held in 8. The array is
- * read during the call only. */
+ * with the new m and v in 32 bits, before they are held in 8, denormals among
+ * them. An eps between 0 and 2^-126 counts as 2^-126. With an eps of 0 a value
+ * whose new v is 0 is divided by 0: NaN where m is 0 too, infinite where 8-bit
+ * states have kept m and not v. The array is read during the call only. */
 int massive_adamw(const massive_adamw_tensor* tensors, int64_t count, const massive_adamw_args* args, void* stream);
 
 /* What 8-bit states stand for, as floats: n codes of m and of v with their

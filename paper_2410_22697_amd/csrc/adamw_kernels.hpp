@@ -63,6 +63,13 @@ __device__ __forceinline__ float value_v(uint32_t c, float scale) {
   return (s * s) * scale;
 }
 
+// sqrt(v) to a unit or two in its last place, also where v is a denormal, which
+// the hardware's root takes as 0.
+__device__ __forceinline__ float root_of_moment(float v) {
+  const bool small = v < 0x1p-96f;
+  return __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? 0x1p-32f : 1.0f);
+}
+
 // A block's scale from the bits of its largest magnitude, and the reciprocal
 // (0 where every code is 0): NaN if a value is not finite.
 __device__ __forceinline__ void state_scale(uint32_t mag, float top, float least, float& scale, float& inv) {
@@ -129,8 +136,9 @@ __global__ __launch_bounds__(kAdamwNT) void k_adamw(AdamwLaunch a) {
       m[q] = m[q] * a.b1 + g[q] * a.b1c;
       v[q] = v[q] * a.b2 + (g[q] * g[q]) * a.b2c;
       p[q] = p[q] * a.decay;
-      // (the quotient to a few units in its last place: it is small beside p)
-      p[q] = p[q] - (m[q] * a.lr) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[q]) * a.v_factor + a.eps);
+      // (the quotient to a few units in its last place: it is small beside p. Its
+      // divisor is 0, or a normal number)
+      p[q] = p[q] - (m[q] * a.lr) * __builtin_amdgcn_rcpf(root_of_moment(v[q]) * a.v_factor + a.eps);
       mag_m = max(mag_m, __float_as_uint(m[q]) & 0x7FFFFFFFu);
       mag_v = max(mag_v, __float_as_uint(v[q]) & 0x7FFFFFFFu);
     }

@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <limits>
 #include <tuple>
 #include <type_traits>
 #include <utility>
@@ -580,7 +581,9 @@ int adamw(const massive_adamw_tensor* tensors, int64_t count, const massive_adam
   l.b2c = (float)(1.0 - a->beta_second);
   l.lr = (float)(a->lr / (1.0 - std::pow(a->beta_first, (double)a->t)));
   l.v_factor = (float)(1.0 / std::sqrt(1.0 - std::pow(a->beta_second, (double)a->t)));
-  l.eps = (float)a->eps;
+  // the least normal number stands for all below it: the device divides by
+  // normal numbers, and beside the root of any v that fp32 holds neither counts
+  l.eps = a->eps > 0 ? std::max((float)a->eps, std::numeric_limits<float>::min()) : 0.0f;
   for (int64_t i = 0; i < count;) {
     l.count = 0;
     int64_t blocks = 0;
