@@ -425,9 +425,17 @@ def _pointers(tensors):
     return np.fromiter(map(torch.Tensor.data_ptr, tensors), np.uint64, len(tensors))
 
 
+def _disjoint(tensors):
+    """Refuses tensors (contiguous, or None) that share memory: a call's blocks would write it at the same time."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors if t is not None and t.numel())
+    for (_, end), (begin, _) in zip(spans, spans[1:]):
+        if begin < end:
+            raise ValueError("parameters or copies share memory")
+
+
 class AdamW:
-    """AdamW over a list of tensors, contiguous and of one type (float32 or
-    bfloat16), updated in place by `step`. state_bits 32 keeps the two moments
+    """AdamW over a list of tensors, contiguous, of one type (float32 or
+    bfloat16) and in memory of their own, updated in place by `step`. state_bits 32 keeps the two moments
     as float32, 8 as bytes with a float32 scale for each 256 values. copies: for
     each parameter a bfloat16 tensor of its shape that receives the new values,
     or None.
@@ -454,6 +462,7 @@ class AdamW:
                 raise ValueError("parameters must be contiguous and of one type")
             if c is not None and (c.dtype != torch.bfloat16 or c.shape != p.shape or not c.is_contiguous()):
                 raise ValueError("a copy must be a contiguous bfloat16 tensor of its parameter's shape")
+        _disjoint(self.params + self.copies)
         self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
         self.state_bits, self.t = state_bits, 0
         device = self.params[0].device
@@ -491,11 +500,14 @@ class AdamW:
     def _own_memory(self):
         """The parameters' and copies' memory may have been replaced since it was last seen."""
         now = _pointers(self.params)
-        for i in np.flatnonzero(now != self._table["param"]):
+        moved = np.flatnonzero(now != self._table["param"])
+        for i in moved:
             p = self.params[i]
             if p.dtype != self.dtype or p.numel() != self._sizes[i] or not p.is_contiguous():
                 raise ValueError("a parameter's memory was replaced by another type, size or layout")
             _on_gpu(p)
+        if len(moved):
+            _disjoint(self.params + self.copies)
         self._table["param"] = now
         for i, c in enumerate(self.copies):
             if c is not None and c.data_ptr() != self._table["copy"][i]:
