@@ -418,7 +418,7 @@ def linear_backward(dy, x, weight, act: str = "none", pre=None, x2=None, bias: b
 
 
 # ------------------------------------------------------------------------ AdamW
-_dtype_of = operator.attrgetter("dtype")
+_dtype_of, _shape_of = operator.attrgetter("dtype"), operator.attrgetter("shape")
 
 
 def _pointers(tensors):
@@ -488,6 +488,7 @@ class AdamW:
             self._table["m_scale"] = self.m_scale.data_ptr() + starts // 256 * 4
             self._table["v_scale"] = self.v_scale.data_ptr() + starts // 256 * 4
         self._sizes = np.array([p.numel() for p in self.params], np.int64)
+        self._shapes = list(map(_shape_of, self.params))
         self._table["param"] = _pointers(self.params)
         self._table["copy"] = [0 if c is None else c.data_ptr() for c in self.copies]
         self._changed = self._written(range(len(self.params)))
@@ -500,15 +501,15 @@ class AdamW:
     def _own_memory(self):
         """The parameters' and copies' memory may have been replaced since it was last seen."""
         now = _pointers(self.params)
-        moved = np.flatnonzero(now != self._table["param"])
-        for i in moved:
-            p = self.params[i]
-            if p.dtype != self.dtype or p.numel() != self._sizes[i] or not p.is_contiguous():
-                raise ValueError("a parameter's memory was replaced by another type, size or layout")
-            _on_gpu(p)
-        if len(moved):
+        moved = not np.array_equal(now, self._table["param"])
+        shapes = list(map(_shape_of, self.params))
+        if moved or shapes != self._shapes or not all(map(torch.Tensor.is_contiguous, self.params)):
+            for p, n in zip(self.params, self._sizes):
+                if p.dtype != self.dtype or p.numel() != n or not p.is_contiguous():
+                    raise ValueError("a parameter's memory was replaced by another type, size or layout")
+            _on_gpu(*self.params)
             _disjoint(self.params + self.copies)
-        self._table["param"] = now
+            self._table["param"], self._shapes = now, shapes
         for i, c in enumerate(self.copies):
             if c is not None and c.data_ptr() != self._table["copy"][i]:
                 raise ValueError("a copy's memory was replaced")
@@ -532,10 +533,11 @@ class AdamW:
         types = set(map(_dtype_of, grads))
         if len(types) != 1 or not types <= _TYPES.keys():
             raise ValueError("gradients must be of one type, float32 or bfloat16")
-        if set(map(torch.Tensor.get_device, grads)) != {here} or not all(map(torch.Tensor.is_contiguous, grads)) or \
-                not np.array_equal(np.fromiter(map(torch.Tensor.numel, grads), np.int64, len(grads)), self._sizes[there]):
-            raise ValueError("a gradient must be a contiguous tensor of its parameter's shape, on cuda:%d" % here)
         self._own_memory()
+        shapes = self._shapes if isinstance(there, slice) else [self._shapes[i] for i in there]
+        if set(map(torch.Tensor.get_device, grads)) != {here} or not all(map(torch.Tensor.is_contiguous, grads)) or \
+                list(map(_shape_of, grads)) != shapes:
+            raise ValueError("a gradient must be a contiguous tensor of its parameter's shape, on cuda:%d" % here)
         self._table["n"] = 0
         self._table["n"][there] = self._sizes[there]
         self._table["grad"][there] = _pointers(grads)
