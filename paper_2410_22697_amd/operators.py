@@ -262,8 +262,9 @@ class _BlockMean(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dout):
         indptr, indices = ctx.saved_tensors
-        # summed in the gradient's type, and given in the input's
-        return block_mean_backward(dout.contiguous(), indptr, indices, ctx.rows).to(ctx.dtype), None, None, None
+        # sums are fp32, and rounded to dout's type: a gradient of bfloat16 for an fp32 input is widened before them
+        wider = torch.promote_types(dout.dtype, ctx.dtype)
+        return block_mean_backward(dout.to(wider).contiguous(), indptr, indices, ctx.rows).to(ctx.dtype), None, None, None
 
 
 def block_mean(x, indptr, indices, fmt: Optional[RowFormat] = None, dtype=None):
