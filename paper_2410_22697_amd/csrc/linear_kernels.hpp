@@ -23,18 +23,24 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 enum { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
 
 // ------------------------------------------------------------- activations
-// Phi is Abramowitz and Stegun's 7.1.26: for s = |z|,
-//   1 - Phi(s) = (a1 t + .. + a5 t^5) exp(-s^2 / 2) / 2, t = 1 / (1 + p s / sqrt(2)),
-// which is off by 0.75e-7 at most and shares its exponential with the slope:
-// gelu's slope is ~20 instructions, where the compiler's erfcf and expf made a
-// wide layer's gradients in fp32 half as slow again as the matrix unit is.
-// Exponentials and reciprocals are the hardware's, one unit in the last place.
-constexpr float kErfP = 0.3275911f * 0.70710678f;
+// gelu by the tail q = 1 - Phi(s), s = |z|: z q below 0 and z - z q above, so
+// that small results are products and no differences.
+//   q = exp(-s^2 / 2) t P(t), t = 1 / (1 + 0.34 s),
+// P a polynomial of degree 6 with the least largest |error| / (q + 1e-5) for s
+// up to 14 (fitted in 64 bits): 7.7e-8. Exponentials and reciprocals are the
+// hardware's, one unit in the last place. Over 300K normal values in fp32 the
+// root of the mean squared error is 2.2e-8 for gelu and 3.7e-8 for its slope
+// (2.5e-8 and 2.6e-8 for the formulas with erf, each operation rounded to
+// fp32), and down to z = -6 both are 3e-6 of their size off. The slope shares
+// the exponential and is ~20 instructions, where the compiler's erfcf and expf
+// made a wide layer's gradients in fp32 half as slow again as the matrix unit
+// is.
+constexpr float kTailP = 0.34f;
 constexpr float kLog2e = 1.44269504f;
 
-// (a1 + a2 t + .. + a5 t^4) / 2
+// P(t)
 __device__ __forceinline__ float tail_poly(float t) {
-  return 0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f)));
+  return 0.13619301f + t * (0.128087512f + t * (0.163103034f + t * (-0.0440031517f + t * (0.278884839f + t * (-0.209133778f + t * 0.0468685945f)))));
 }
 // exp(-z^2 / 2) and 1 / (1 + exp(-z))
 __device__ __forceinline__ float bell(float z) { return __builtin_amdgcn_exp2f(z * (z * (-0.5f * kLog2e))); }
@@ -43,8 +49,9 @@ __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcp
 __device__ __forceinline__ float act_value(float z, int act) {
   if (act == kActRelu) return z <= 0.0f ? 0.0f : z;  // a NaN stays one
   if (act == kActGelu) {
-    const float t = __builtin_amdgcn_rcpf(1.0f + kErfP * fabsf(z));
-    return z * (0.5f + copysignf(0.5f - bell(z) * (t * tail_poly(t)), z));
+    const float t = __builtin_amdgcn_rcpf(1.0f + kTailP * fabsf(z));
+    const float q = bell(z) * (t * tail_poly(t));
+    return z < 0.0f ? z * q : z - fminf(z, 40.0f) * q;  // (infinity times a q of 0 would be a NaN)
   }
   return act == kActSilu ? z * logistic(z) : z;
 }
@@ -57,9 +64,9 @@ __device__ __forceinline__ float act_grad(float g, float z, int act) {
   if (act == kActGelu) {
     // Phi(z) + z phi(z) is r below 0 and 1 - r above, r = (1 - Phi(s)) - s phi(s)
     const float s = fminf(fabsf(z), 40.0f);
-    const float t = __builtin_amdgcn_rcpf(1.0f + kErfP * s);
-    const float half_less_r = 0.5f - bell(z) * (t * tail_poly(t) - 0.39894228f * s);
-    return g * (0.5f + copysignf(half_less_r, z));
+    const float t = __builtin_amdgcn_rcpf(1.0f + kTailP * s);
+    const float r = bell(z) * (t * tail_poly(t) - 0.39894228f * s);
+    return g * (z < 0.0f ? r : 1.0f - r);
   }
   const float s = fminf(fmaxf(z, -100.0f), 100.0f), q = logistic(z);
   return g * (q + q * (s - s * q));
