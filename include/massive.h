@@ -416,7 +416,8 @@ typedef struct {
 
 typedef struct {
   double lr, beta_first, beta_second, eps, weight_decay;
-  int64_t t;          /* the step's number, from 1 */
+  int64_t t;          /* the step's number, from 1: tensors that have taken
+                         different numbers of steps go in calls of their own */
   int32_t state_bits; /* 32 or 8 */
   int32_t param_type, grad_type;
   int32_t reserved;   /* 0 */

@@ -423,7 +423,7 @@ _dtype_of, _shape_of = operator.attrgetter("dtype"), operator.attrgetter("shape"
 
 
 def _pointers(tensors):
-    return np.fromiter(map(torch.Tensor.data_ptr, tensors), np.uint64, len(tensors))
+    return list(map(torch.Tensor.data_ptr, tensors))
 
 
 def _disjoint(tensors):
@@ -442,7 +442,8 @@ class AdamW:
     or None.
 
     The states of all tensors lie in flat arrays, each tensor's from a multiple
-    of 256 values on (`starts`)."""
+    of 256 values on (`starts`). Steps are counted for each tensor; `t` is the
+    largest count, and sets all of them where it is assigned."""
 
     def __init__(self, params: Sequence, lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, state_bits: int = 32, copies: Optional[Sequence] = None):
@@ -465,7 +466,7 @@ class AdamW:
                 raise ValueError("a copy must be a contiguous bfloat16 tensor of its parameter's shape")
         _disjoint(self.params + self.copies)
         self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
-        self.state_bits, self.t = state_bits, 0
+        self.state_bits, self._counts = state_bits, np.zeros(len(self.params), np.int64)
         device = self.params[0].device
         self.starts: List[int] = []
         total = 0
@@ -490,8 +491,9 @@ class AdamW:
             self._table["v_scale"] = self.v_scale.data_ptr() + starts // 256 * 4
         self._sizes = np.array([p.numel() for p in self.params], np.int64)
         self._shapes = list(map(_shape_of, self.params))
-        self._table["param"] = _pointers(self.params)
+        self._memory = self._table["param"] = _pointers(self.params)
         self._table["copy"] = [0 if c is None else c.data_ptr() for c in self.copies]
+        self._copy_memory = _pointers(c for c in self.copies if c is not None)
         self._changed = self._written(range(len(self.params)))
 
     def _written(self, at):
@@ -499,26 +501,41 @@ class AdamW:
         states = [s for s in (self.m, self.v, self.m_scale, self.v_scale) if s is not None]
         return [self.params[i] for i in at] + [self.copies[i] for i in at if self.copies[i] is not None] + states
 
+    @property
+    def t(self) -> int:
+        return int(self._counts.max())
+
+    @t.setter
+    def t(self, steps: int):
+        self._counts[:] = steps
+
     def _own_memory(self):
         """The parameters' and copies' memory may have been replaced since it was last seen."""
         now = _pointers(self.params)
-        moved = not np.array_equal(now, self._table["param"])
-        shapes = list(map(_shape_of, self.params))
-        if moved or shapes != self._shapes or not all(map(torch.Tensor.is_contiguous, self.params)):
+        if now != self._memory or not all(map(torch.Tensor.is_contiguous, self.params)):
             for p, n in zip(self.params, self._sizes):
                 if p.dtype != self.dtype or p.numel() != n or not p.is_contiguous():
                     raise ValueError("a parameter's memory was replaced by another type, size or layout")
             _on_gpu(*self.params)
             _disjoint(self.params + self.copies)
-            self._table["param"], self._shapes = now, shapes
-        for i, c in enumerate(self.copies):
-            if c is not None and c.data_ptr() != self._table["copy"][i]:
-                raise ValueError("a copy's memory was replaced")
+            self._memory = self._table["param"] = now
+        if _pointers(c for c in self.copies if c is not None) != self._copy_memory:
+            raise ValueError("a copy's memory was replaced")
+
+    def _shapes_of(self, there, grads):
+        """Whether the gradients have their parameters' shapes, and those the sizes that they began with."""
+        now = list(map(_shape_of, grads))
+        if now == (self._shapes if isinstance(there, slice) else [self._shapes[i] for i in there]):
+            return True
+        self._shapes = list(map(_shape_of, self.params))  # which a view of the same memory may have changed
+        return all(p.numel() == n for p, n in zip(self.params, self._sizes)) and \
+            now == [self._shapes[i] for i in np.arange(len(self.params))[there]]
 
     def step(self, grads: Optional[Sequence] = None):
         """One step. grads: a contiguous tensor of each parameter's shape, all
         of one type (float32 or bfloat16); by default the parameters' .grad.
-        A parameter whose gradient is None stays as it is."""
+        A parameter whose gradient is None stays as it is, its count of steps
+        too."""
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params):
             raise ValueError("%d parameters, and %d gradients" % (len(self.params), len(grads)))
@@ -529,24 +546,29 @@ class AdamW:
             if not grads:
                 return
             changed = self._written(there)
-        _no_tangent(*self.params, *grads)
+        if forward_ad._current_level >= 0:
+            _no_tangent(*self.params, *grads)
         here = _on_gpu(self.params[0])
         types = set(map(_dtype_of, grads))
         if len(types) != 1 or not types <= _TYPES.keys():
             raise ValueError("gradients must be of one type, float32 or bfloat16")
         self._own_memory()
-        shapes = self._shapes if isinstance(there, slice) else [self._shapes[i] for i in there]
         if set(map(torch.Tensor.get_device, grads)) != {here} or not all(map(torch.Tensor.is_contiguous, grads)) or \
-                list(map(_shape_of, grads)) != shapes:
+                not self._shapes_of(there, grads):
             raise ValueError("a gradient must be a contiguous tensor of its parameter's shape, on cuda:%d" % here)
-        self._table["n"] = 0
-        self._table["n"][there] = self._sizes[there]
-        self._table["grad"][there] = _pointers(grads)
-        a = _AdamwArgs(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, self.t + 1, self.state_bits,
-                       _TYPES[self.dtype], _TYPES[types.pop()], 0)
-        _check(_load().massive_adamw(self._list, len(self._list), ctypes.byref(a), _stream(here)))
+        self._table["grad"][there] = np.fromiter(map(torch.Tensor.data_ptr, grads), np.uint64, len(grads))
+        grad_type, stream = _TYPES[types.pop()], _stream(here)
+        counts = self._counts[there] + 1
+        groups = set(counts.tolist())  # one, unless some tensors went without a gradient before
+        for t in groups:
+            at = there if len(groups) == 1 else np.arange(len(self.params))[there][counts == t]
+            self._table["n"] = 0
+            self._table["n"][at] = self._sizes[at]
+            a = _AdamwArgs(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, t, self.state_bits,
+                           _TYPES[self.dtype], grad_type, 0)
+            _check(_load().massive_adamw(self._list, len(self._list), ctypes.byref(a), stream))
+            self._counts[at] = t
         increment_version(changed)
-        self.t += 1
 
     def states(self):
         """(m, v), flat float32 arrays of what the states stand for (`starts`
