@@ -449,6 +449,7 @@ int linear(const massive_linear_args* a, void* stream) {
 struct DwPlan {
   int bn, bk, second;
   int64_t tiles_n, tiles_k, part, parts, dw_floats, bytes;
+  int64_t blocks, join_blocks;
 };
 DwPlan dw_plan(const massive_linear_grads* a) {
   DwPlan p = {};
@@ -471,6 +472,9 @@ DwPlan dw_plan(const massive_linear_grads* a) {
   p.parts = cdiv(a->rows, p.part);
   p.dw_floats = a->dw ? p.parts * a->n * ((int64_t)a->k + a->k_second) : 0;
   p.bytes = 4 * (round_up(p.dw_floats, 4) + (a->dbias ? p.parts * a->n : 0));
+  p.blocks = p.parts * p.tiles_n * p.tiles_k;
+  const int64_t values = (int64_t)a->n * ((a->dw ? (int64_t)a->k + a->k_second : 0) + (a->dbias ? 1 : 0));
+  p.join_blocks = cdiv(values, ms::kLinNT / ms::kJoinWays);
   return p;
 }
 
@@ -531,19 +535,15 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
   f.second = p.second;
   f.tiles_n = (int)p.tiles_n;
   f.tiles_k = (int)p.tiles_k;
-  const int64_t blocks = p.parts * p.tiles_n * p.tiles_k;
-  const int64_t values = (int64_t)a->n * ((a->dw ? k[0] + k[1] : 0) + (a->dbias ? 1 : 0));
-  const int64_t join_blocks = cdiv(values, ms::kLinNT / ms::kJoinWays);
-  if (blocks > kMostBlocks / 2 || join_blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
   auto go = [&](auto bn, auto bk) {
-    return launch("massive_linear_backward", slope ? ms::k_linear_dw<T, true, bn(), bk()> : ms::k_linear_dw<T, false, bn(), bk()>, blocks, ms::kDwNT, 0,
-                  stream, f, blocks);
+    return launch("massive_linear_backward", slope ? ms::k_linear_dw<T, true, bn(), bk()> : ms::k_linear_dw<T, false, bn(), bk()>, p.blocks, ms::kDwNT, 0,
+                  stream, f, p.blocks);
   };
   using std::integral_constant;
   const int rc = p.bn == 128 ? go(integral_constant<int, 128>(), integral_constant<int, 128>())
                              : go(integral_constant<int, 64>(), integral_constant<int, 256>());
   if (rc) return rc;
-  return launch("massive_linear_backward", ms::k_linear_join<T>, join_blocks, ms::kLinNT, 0,
+  return launch("massive_linear_backward", ms::k_linear_join<T>, p.join_blocks, ms::kLinNT, 0,
                 stream, (const float*)f.dw, (const float*)f.dbias, p.parts, a->n, (int)(k[0] + k[1]), (T*)a->dw, a->dw_stride,
                 (T*)a->dbias);
 }
@@ -710,10 +710,11 @@ int massive_linear_backward(const massive_linear_grads* a, void* workspace, int6
                         a->n, (int)k, (bf16*)a->dw, a->dw_stride, (bf16*)a->dbias);
   }
   if (a->dw || a->dbias) {
-    const int64_t need = dw_plan(a).bytes;
-    if (!workspace || workspace_bytes < need)
+    const DwPlan p = dw_plan(a);
+    if (p.blocks > kMostBlocks / 2 || p.join_blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
+    if (!workspace || workspace_bytes < p.bytes)
       return call_error(MASSIVE_ECAPACITY, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0),
-                        (long long)need);
+                        (long long)p.bytes);
     if (!aligned(workspace, 16)) REFUSE("workspace is not 16-byte aligned");
   }
   return a->type == MASSIVE_F32 ? linear_backward<float>(a, workspace, stream) : linear_backward<bf16>(a, workspace, stream);
