@@ -181,7 +181,7 @@ __device__ __forceinline__ void stream_product(const StreamSegment<T> (&segs)[2]
       }
       // the weights of a few blocks of outputs at a time, the reads of the next
       // under way meanwhile
-      constexpr int kGroup = NB < 4 ? NB : SLOPE && NB == 8 ? 2 : 4, kGroups = kStreamSteps * NB / kGroup;
+      constexpr int kGroup = NB < 4 ? NB : 4, kGroups = kStreamSteps * NB / kGroup;
       u32x4 v[2][kGroup];
       auto weights = [&](int at) {
         const int s = at * kGroup / NB, b0 = at * kGroup % NB;

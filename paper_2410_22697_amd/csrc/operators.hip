@@ -434,8 +434,7 @@ int linear(const massive_linear_args* a, void* stream) {
     });
   }
   const int tiles_n = (int)cdiv(a->n, 32);
-  const int64_t blocks = cdiv(a->rows, 32) * tiles_n;
-  if (blocks > kMostBlocks / 2) REFUSE("too many outputs for so many rows");
+  const int64_t blocks = cdiv(a->rows, 32) * tiles_n;  // under 2^16: more are streamed
   return launch("massive_linear", ms::k_linear_few<T>, blocks, ms::kFewNT, 0, stream, f, tiles_n);
 }
 
@@ -513,8 +512,7 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
       rc = slope ? stream_with(std::true_type()) : stream_with(std::false_type());
     } else {
       const int tiles_n = (int)cdiv(f.cols, 32);
-      const int64_t blocks = cdiv(a->rows, 32) * tiles_n;
-      if (blocks > kMostBlocks / 2) REFUSE("too many columns for so many rows");
+      const int64_t blocks = cdiv(a->rows, 32) * tiles_n;  // under 2^16: more are streamed
       rc = launch("massive_linear_backward", slope ? ms::k_linear_dx_few<T, true> : ms::k_linear_dx_few<T, false>, blocks, ms::kFewNT, 0, stream, f, tiles_n);
     }
     if (rc) return rc;
