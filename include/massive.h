@@ -372,13 +372,13 @@ int massive_linear(const massive_linear_args* args, void* stream);
 
 /* The layer's gradients: dz = dy * act'(pre), dx = dz w (columns of x and x2
  * apart), dw = dz^T [x | x2], dbias = sum of dz over the rows. dx, dx_second,
- * dw and dbias may each be NULL; the residual's gradient is dy. pre is z as
- * massive_linear wrote it (for relu, y without a residual serves as well), and
- * NULL for MASSIVE_ACT_NONE. With MASSIVE_BF16, dz is rounded to bf16 before
- * the products dx and dw, whose factors are bf16 (dz is one already for the
- * identity and relu; for gelu and silu a gradient of normal values is 0.0023
- * of its size off, where its own rounding leaves 0.0017). dbias sums it
- * unrounded. */
+ * dw and dbias may each be NULL; the residual's gradient is dy. w is read for
+ * dx and dx_second, x and x_second for dw. pre is z as massive_linear wrote it
+ * (for relu, y without a residual serves as well), and NULL for
+ * MASSIVE_ACT_NONE. With MASSIVE_BF16, dz is rounded to bf16 before the
+ * products dx and dw, whose factors are bf16 (dz is one already for the identity
+ * and relu; for gelu and silu a gradient of normal values is 0.0023 of its size
+ * off, where its own rounding leaves 0.0017). dbias sums it unrounded. */
 typedef struct {
   const void *dy, *pre, *x, *x_second, *w;
   void *dx, *dx_second, *dw, *dbias;

@@ -81,13 +81,15 @@ __device__ __forceinline__ u32x4 dw_fragment(const char* lds, int c0, int k) {
   }
 }
 
-template <typename T, bool SLOPE, int TN, int TK>
+// DW: dw, and dbias if it is asked for; else dbias alone, by one block for each
+// TN outputs and part, which reads no x.
+template <typename T, bool SLOPE, int TN, int TK, bool DW>
 __global__ __launch_bounds__(kDwNT) void k_linear_dw(LinearDw<T> a, int64_t blocks) {
   constexpr int kV = 16 / sizeof(T), kRows = 64 / sizeof(T);  // rows of a step
   constexpr int kVn = TN / kV, kVk = TK / kV;                 // vectors of a row
   constexpr int kPn = (kRows * kVn + kDwNT - 1) / kDwNT, kPk = (kRows * kVk + kDwNT - 1) / kDwNT;
   constexpr int kWn = TN / 64, kWk = 8 / kWn, kI = 2, kJ = TK / kWk / 32;  // waves, and 32x32 squares of a wave
-  constexpr int kTileN = kRows * dw_pitch<T, TN>(), kTileK = kRows * dw_pitch<T, TK>();
+  constexpr int kTileN = kRows * dw_pitch<T, TN>(), kTileK = DW ? kRows * dw_pitch<T, TK>() : 0;
   __shared__ __align__(16) char lds[2 * (kTileN + kTileK)];
   const int64_t tile = tile_of_block(blockIdx.x, blocks);
   const int64_t part = tile / (a.tiles_k * a.tiles_n);
@@ -116,6 +118,7 @@ __global__ __launch_bounds__(kDwNT) void k_linear_dw(LinearDw<T> a, int64_t bloc
         if constexpr (SLOPE) z[S][i] = dw_load(a.dz.pre + r * a.dz.pre_stride, c, a.n);
       }
     }
+    if constexpr (!DW) return;
 #pragma unroll
     for (int i = 0; i < kPk; ++i) {
       const int id = threadIdx.x + i * kDwNT;
@@ -140,8 +143,9 @@ __global__ __launch_bounds__(kDwNT) void k_linear_dw(LinearDw<T> a, int64_t bloc
 #pragma unroll
         for (int q = 0; q < kV; ++q) sums[q] += (float)g[q];
       }
-      if (id < kRows * kVn) *reinterpret_cast<u32x4*>(to + id / kVn * dw_pitch<T, TN>() + id % kVn * 16) = __builtin_bit_cast(u32x4, g);
+      if (DW && id < kRows * kVn) *reinterpret_cast<u32x4*>(to + id / kVn * dw_pitch<T, TN>() + id % kVn * 16) = __builtin_bit_cast(u32x4, g);
     }
+    if constexpr (!DW) return;
 #pragma unroll
     for (int i = 0; i < kPk; ++i) {
       const int id = threadIdx.x + i * kDwNT;
@@ -150,6 +154,7 @@ __global__ __launch_bounds__(kDwNT) void k_linear_dw(LinearDw<T> a, int64_t bloc
   };
   f32x16 acc[kI][kJ] = {};
   auto multiply = [&](auto set) {
+    if constexpr (!DW) return;
     const char* from = lds + set() * (kTileN + kTileK);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -205,7 +210,7 @@ __global__ __launch_bounds__(kDwNT) void k_linear_dw(LinearDw<T> a, int64_t bloc
       a.dbias[part * a.n + col] = t;
     }
   }
-  if (!a.dw) return;
+  if constexpr (!DW) return;
   const int all = a.k[0] + a.k[1];
   float* dw = a.dw + part * a.n * (int64_t)all;
 #pragma unroll

@@ -444,7 +444,7 @@ int linear(const massive_linear_args* a, void* stream) {
 // (256 by 128 read x fewer times and left room for half the waves: the dw of
 // 110K x 1024 by 128 with gelu's slope 165 us with it, 145 with 128 by 128.)
 // Enough parts for the chip, none of less than four steps of rows where there
-// are more.
+// are more. dbias alone is tiles of 128 outputs, without columns.
 struct DwPlan {
   int bn, bk, second;
   int64_t tiles_n, tiles_k, part, parts, dw_floats, bytes;
@@ -466,6 +466,11 @@ DwPlan dw_plan(const massive_linear_grads* a) {
   }
   p.tiles_n = cdiv(a->n, p.bn);
   p.tiles_k = cdiv(cols, p.bk);
+  if (!a->dw) {
+    p.bn = p.bk = 128;
+    p.tiles_n = cdiv(a->n, p.bn);
+    p.tiles_k = 1;
+  }
   const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 4 * step));
   p.part = round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, 512 / (p.tiles_n * p.tiles_k)))), step);
   p.parts = cdiv(a->rows, p.part);
@@ -533,13 +538,14 @@ int linear_backward(const massive_linear_grads* a, void* workspace, void* stream
   f.second = p.second;
   f.tiles_n = (int)p.tiles_n;
   f.tiles_k = (int)p.tiles_k;
-  auto go = [&](auto bn, auto bk) {
-    return launch("massive_linear_backward", slope ? ms::k_linear_dw<T, true, bn(), bk()> : ms::k_linear_dw<T, false, bn(), bk()>, p.blocks, ms::kDwNT, 0,
-                  stream, f, p.blocks);
+  auto go = [&](auto bn, auto bk, auto dw) {
+    return launch("massive_linear_backward", slope ? ms::k_linear_dw<T, true, bn(), bk(), dw()> : ms::k_linear_dw<T, false, bn(), bk(), dw()>, p.blocks,
+                  ms::kDwNT, 0, stream, f, p.blocks);
   };
   using std::integral_constant;
-  const int rc = p.bn == 128 ? go(integral_constant<int, 128>(), integral_constant<int, 128>())
-                             : go(integral_constant<int, 64>(), integral_constant<int, 256>());
+  const int rc = !a->dw        ? go(integral_constant<int, 128>(), integral_constant<int, 128>(), std::false_type())
+                 : p.bn == 128 ? go(integral_constant<int, 128>(), integral_constant<int, 128>(), std::true_type())
+                               : go(integral_constant<int, 64>(), integral_constant<int, 256>(), std::true_type());
   if (rc) return rc;
   return launch("massive_linear_backward", ms::k_linear_join<T>, p.join_blocks, ms::kLinNT, 0,
                 stream, (const float*)f.dw, (const float*)f.dbias, p.parts, a->n, (int)(k[0] + k[1]), (T*)a->dw, a->dw_stride,
@@ -684,7 +690,7 @@ int massive_linear_backward(const massive_linear_grads* a, void* workspace, int6
   if (a->rows > 0) {
     if (!a->dy || (a->act != MASSIVE_ACT_NONE && !a->pre)) REFUSE("dy / pre are NULL");
     if ((a->dx || a->dx_second) && !a->w) REFUSE("w is NULL");
-    if ((a->dw || a->dbias) && !a->x) REFUSE("x is NULL");
+    if (a->dw && !a->x) REFUSE("x is NULL");
     if (a->dy_stride < a->n || (a->act != MASSIVE_ACT_NONE && a->pre_stride < a->n) || (a->x && a->x_stride < a->k) ||
         (a->x_second && a->x_second_stride < a->k_second) || (a->w && a->w_stride < k) || (a->dx && a->dx_stride < a->k) ||
         (a->dx_second && a->dx_second_stride < a->k_second))
