@@ -258,7 +258,8 @@ int massive_get_timing(massive_ctx* ctx, double* out_ms, int64_t* out_calls);
  * They take no context. Every call checks its arguments on the host, enqueues
  * its kernels on `stream` and returns without waiting; it allocates nothing
  * and keeps nothing. Pointers are device memory of the current device unless
- * said otherwise, and a table of packed rows may also be pinned host memory.
+ * said otherwise, and a table of packed rows that is read may also be pinned
+ * host memory, to be kept as it is until the stream has passed the call.
  * What a call reads and writes must not overlap, except where an argument is
  * documented as updated in place. Arrays hold 32-bit or bf16 values
  * (MASSIVE_F32, MASSIVE_BF16) at their natural alignment; strides are in

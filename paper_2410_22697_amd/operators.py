@@ -179,6 +179,14 @@ def _table(t, fmt, name="table", pinned=False) -> int:
     return t.shape[0]
 
 
+def _read_later(table):
+    """The current stream reads a pinned table after the call has returned: a copy of its first byte, which torch's
+    allocator of pinned memory waits for before it hands the memory out again. (A captured graph's tables are the
+    program's to keep, as all that it reads.)"""
+    if not table.is_cuda and table.numel() and not torch.cuda.is_current_stream_capturing():
+        table.view(-1)[:1].to("cuda", non_blocking=True)
+
+
 def pack_rows(x, fmt: RowFormat, out=None, slots=None):
     """Writes x's rows (float32 or bfloat16, [n, d]) in fmt to rows slots[i]
     (int32, distinct; one outside the table is left out) of the uint8 table
@@ -207,7 +215,8 @@ def pack_rows(x, fmt: RowFormat, out=None, slots=None):
 def unpack_rows(table, fmt: RowFormat, index=None, dtype=torch.float32, out=None):
     """Reads rows index[i] (int32; one outside the table reads as zeros), or
     every row without an index, of a table on the GPU or in pinned memory, to
-    a new tensor of dtype, or to `out`."""
+    a new tensor of dtype, or to `out`. A pinned table is read when the stream
+    comes to it: until then it may be dropped, but not written to."""
     rows = _table(table, fmt, pinned=True)
     here = _on_gpu(index, out)
     n = rows if index is None else _ids(index, "index")
@@ -220,6 +229,7 @@ def unpack_rows(table, fmt: RowFormat, index=None, dtype=torch.float32, out=None
     stride = _matrix(out, "out", cols=fmt.d, rows=n)
     _check(_load().massive_unpack_rows(ctypes.byref(fmt.c), table.data_ptr(), rows, None if index is None else index.data_ptr(), n,
                                        out.data_ptr(), _TYPES[out.dtype], stride, _stream(here)))
+    _read_later(table)
     increment_version(out)
     return out
 
@@ -248,6 +258,7 @@ def _block_mean(x, indptr, indices, fmt, dtype):
     out = torch.empty((b.n, d), dtype=dtype, device="cuda")
     _check(_load().massive_block_mean(ctypes.byref(b), x.data_ptr(), kind, stride, c, d, out.data_ptr(), _TYPES[dtype], d,
                                       _stream(here)))
+    _read_later(x)
     return out
 
 
@@ -272,8 +283,9 @@ def block_mean(x, indptr, indices, fmt: Optional[RowFormat] = None, dtype=None):
     an empty list. indptr (n + 1) and indices are int32, such as hop k's of a
     batch: `bb.indptr[k][:n + 1]`, `bb.indices[k][:e]`, with x the rows of the
     next frontier. x is float32 or bfloat16, or with fmt a table of packed
-    rows. The result has x's type (float32 for packed rows) unless dtype says
-    otherwise. An index outside x stands for a row of zeros."""
+    rows, pinned ones as in unpack_rows. The result has x's type (float32 for
+    packed rows) unless dtype says otherwise. An index outside x stands for a
+    row of zeros."""
     _no_tangent(x)
     if fmt is None and x.requires_grad and torch.is_grad_enabled():
         return _BlockMean.apply(x, indptr, indices, dtype)
