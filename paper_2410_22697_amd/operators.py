@@ -547,7 +547,9 @@ class AdamW:
         """One step. grads: a contiguous tensor of each parameter's shape, all
         of one type (float32 or bfloat16); by default the parameters' .grad.
         A parameter whose gradient is None stays as it is, its count of steps
-        too."""
+        too. A step captured into a graph keeps its lr and its counts: replays
+        neither count nor correct the moments for the steps between, so while
+        1 - beta^t is not 1 yet a step belongs outside the graph."""
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params):
             raise ValueError("%d parameters, and %d gradients" % (len(self.params), len(grads)))
