@@ -452,10 +452,12 @@ __global__ __launch_bounds__(kMeanNT) void k_block_mean_join(const uint32_t* __r
 
 // The gradient of a block of few edges, in one launch: a wave per source row
 // reads all indices and lists, in LDS and in order, the rows that list its
-// source; the block has found each edge's row before. It is bound by its latency:
-// with 128 floats, 300 edges 9.1 us a call, 2000 edges 9.9, where the sort's
-// launches take 20 and 26. A source reads all indices, so larger blocks go to
-// the sort.
+// source; the block has found each edge's row before. It is bound by its latency,
+// of which a source that many rows list has most: with 128 floats, 300 edges
+// 8.8 us a call, 2000 edges over 500, 2000 and 8192 sources 19, 13 and 16, where
+// the sort's launches take 20, and 20, 26 and 30. A source reads all indices, so
+// more edges or sources go to the sort (2000 edges over 16K sources 26 and 30
+// us, over 32K 44 and 30).
 constexpr int kFewEdges = 2048, kFewRows = 2048;  // of the block
 constexpr int kFewSources = 8192;
 

@@ -227,7 +227,10 @@ MeanPlan mean_plan(const massive_block* b, int64_t d) {
   p.chunk = std::max<int64_t>(MS_WAVE, round_up(cdiv(b->edges, ms::kChunksMost), MS_WAVE));
   p.chunks = (int)cdiv(b->edges, p.chunk);
   // shorter spans fill the chip, longer ones leave fewer sums to join. 128 floats,
-  // us with 16 / 32 / 64: 10K edges 31 / 34 / 43, 240K 67 / 61 / 67, 800K 156 / 148 / 152
+  // sources listed in proportion to their degrees, us of a call with 16 / 32 / 64:
+  // 24K edges 37 / 40 / 48, 90K 50 / 51 / 57, 200K 71 / 66 / 69, 300K 93 / 92 / 83,
+  // 550K 153 / 146 / 147, 800K 209 / 196 / 185 (256 floats 305 / 286 / 277). 128 of
+  // bf16 change over later: 300K 86 / 81 / 87, 800K 169 / 153 / 146
   p.span = b->edges <= (1 << 16) ? 16 : b->edges <= (1 << 18) ? 32 : 64;
   p.spans = cdiv(b->edges, p.span);
   int64_t at = 0;
@@ -403,7 +406,8 @@ int with_stream(const StreamPlan& p, F f) {
 // launch, and the form for few rows has more blocks; above, it reads its
 // operands too often. Measured, us, few rows' form / streaming, 256 -> 256: bf16
 // 4000 rows 11 / 20, 8000 21 / 20, 16000 41 / 21; fp32 8000 39 / 44, 16000
-// 75 / 46.
+// 75 / 46. dx in bf16, whose few rows read weights across: 2000 rows 9.8 / 10.1,
+// 4000 15 / 10, 8000 22 / 11, and with gelu's slope 16 / 21, 27 / 21, 47 / 22.
 bool streams(int64_t rows, int64_t cols, int log2_least) { return rows * round_up(cols, 32) >= int64_t(1) << log2_least; }
 
 template <typename T>
