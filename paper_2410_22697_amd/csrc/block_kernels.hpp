@@ -457,7 +457,7 @@ __global__ __launch_bounds__(kMeanNT) void k_block_mean_join(const uint32_t* __r
 // 8.8 us a call, 2000 edges over 500, 2000 and 8192 sources 19, 13 and 16, where
 // the sort's launches take 20, and 20, 26 and 30. A source reads all indices, so
 // more edges or sources go to the sort (2000 edges over 16K sources 26 and 30
-// us, over 32K 44 and 30).
+// us, over 32K 44 and 30), and so do long lists.
 constexpr int kFewEdges = 2048, kFewRows = 2048;  // of the block
 constexpr int kFewSources = 8192;
 

@@ -252,9 +252,14 @@ MeanPlan mean_plan(const massive_block* b, int64_t d) {
 }
 
 // Whether the gradient takes the one-launch form, which reads every index for
-// each source.
+// each source, and in which a source adds up its list by itself: 0.1 us an
+// entry. Where sources are listed in proportion to their degrees the longest
+// list has about edges / sqrt(rows) entries, of which 128 take as long as the
+// sort's launches. One launch / sort, us with 128 floats: 1000 edges over 256
+// sources 12 / 20, 64 19 / 20, 16 32 / 20, 1 107 / 26; 296 over 16 11 / 20, 4
+// 19 / 20, 1 33 / 20.
 bool few(const massive_block* b) {
-  return b->edges <= ms::kFewEdges && b->n <= ms::kFewRows && b->rows <= ms::kFewSources;
+  return b->edges <= ms::kFewEdges && b->n <= ms::kFewRows && b->rows <= ms::kFewSources && b->edges * b->edges <= (b->rows << 14);
 }
 
 int block_mean_backward(const massive_block* b, const void* dout, int32_t type, int64_t dout_stride, int32_t d,
