@@ -502,7 +502,7 @@ class AdamW:
             self._table["m_scale"] = self.m_scale.data_ptr() + starts // 256 * 4
             self._table["v_scale"] = self.v_scale.data_ptr() + starts // 256 * 4
         self._sizes = np.array([p.numel() for p in self.params], np.int64)
-        self._shapes = list(map(_shape_of, self.params))
+        self._own_layout()
         self._memory = self._table["param"] = _pointers(self.params)
         self._table["copy"] = [0 if c is None else c.data_ptr() for c in self.copies]
         self._copy_memory = _pointers(c for c in self.copies if c is not None)
@@ -524,24 +524,31 @@ class AdamW:
     def _own_memory(self):
         """The parameters' and copies' memory may have been replaced since it was last seen."""
         now = _pointers(self.params)
-        if now != self._memory or not all(map(torch.Tensor.is_contiguous, self.params)):
-            for p, n in zip(self.params, self._sizes):
-                if p.dtype != self.dtype or p.numel() != n or not p.is_contiguous():
-                    raise ValueError("a parameter's memory was replaced by another type, size or layout")
+        if now != self._memory or not all(map(torch.Tensor.is_contiguous, self._even)):
+            self._own_layout()
             _on_gpu(*self.params)
             _disjoint(self.params + self.copies)
             self._memory = self._table["param"] = now
         if _pointers(c for c in self.copies if c is not None) != self._copy_memory:
             raise ValueError("a copy's memory was replaced")
 
-    def _shapes_of(self, there, grads):
-        """Whether the gradients have their parameters' shapes, and those the sizes that they began with."""
+    def _own_layout(self):
+        """The parameters still have the type, size and layout that they began with; takes over their shapes."""
+        for p, n in zip(self.params, self._sizes):
+            if p.dtype != self.dtype or p.numel() != n or not p.is_contiguous():
+                raise ValueError("a parameter's memory was replaced by another type, size or layout")
+        self._shapes = list(map(_shape_of, self.params))
+        # those of which a transposition has the same shape
+        self._even = [p for p in self.params if len(set(p.shape) - {1}) < sum(n != 1 for n in p.shape)]
+
+    def _shaped(self, grads, there) -> bool:
+        """Whether the gradients have their parameters' shapes."""
         now = list(map(_shape_of, grads))
-        if now == (self._shapes if isinstance(there, slice) else [self._shapes[i] for i in there]):
+        at = np.arange(len(self.params))[there]
+        if now == (self._shapes if len(at) == len(self.params) else [self._shapes[i] for i in at]):
             return True
-        self._shapes = list(map(_shape_of, self.params))  # which a view of the same memory may have changed
-        return all(p.numel() == n for p, n in zip(self.params, self._sizes)) and \
-            now == [self._shapes[i] for i in np.arange(len(self.params))[there]]
+        self._own_layout()  # a parameter may have been given another view of its memory
+        return now == [self._shapes[i] for i in at]
 
     def step(self, grads: Optional[Sequence] = None):
         """One step. grads: a contiguous tensor of each parameter's shape, all
@@ -568,7 +575,7 @@ class AdamW:
             raise ValueError("gradients must be of one type, float32 or bfloat16")
         self._own_memory()
         if set(map(torch.Tensor.get_device, grads)) != {here} or not all(map(torch.Tensor.is_contiguous, grads)) or \
-                not self._shapes_of(there, grads):
+                not self._shaped(grads, there):
             raise ValueError("a gradient must be a contiguous tensor of its parameter's shape, on cuda:%d" % here)
         self._table["grad"][there] = np.fromiter(map(torch.Tensor.data_ptr, grads), np.uint64, len(grads))
         grad_type, stream = _TYPES[types.pop()], _stream(here)
