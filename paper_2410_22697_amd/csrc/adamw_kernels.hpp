@@ -7,8 +7,8 @@
 // largest magnitude is a reduction within the wave. Each value is read and
 // written once; the kernel is bound by memory.
 //
-// Measured: 160M values, states in 8 bits 470 us (2.6 GB, 5.4 TB/s), the states
-// read back as floats 275 us; nine weights of 131072 in all 6.9 us.
+// Measured: 160M values, states in 8 bits 480 us (2.6 GB, 5.3 TB/s), the states
+// read back as floats 275 us; nine weights of 131072 in all 7.0 us.
 #pragma once
 
 #include "common.hpp"

@@ -11,7 +11,7 @@
 // buffers.
 //
 // Measured: y of 242K rows, 128 + 128 -> 256, in bf16 80 us (3.1 TB/s, 395
-// TFLOP/s); dx of 110K x 1024 by 128 in bf16 with gelu's slope 142 us (3.4 TB/s),
+// TFLOP/s); dx of 110K x 1024 by 128 in bf16 with gelu's slope 151 us (3.2 TB/s),
 // about half of it vector instructions of the slope; dx of 16K x 47 by 512 in fp32
 // 28 us.
 #pragma once
