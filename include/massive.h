@@ -273,9 +273,9 @@ int massive_get_timing(massive_ctx* ctx, double* out_ms, int64_t* out_calls);
  *
  * A call may be captured into a HIP graph. Its replays read and write the same
  * addresses, and keep the arguments that the call had on the host, among them
- * massive_adamw's lr and t: a graph that holds a step repeats that step's bias
- * corrections (with t set far on, when both are 1, that is what is wanted;
- * before, the step belongs behind the graph's replay).
+ * massive_adamw's lr and t: every replay repeats the captured step's bias
+ * corrections. That is right only once both are 1; until then the step belongs
+ * outside the graph.
  */
 #define MASSIVE_F32 0
 #define MASSIVE_BF16 1

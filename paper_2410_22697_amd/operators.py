@@ -539,7 +539,7 @@ class AdamW:
                 raise ValueError("a parameter's memory was replaced by another type, size or layout")
         self._shapes = list(map(_shape_of, self.params))
         # those of which a transposition has the same shape
-        self._even = [p for p in self.params if len(set(p.shape) - {1}) < sum(n != 1 for n in p.shape)]
+        self._even = [p for p in self.params if p.dim() > 1 and len(set(p.shape)) < p.dim()]
 
     def _shaped(self, grads, there) -> bool:
         """Whether the gradients have their parameters' shapes."""
