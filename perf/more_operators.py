@@ -154,8 +154,8 @@ def run(state):
 def _dropout_own(s):
     lib, case = s["lib"], s["case"]
     if case["backward"]:
-        return lib.dropout_backward(s["x"], case["p"], s["key"], stream=s["layer"])
-    return lib.dropout(s["x"], case["p"], s["key"], stream=s["layer"], residual=s["residual"])
+        return lib.dropout_backward(s["x"], case["p"], s["key"], draw=s["layer"])
+    return lib.dropout(s["x"], case["p"], s["key"], draw=s["layer"], residual=s["residual"])
 
 
 def _norm_own(s):
