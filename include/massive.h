@@ -400,6 +400,75 @@ typedef struct {
 int massive_linear_workspace(const massive_linear_grads* args, int64_t* bytes);
 int massive_linear_backward(const massive_linear_grads* args, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Dropout: y = residual + (x kept ? x / (1 - p) : 0), over rows of d columns;
+ * residual may be NULL. The mask is drawn where it is used and not stored:
+ * column j of row i is kept if word j % 4 of Philox4x32-10 at the counter
+ * (j / 4, i, draw, 0), under the seed (its low word first), is at least p 2^32,
+ * rounded to a whole number. It hangs on the column's place alone, so the
+ * gradient of x is the same call on y's, without a residual. Draws of one seed
+ * (a step's layers, say) have masks of their own. With seed_at, the seed is
+ * read there when the stream comes to the call, so that replays of a captured
+ * call can each have another. A column that is not kept gives 0 whatever it
+ * held. */
+typedef struct {
+  const void* x;           /* [rows, d]                                       */
+  const void* residual;    /* [rows, d] or NULL                               */
+  void* y;                 /* [rows, d]                                       */
+  const uint64_t* seed_at; /* device memory, or NULL: `seed`                  */
+  int64_t rows;
+  int64_t x_stride, residual_stride, y_stride;
+  uint64_t seed;
+  double p;                /* in [0, 1]                                       */
+  uint32_t draw;
+  int32_t d, type;
+} massive_dropout_args;
+
+int massive_dropout(const massive_dropout_args* args, void* stream);
+
+/* The root-mean-square norm of rows of d columns: s = x + residual (which may
+ * be NULL), y = s / sqrt(mean(s^2) + eps) * weight (NULL for ones). sum, if not
+ * NULL, receives s; y is computed from s before that is rounded. With fmt
+ * (fmt->d = d), y is a table of table_rows packed rows as massive_pack_rows
+ * writes them, row i of the norm going to row slots[i], or to row i if slots is
+ * NULL; y_stride is ignored. An eps between 0 and 2^-126 counts as 2^-126. Rows
+ * whose squares leave fp32's range are normed all the same; a row of zeros with
+ * an eps of 0 is NaN, and in a row with an infinity the finite values give 0
+ * and the infinities NaN. */
+typedef struct {
+  const void* x;        /* [rows, d]                                          */
+  const void* residual; /* [rows, d] or NULL                                  */
+  const void* weight;   /* [d] or NULL                                        */
+  void* sum;            /* [rows, d] or NULL                                  */
+  void* y;              /* [rows, d], or a table                              */
+  const massive_row_format* fmt;
+  const int32_t* slots;
+  int64_t table_rows;
+  int64_t rows;
+  int64_t x_stride, residual_stride, sum_stride, y_stride;
+  double eps;
+  int32_t d, type;
+} massive_norm_args;
+
+int massive_rms_norm(const massive_norm_args* args, void* stream);
+
+/* Its gradients. With r = 1 / sqrt(mean(s^2) + eps), n = s r and g = dy weight:
+ * dx = r (g - n mean(g n)) + ds, which is x's gradient and residual's, and
+ * dweight = sum of dy n over the rows. s is massive_rms_norm's sum (without a
+ * residual, x); ds, which may be NULL, is the gradient that s gets from
+ * elsewhere. dx and dweight may each be NULL. */
+typedef struct {
+  const void *dy, *s, *weight, *ds;
+  void *dx, *dweight;
+  int64_t rows;
+  int64_t dy_stride, s_stride, ds_stride, dx_stride;
+  double eps;
+  int32_t d, type;
+} massive_norm_grads;
+
+/* Bytes of workspace of massive_rms_norm_backward (0 if dweight is not asked for). */
+int massive_rms_norm_workspace(const massive_norm_grads* args, int64_t* bytes);
+int massive_rms_norm_backward(const massive_norm_grads* args, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* One tensor of an AdamW step, n values. Everything but grad is updated in
  * place. With state_bits 32, m and v are float[n] and the scales are NULL.
  * With state_bits 8, m is int8[n] and v uint8[n], and each 256 values share a

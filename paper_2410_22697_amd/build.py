@@ -3,7 +3,7 @@ import os
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(HERE, "csrc", name) for name in ("massive.hip", "operators.hip")]
+SRCS = [os.path.join(HERE, "csrc", name) for name in ("massive.hip", "operators.hip", "layers.hip")]
 LIB = os.path.join(HERE, "libmassive.so")
 ARCH = os.environ.get("MASSIVE_OFFLOAD_ARCH", "gfx950")
 

@@ -1,0 +1,383 @@
+// norm_kernels.hpp - the root-mean-square norm of x + residual, and its gradients.
+//
+//   s = x + residual          r = 1 / sqrt(mean(s^2) + eps)      y = s r w
+//   n = s r, g = dy w:        dx = r (g - n mean(g n)) + ds      dw = sum over the rows of dy n
+//
+// A row belongs to a team of lanes that holds it in registers (of long rows
+// the first columns, the others are read again), so that it is read once, and
+// y may leave as the codes of a packed row.
+#pragma once
+
+#include "common.hpp"
+#include "rows_kernels.hpp"
+#include "values.hpp"
+
+namespace ms {
+
+constexpr int kNormNT = 256;     // threads of a block of teams
+constexpr int kNormLong = 512;   // threads of a block that has one row at a time
+
+template <typename T>
+struct Norm {
+  const T *x, *residual, *weight;
+  T *sum, *y;
+  uint8_t* table;  // packed rows in y's place
+  const int32_t* slots;
+  int64_t rows, x_stride, residual_stride, sum_stride, y_stride, table_rows;
+  PackedRows f;
+  int32_t d;
+  float inv_d, eps;
+};
+
+template <typename T>
+struct NormGrads {
+  const T *dy, *s, *weight, *ds;
+  T* dx;
+  float* parts;  // [blocks][d] of dw, or null
+  int64_t rows, dy_stride, s_stride, ds_stride, dx_stride;
+  int32_t d;
+  float inv_d, eps;
+};
+
+// A reduction over a team: aligned lanes of a wave, or the whole block.
+template <int TEAM, typename V, typename F>
+__device__ __forceinline__ V norm_reduce(V x, F pick) {
+  if constexpr (TEAM <= MS_WAVE) {
+    return team_reduce(x, TEAM, pick);
+  } else {
+    __shared__ V of_wave[TEAM / MS_WAVE];
+    x = team_reduce(x, MS_WAVE, pick);
+    __syncthreads();
+    if (lane_id() == 0) of_wave[wave_id()] = x;
+    __syncthreads();
+    x = of_wave[0];
+#pragma unroll
+    for (int w = 1; w < TEAM / MS_WAVE; ++w) x = pick(x, of_wave[w]);
+    return x;
+  }
+}
+template <int TEAM>
+__device__ __forceinline__ float norm_sum(float x) {
+  return norm_reduce<TEAM>(x, [](float a, float b) { return a + b; });
+}
+template <int TEAM>
+__device__ __forceinline__ uint32_t norm_max(uint32_t x) {
+  return norm_reduce<TEAM>(x, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+
+// 1 / sqrt(mean + eps) is r 2^-e, and a row's values are taken times 2^-e before
+// they are multiplied by r. e is 0 unless the squares leave fp32's range.
+struct NormScale {
+  float r;
+  int e;
+  __device__ __forceinline__ float of(float s) const { return e ? ldexpf(s, -e) : s; }
+};
+
+// The scale of a row: each(f) gives f every column's value that this lane has,
+// the same for all lanes of the team to take part in reductions after it.
+template <int TEAM, typename E>
+__device__ __forceinline__ NormScale norm_scale(E each, float inv_d, float eps) {
+  float sum = 0.0f;
+  each([&](float s) { sum += s * s; });
+  const float t = norm_sum<TEAM>(sum) * inv_d + eps;
+  if (t > 0x1p-96f && t < 0x1p96f) return {__builtin_amdgcn_rsqf(t), 0};
+  // squares too large or too small for fp32, or not finite: again, by the largest magnitude's power of two
+  uint32_t bits = 0;
+  each([&](float s) { bits = max(bits, __float_as_uint(s) & 0x7FFFFFFFu); });
+  const float most = fmaxf(__uint_as_float(norm_max<TEAM>(bits)), sqrtf(eps));
+  if (!(most < __builtin_inff())) return {most == __builtin_inff() ? 0.0f : __builtin_nanf(""), 0};
+  if (most == 0.0f) return {__builtin_inff(), 0};
+  int e;
+  frexpf(most, &e);
+  sum = 0.0f;
+  each([&](float s) {
+    s = ldexpf(s, -e);
+    sum += s * s;
+  });
+  return {__builtin_amdgcn_rsqf(norm_sum<TEAM>(sum) * inv_d + ldexpf(eps, -2 * e)), e};
+}
+
+template <typename T, int TEAM, int V, int Q, int BITS>
+__global__ __launch_bounds__(TEAM > MS_WAVE ? TEAM : kNormNT) void k_rms_norm(Norm<T> a) {
+  constexpr int kTeams = TEAM > MS_WAVE ? 1 : kNormNT / TEAM, kTurn = TEAM * Q;
+  constexpr bool kLong = TEAM > MS_WAVE;  // columns may lie beyond the registers
+  const int lane = threadIdx.x % TEAM, d = a.d;
+  float w[V][Q];
+#pragma unroll
+  for (int t = 0; t < V; ++t) {
+    const int c = t * kTurn + lane * Q;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) w[t][q] = 1.0f;
+    if (a.weight && c < d) load_cols<T, Q>(a.weight + c, d - c, w[t], 0.0f);
+  }
+  const int64_t step = (int64_t)gridDim.x * kTeams;
+  for (int64_t i = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; i < a.rows; i += step) {
+    const T* x = a.x + i * a.x_stride;
+    const T* res = a.residual ? a.residual + i * a.residual_stride : nullptr;
+    auto load = [&](int c, float (&s)[Q]) {
+      load_cols<T, Q>(x + c, d - c, s);
+      if (res) {
+        float r[Q];
+        load_cols<T, Q>(res + c, d - c, r);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) s[q] += r[q];
+      }
+    };
+    float s[V][Q];
+#pragma unroll
+    for (int t = 0; t < V; ++t) {
+      const int c = t * kTurn + lane * Q;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) s[t][q] = 0.0f;
+      if (c < d) load(c, s[t]);
+    }
+    // f(first column, values), zeros where columns are missing; all lanes take part
+    auto turns = [&](auto f) {
+#pragma unroll
+      for (int t = 0; t < V; ++t) f(t * kTurn + lane * Q, s[t], w[t]);
+      if constexpr (kLong) {
+        for (int c0 = V * kTurn; c0 < d; c0 += kTurn) {
+          const int c = c0 + lane * Q;
+          float u[Q] = {}, v[Q];
+#pragma unroll
+          for (int q = 0; q < Q; ++q) v[q] = 1.0f;
+          if (c < d) {
+            load(c, u);
+            if (a.weight) load_cols<T, Q>(a.weight + c, d - c, v, 0.0f);
+          }
+          f(c, u, v);
+        }
+      }
+    };
+    if (a.sum)
+      turns([&](int c, const float (&v)[Q], const float (&)[Q]) {
+        if (c < d) store_cols<T, Q>(a.sum + i * a.sum_stride + c, d - c, v);
+      });
+    const NormScale scale = norm_scale<TEAM>(
+        [&](auto f) {
+          turns([&](int, const float (&v)[Q], const float (&)[Q]) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) f(v[q]);
+          });
+        },
+        a.inv_d, a.eps);
+    // (a product of its own also where a difference follows, so that codes are those of the value that would be stored)
+    auto normed = [&](const float (&v)[Q], const float (&wv)[Q], float (&y)[Q]) {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int q = 0; q < Q; ++q) y[q] = scale.of(v[q]) * scale.r * wv[q];
+    };
+    if constexpr (BITS == 0) {
+      turns([&](int c, const float (&v)[Q], const float (&wv)[Q]) {
+        float y[Q];
+        normed(v, wv, y);
+        if (c < d) store_cols<T, Q>(a.y + i * a.y_stride + c, d - c, y);
+      });
+    } else {
+      const int64_t slot = a.slots ? (int64_t)a.slots[i] : i;
+      if (slot < 0 || slot >= a.table_rows) continue;  // the same for the whole team
+      uint8_t* row = a.table + slot * a.f.row_bytes;
+      float* floats = reinterpret_cast<float*>(row + a.f.floats_at);
+      float size, inv;
+      if (a.f.group_log2 == 31) {
+        GroupEnds<BITS> ends;
+        turns([&](int c, const float (&v)[Q], const float (&wv)[Q]) {
+          float y[Q];
+          normed(v, wv, y);
+          ends.add(y, d - c);
+        });
+        ends.mag = norm_max<TEAM>(ends.mag);
+        if constexpr (BITS == 4) {
+          ends.lo = norm_reduce<TEAM>(ends.lo, [](float p, float q) { return fminf(p, q); });
+          ends.hi = norm_reduce<TEAM>(ends.hi, [](float p, float q) { return fmaxf(p, q); });
+        }
+        ends.scale(size, inv);
+        turns([&](int c, const float (&v)[Q], const float (&wv)[Q]) {
+          float y[Q];
+          normed(v, wv, y);
+          if (c < d) store_codes<BITS>(row, c, d, y, d - c, ends.lo, inv);
+        });
+        if (lane == 0) {
+          if (BITS == 4) floats[0] = ends.lo;
+          floats[BITS == 4 ? 1 : 0] = size;
+        }
+      } else {
+        const int width = 1 << (a.f.group_log2 - 3);  // lanes that share a group: never more than a turn's of a wave
+        turns([&](int c, const float (&v)[Q], const float (&wv)[Q]) {
+          float y[Q];
+          normed(v, wv, y);
+          GroupEnds<BITS> ends;
+          ends.add(y, d - c);
+          ends.join(width);
+          ends.scale(size, inv);
+          if (c < d) {
+            store_codes<BITS>(row, c, d, y, d - c, ends.lo, inv);
+            if (lane % width == 0) {
+              const int g = c >> a.f.group_log2;
+              if (BITS == 4) floats[2 * g] = ends.lo;
+              floats[BITS == 4 ? 2 * g + 1 : g] = size;
+            }
+          }
+        });
+      }
+    }
+  }
+}
+
+template <typename T, int TEAM, int V, int Q>
+__global__ __launch_bounds__(TEAM > MS_WAVE ? TEAM : kNormNT) void k_rms_norm_backward(NormGrads<T> a) {
+  constexpr int kTeams = TEAM > MS_WAVE ? 1 : kNormNT / TEAM, kTurn = TEAM * Q;
+  constexpr bool kLong = TEAM > MS_WAVE;
+  __shared__ float joined[kLong ? 1 : kNormNT * Q];
+  const int lane = threadIdx.x % TEAM, d = a.d;
+  float* part = a.parts ? a.parts + (int64_t)blockIdx.x * d : nullptr;
+  float w[V][Q], dw[V][Q];
+#pragma unroll
+  for (int t = 0; t < V; ++t) {
+    const int c = t * kTurn + lane * Q;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      w[t][q] = 1.0f;
+      dw[t][q] = 0.0f;
+    }
+    if (a.weight && c < d) load_cols<T, Q>(a.weight + c, d - c, w[t], 0.0f);
+  }
+  if (kLong && part)  // the columns beyond the registers are summed where they end up, by the lane that owns them
+    for (int c0 = V * kTurn; c0 < d; c0 += kTurn)
+      for (int q = 0; q < Q; ++q)
+        if (c0 + lane * Q + q < d) part[c0 + lane * Q + q] = 0.0f;
+  const int64_t step = (int64_t)gridDim.x * kTeams;
+  for (int64_t i = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; i < a.rows; i += step) {
+    const T *dyr = a.dy + i * a.dy_stride, *sr = a.s + i * a.s_stride;
+    const T* dsr = a.ds ? a.ds + i * a.ds_stride : nullptr;
+    float s[V][Q], dy[V][Q], ds[V][Q];
+#pragma unroll
+    for (int t = 0; t < V; ++t) {
+      const int c = t * kTurn + lane * Q;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) s[t][q] = dy[t][q] = ds[t][q] = 0.0f;
+      if (c < d) {
+        load_cols<T, Q>(sr + c, d - c, s[t]);
+        load_cols<T, Q>(dyr + c, d - c, dy[t]);
+        if (dsr) load_cols<T, Q>(dsr + c, d - c, ds[t]);
+      }
+    }
+    const NormScale scale = norm_scale<TEAM>(
+        [&](auto f) {
+#pragma unroll
+          for (int t = 0; t < V; ++t)
+#pragma unroll
+            for (int q = 0; q < Q; ++q) f(s[t][q]);
+          if constexpr (kLong)
+            for (int c = V * kTurn + lane * Q; c < d; c += kTurn) {
+              float u[Q];
+              load_cols<T, Q>(sr + c, d - c, u);
+#pragma unroll
+              for (int q = 0; q < Q; ++q) f(u[q]);
+            }
+        },
+        a.inv_d, a.eps);
+    float dot = 0.0f;
+#pragma unroll
+    for (int t = 0; t < V; ++t)
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        s[t][q] = scale.of(s[t][q]) * scale.r;
+        dw[t][q] += dy[t][q] * s[t][q];
+        dy[t][q] *= w[t][q];
+        dot += dy[t][q] * s[t][q];
+      }
+    // the columns beyond the registers: f(column, normed value, dy, weight)
+    auto beyond = [&](auto f) {
+      for (int c = V * kTurn + lane * Q; c < d; c += kTurn) {
+        float u[Q], g[Q], v[Q];
+        load_cols<T, Q>(sr + c, d - c, u);
+        load_cols<T, Q>(dyr + c, d - c, g);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) v[q] = 1.0f;
+        if (a.weight) load_cols<T, Q>(a.weight + c, d - c, v);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) u[q] = scale.of(u[q]) * scale.r;
+        f(c, u, g, v);
+      }
+    };
+    if constexpr (kLong)
+      beyond([&](int c, const float (&n)[Q], const float (&g)[Q], const float (&v)[Q]) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          dot += g[q] * v[q] * n[q];
+          if (part && c + q < d) part[c + q] += g[q] * n[q];
+        }
+      });
+    const float mean = norm_sum<TEAM>(dot) * a.inv_d;
+    auto back = [&](float g, float n, float add) {
+      const float v = scale.r * (g - n * mean);
+      return (scale.e ? ldexpf(v, -scale.e) : v) + add;
+    };
+    T* dxr = a.dx + i * a.dx_stride;
+    if (a.dx) {
+#pragma unroll
+      for (int t = 0; t < V; ++t) {
+        const int c = t * kTurn + lane * Q;
+        float v[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) v[q] = back(dy[t][q], s[t][q], ds[t][q]);
+        if (c < d) store_cols<T, Q>(dxr + c, d - c, v);
+      }
+      if constexpr (kLong)
+        beyond([&](int c, const float (&n)[Q], const float (&g)[Q], const float (&v)[Q]) {
+          float add[Q] = {}, u[Q];
+          if (dsr) load_cols<T, Q>(dsr + c, d - c, add);
+#pragma unroll
+          for (int q = 0; q < Q; ++q) u[q] = back(g[q] * v[q], n[q], add[q]);
+          store_cols<T, Q>(dxr + c, d - c, u);
+        });
+    }
+  }
+  if (!part) return;
+#pragma unroll
+  for (int t = 0; t < V; ++t) {
+    const int c = t * kTurn + lane * Q;
+    if constexpr (kLong) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+        if (c + q < d) part[c + q] = dw[t][q];
+    } else {
+      // the block's teams add up in order
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < Q; ++q) joined[(threadIdx.x / TEAM) * kTurn + lane * Q + q] = dw[t][q];
+      __syncthreads();
+      for (int j = threadIdx.x; j < kTurn && t * kTurn + j < d; j += kNormNT) {
+        float sum = 0.0f;
+#pragma unroll 8
+        for (int team = 0; team < kTeams; ++team) sum += joined[team * kTurn + j];
+        part[t * kTurn + j] = sum;
+      }
+    }
+  }
+}
+
+// Adds the blocks' parts of dw: sixteen threads a column, each over every
+// sixteenth part, then in order.
+constexpr int kNormJoinWays = 16;
+template <typename T>
+__global__ __launch_bounds__(kNormNT) void k_rms_norm_join(const float* __restrict__ parts, int64_t count, int32_t d, T* __restrict__ dw) {
+  constexpr int kCols = kNormNT / kNormJoinWays;
+  __shared__ float sums[kNormJoinWays][kCols];
+  const int way = threadIdx.x / kCols, at = threadIdx.x % kCols;
+  const int64_t c = (int64_t)blockIdx.x * kCols + at;
+  float t = 0.0f;
+  if (c < d) {
+#pragma unroll 8
+    for (int64_t p = way; p < count; p += kNormJoinWays) t += parts[p * d + c];
+  }
+  sums[way][at] = t;
+  __syncthreads();
+  if (way || c >= d) return;
+#pragma unroll
+  for (int w = 1; w < kNormJoinWays; ++w) t += sums[w][at];
+  dw[c] = (T)t;
+}
+
+}  // namespace ms

@@ -53,6 +53,24 @@ class _LinearGrads(ctypes.Structure):
         [(f, _i32) for f in ("n", "k", "k_second", "type", "act")]
 
 
+class _DropoutArgs(ctypes.Structure):
+    _fields_ = [(f, _vp) for f in ("x", "residual", "y", "seed_at")] + \
+        [(f, _i64) for f in ("rows", "x_stride", "residual_stride", "y_stride")] + \
+        [("seed", ctypes.c_uint64), ("p", ctypes.c_double), ("draw", ctypes.c_uint32), ("d", _i32), ("type", _i32)]
+
+
+class _NormArgs(ctypes.Structure):
+    _fields_ = [(f, _vp) for f in ("x", "residual", "weight", "sum", "y")] + [("fmt", ctypes.POINTER(_Format)), ("slots", _vp)] + \
+        [(f, _i64) for f in ("table_rows", "rows", "x_stride", "residual_stride", "sum_stride", "y_stride")] + \
+        [("eps", ctypes.c_double), ("d", _i32), ("type", _i32)]
+
+
+class _NormGrads(ctypes.Structure):
+    _fields_ = [(f, _vp) for f in ("dy", "s", "weight", "ds", "dx", "dweight")] + \
+        [(f, _i64) for f in ("rows", "dy_stride", "s_stride", "ds_stride", "dx_stride")] + \
+        [("eps", ctypes.c_double), ("d", _i32), ("type", _i32)]
+
+
 class _AdamwTensor(ctypes.Structure):
     _fields_ = [(f, _vp) for f in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", _i64)]
 
@@ -82,6 +100,10 @@ def _load():
         lib.massive_linear.argtypes = [p(_LinearArgs), _vp]
         lib.massive_linear_workspace.argtypes = [p(_LinearGrads), p(_i64)]
         lib.massive_linear_backward.argtypes = [p(_LinearGrads), _vp, _i64, _vp]
+        lib.massive_dropout.argtypes = [p(_DropoutArgs), _vp]
+        lib.massive_rms_norm.argtypes = [p(_NormArgs), _vp]
+        lib.massive_rms_norm_workspace.argtypes = [p(_NormGrads), p(_i64)]
+        lib.massive_rms_norm_backward.argtypes = [p(_NormGrads), _vp, _i64, _vp]
         lib.massive_adamw.argtypes = [p(_AdamwTensor), _i64, p(_AdamwArgs), _vp]
         lib.massive_adamw_states.argtypes = [_vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp]
         _lib = lib
@@ -428,6 +450,181 @@ def linear_backward(dy, x, weight, act: str = "none", pre=None, x2=None, bias: b
     work = torch.empty(need.value, dtype=torch.uint8, device="cuda") if need.value else None
     _check(lib.massive_linear_backward(ctypes.byref(g), _ptr(work), need.value, _stream(here)))
     return dx, dx2, dw, db
+
+
+# ---------------------------------------------------------------------- dropout
+def _seed(seed, draw):
+    """The seed as (64 bits, or the tensor that holds them), and draw, checked."""
+    if not isinstance(draw, int) or not 0 <= draw < 2 ** 32:
+        raise ValueError("draw must be a whole number in 0..2^32 - 1, not %r" % (draw,))
+    if isinstance(seed, torch.Tensor):
+        if seed.dtype != torch.int64 or seed.numel() != 1:
+            raise ValueError("a seed in a tensor must be one int64 value")
+        return 0, seed
+    if not isinstance(seed, int) or not -2 ** 63 <= seed < 2 ** 64:
+        raise ValueError("seed must be a whole number of 64 bits, or an int64 tensor, not %r" % (seed,))
+    return seed % 2 ** 64, None
+
+
+def _dropout(x, p, seed, draw, residual):
+    bits, at = _seed(seed, draw)
+    stride = _matrix(x, "x")
+    here = _on_gpu(x, residual, at)
+    rows, d = x.shape
+    res_stride = 0 if residual is None else _matrix(residual, "residual", cols=d, rows=rows, dtype=x.dtype)
+    if not 0 <= p <= 1:
+        raise ValueError("p must be in [0, 1], not %r" % (p,))
+    y = torch.empty((rows, d), dtype=x.dtype, device="cuda")
+    a = _DropoutArgs(x.data_ptr(), _ptr(residual), y.data_ptr(), _ptr(at), rows, stride, res_stride, d, bits, p, draw, d, _TYPES[x.dtype])
+    if d:
+        _check(_load().massive_dropout(ctypes.byref(a), _stream(here)))
+    return y
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, draw, residual):
+        at = seed if isinstance(seed, torch.Tensor) else None
+        ctx.save_for_backward(at)  # a seed changed before the backward pass would draw another mask: autograd raises
+        ctx.how = p, seed if at is None else None, draw
+        return _dropout(x, p, seed, draw, residual)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        at, = ctx.saved_tensors
+        p, seed, draw = ctx.how
+        dx = _dropout(dy.contiguous(), p, seed if at is None else at, draw, None) if ctx.needs_input_grad[0] else None
+        return dx, None, None, None, dy if ctx.needs_input_grad[4] else None
+
+
+def dropout(x, p: float, seed, draw: int = 0, residual=None):
+    """residual + dropout(x): x / (1 - p) where a column is kept, 0 where it is
+    not, whatever it held. x [rows, d] and residual are float32 or bfloat16, rows
+    of any stride. Column j of row i is kept if word j % 4 of Philox4x32-10 at
+    the counter (j / 4, i, draw, 0) under the seed is at least p 2^32, so the
+    mask is the same wherever it is drawn, and none is stored. draw (0 to
+    2^32 - 1) tells a seed's masks apart: a number for each layer, say, and a
+    seed for each step. seed is a whole number of 64 bits, or an int64 tensor
+    of one value on the GPU, which is read when the stream comes to it (replays
+    of a captured call can have masks of their own) and stays as it is until
+    the backward pass has read it too."""
+    _no_tangent(x, residual)
+    if torch.is_grad_enabled() and (x.requires_grad or (residual is not None and residual.requires_grad)):
+        return _Dropout.apply(x, p, seed, draw, residual)
+    return _dropout(x, p, seed, draw, residual)
+
+
+def dropout_backward(dy, p: float, seed, draw: int = 0):
+    """The gradient of dropout's x: dy under the mask of the same p, seed and
+    draw. The residual's gradient is dy."""
+    _no_tangent(dy)
+    return _dropout(dy, p, seed, draw, None)
+
+
+# ------------------------------------------------------------------------- norm
+def _rms_norm(x, weight, eps, residual, fmt, out, slots):
+    stride = _matrix(x, "x")
+    rows, d = x.shape
+    here = _on_gpu(x, weight, residual, slots)
+    dtype = x.dtype
+    if weight is not None:
+        _vector(weight, "weight", d, dtype)
+    res_stride = 0 if residual is None else _matrix(residual, "residual", cols=d, rows=rows, dtype=dtype)
+    if slots is not None and _ids(slots, "slots") != rows:
+        raise ValueError("x has %d rows, and there are %d slots" % (rows, slots.numel()))
+    table_rows = 0
+    if fmt is None:
+        if out is not None or slots is not None:
+            raise ValueError("out and slots are for packed rows, which fmt asks for")
+        y = torch.empty((rows, d), dtype=dtype, device="cuda")
+    else:
+        if fmt.d != d:
+            raise ValueError("x has %d columns, and the row format %d" % (d, fmt.d))
+        if out is None:
+            if slots is not None:
+                raise ValueError("slots without a table to write to")
+            out = torch.empty((rows, fmt.row_bytes), dtype=torch.uint8, device=x.device)
+            if fmt.row_bytes != fmt.least_bytes:
+                out[:, fmt.least_bytes:] = 0
+        table_rows = _table(out, fmt, "out")
+        if slots is None and table_rows < rows:
+            raise ValueError("out has %d rows, and x %d" % (table_rows, rows))
+        y = out
+    total = None if residual is None else torch.empty((rows, d), dtype=dtype, device="cuda")
+    a = _NormArgs(x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(total), y.data_ptr(), None if fmt is None else ctypes.pointer(fmt.c), _ptr(slots),
+                  table_rows, rows, stride, res_stride, d, d, eps, d, _TYPES[dtype])
+    if d:
+        _check(_load().massive_rms_norm(ctypes.byref(a), _stream(here)))
+    if fmt is not None:
+        increment_version(out)
+    return y, total
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, eps, residual):
+        y, total = _rms_norm(x, weight, eps, residual, None, None, None)
+        ctx.save_for_backward(x if total is None else total, weight)
+        ctx.eps = eps
+        ctx.set_materialize_grads(False)
+        return y if total is None else (y, total)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, ds=None):
+        s, weight = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        if dy is None:
+            dx, dw = ds, None
+        else:
+            dx, dw = rms_norm_backward(dy.contiguous(), s, weight, ctx.eps, None if ds is None else ds.contiguous(), need_dx=need[0] or need[3],
+                                       need_dweight=need[1])
+        return dx if need[0] else None, dw, None, dx if need[3] else None
+
+
+def rms_norm(x, weight=None, eps: float = 1e-6, residual=None, fmt: Optional[RowFormat] = None, out=None, slots=None):
+    """s / sqrt(mean(s^2) + eps) * weight over each row of s = x + residual; with
+    a residual, (that, s). x [rows, d], weight [d] and residual are of one type,
+    float32 or bfloat16, rows of any stride; the mean is float32, of s before it
+    is rounded. With fmt the normed rows are packed, before they are rounded to
+    anything else, and written to a table as pack_rows does: to a new one, or
+    to `out`, its rows slots[i] or its first ones; packed rows have no gradient,
+    and tensors that ask for one are refused."""
+    _no_tangent(x, weight, residual)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, residual)):
+        if fmt is not None or out is not None:
+            raise ValueError("packed rows have no gradient, and a tensor requires one")
+        return _RmsNorm.apply(x, weight, eps, residual)
+    y, total = _rms_norm(x, weight, eps, residual, fmt, out, slots)
+    return y if total is None else (y, total)
+
+
+def rms_norm_backward(dy, s, weight=None, eps: float = 1e-6, ds=None, need_dx: bool = True, need_dweight: bool = True):
+    """(dx, dweight) of rms_norm, None for those not asked for, dweight without
+    a weight too. s is what rms_norm returned beside the norm (without a
+    residual, x), ds the gradient that s gets from elsewhere, which is added to
+    dx. dx is the gradient of x and of the residual."""
+    _no_tangent(dy, s, weight, ds)
+    stride = _matrix(s, "s")
+    rows, d = s.shape
+    here = _on_gpu(dy, s, weight, ds)
+    dtype = s.dtype
+    dy_stride = _matrix(dy, "dy", cols=d, rows=rows, dtype=dtype)
+    ds_stride = 0 if ds is None else _matrix(ds, "ds", cols=d, rows=rows, dtype=dtype)
+    if weight is not None:
+        _vector(weight, "weight", d, dtype)
+    dx = torch.empty((rows, d), dtype=dtype, device="cuda") if need_dx else None
+    dw = torch.empty(d, dtype=dtype, device="cuda") if need_dweight and weight is not None else None
+    if d and (dx is not None or dw is not None):
+        g = _NormGrads(dy.data_ptr(), s.data_ptr(), _ptr(weight), _ptr(ds), _ptr(dx), _ptr(dw), rows, dy_stride, stride, ds_stride, d, eps, d,
+                       _TYPES[dtype])
+        lib = _load()
+        need = _i64()
+        _check(lib.massive_rms_norm_workspace(ctypes.byref(g), ctypes.byref(need)))
+        work = torch.empty(need.value, dtype=torch.uint8, device="cuda") if need.value else None
+        _check(lib.massive_rms_norm_backward(ctypes.byref(g), _ptr(work), need.value, _stream(here)))
+    return dx, dw
 
 
 # ------------------------------------------------------------------------ AdamW
