@@ -469,6 +469,43 @@ typedef struct {
 int massive_rms_norm_workspace(const massive_norm_grads* args, int64_t* bytes);
 int massive_rms_norm_backward(const massive_norm_grads* args, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* A gated layer: with [g | u] = [x | x2] w^T + bias, whose weights' first n rows
+ * are the gate's and the others u's, y = act(g) * u, over `rows` rows. x2,
+ * bias and pre are optional; pre receives [g | u] for the backward pass. All
+ * arrays have one type. */
+typedef struct {
+  const void* x;        /* [rows, k]                                          */
+  const void* x_second; /* [rows, k_second] or NULL                           */
+  const void* w;        /* [2 n, k + k_second]                                */
+  const void* bias;     /* [2 n] or NULL                                      */
+  void* y;              /* [rows, n]                                          */
+  void* pre;            /* [rows, 2 n] or NULL                                */
+  int64_t rows;
+  int64_t x_stride, x_second_stride, w_stride, y_stride, pre_stride;
+  int32_t n, k, k_second; /* n at most 2^19                                   */
+  int32_t type, act;
+} massive_gated_args;
+
+int massive_gated(const massive_gated_args* args, void* stream);
+
+/* Its gradients: dg = dy * u * act'(g), du = dy * act(g), dx = [dg | du] w
+ * (columns of x and x2 apart), dw = [dg | du]^T [x | x2], dbias = sum of
+ * [dg | du] over the rows. dx, dx_second, dw and dbias may each be NULL. With
+ * MASSIVE_BF16, dg and du are rounded to bf16 before the products dx and dw,
+ * as massive_linear_backward rounds dz; dbias sums them unrounded. */
+typedef struct {
+  const void *dy, *pre, *x, *x_second, *w;
+  void *dx, *dx_second, *dw, *dbias;
+  int64_t rows;
+  int64_t dy_stride, pre_stride, x_stride, x_second_stride, w_stride, dx_stride, dx_second_stride, dw_stride;
+  int32_t n, k, k_second;
+  int32_t type, act;
+} massive_gated_grads;
+
+/* Bytes of workspace of massive_gated_backward: [dg | du] and the sums' parts. */
+int massive_gated_workspace(const massive_gated_grads* args, int64_t* bytes);
+int massive_gated_backward(const massive_gated_grads* args, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* One tensor of an AdamW step, n values. Everything but grad is updated in
  * place. With state_bits 32, m and v are float[n] and the scales are NULL.
  * With state_bits 8, m is int8[n] and v uint8[n], and each 256 values share a

@@ -14,7 +14,7 @@ from .massive import (EXPORTS, LIB_PATH, MAX_INFLIGHT, TIMING_GROUPS, BatchBuffe
                       MassiveError, StepResult, load)
 
 # what needs torch is loaded when it is first asked for
-_OPERATORS = ("AdamW", "RowFormat", "block_mean", "block_mean_backward", "dropout", "dropout_backward", "linear", "linear_backward", "pack_rows",
+_OPERATORS = ("AdamW", "RowFormat", "block_mean", "block_mean_backward", "dropout", "dropout_backward", "gated", "gated_backward", "linear", "linear_backward", "pack_rows",
               "rms_norm", "rms_norm_backward", "unpack_rows")
 __all__ = ["EXPORTS", "LIB_PATH", "MAX_INFLIGHT", "TIMING_GROUPS", "BatchBuffers", "Massive", "MassiveError", "StepResult", "load", "massive",
            "operators", *_OPERATORS]

@@ -11,6 +11,7 @@
 #include "../../include/massive.h"
 #include "call_launch.hpp"
 #include "dropout_kernels.hpp"
+#include "gated_kernels.hpp"
 #include "norm_kernels.hpp"
 
 namespace {
@@ -147,6 +148,112 @@ int rms_norm_backward(const massive_norm_grads* a, void* workspace, void* stream
   return launch(what, k_rms_norm_join<T>, cdiv(a->d, kNormNT / kNormJoinWays), kNormNT, 0, stream, (const float*)workspace, blocks, a->d, (T*)a->dweight);
 }
 
+// --------------------------------------------------------------- gated layer
+int check_gated(int64_t rows, int32_t n, int32_t k, int32_t k_second, int32_t type, int32_t act, const void* x_second) {
+  if (!is_type(type)) REFUSE("type must be MASSIVE_F32 or MASSIVE_BF16");
+  if (act < MASSIVE_ACT_NONE || act > MASSIVE_ACT_SILU) REFUSE("act is not one of MASSIVE_ACT_*");
+  if (rows < 0 || rows > kMostRows) REFUSE("rows must be in 0..2^29");
+  if (n < 1 || k < 1 || k_second < 0 || n > (1 << 19) || k > kMostCols || k_second > kMostCols)
+    REFUSE("n must be in 1..2^19, k in 1..2^20, k_second in 0..2^20");
+  if ((k_second > 0) != (x_second != nullptr) && rows > 0) REFUSE("k_second columns and x_second go together");
+  return MASSIVE_OK;
+}
+
+template <typename T>
+Operand<T> rows_of(const void* p, int64_t stride, int64_t rows, int64_t k) {
+  return Operand<T>{(const T*)p, nullptr, stride, 0, rows, k, MASSIVE_ACT_NONE};
+}
+
+template <typename T>
+int gated(const massive_gated_args* a, void* stream) {
+  const char* what = "massive_gated";
+  Gated<T> f;
+  f.x[0] = rows_of<T>(a->x, a->x_stride, a->rows, a->k);
+  f.x[1] = rows_of<T>(a->x_second, a->x_second_stride, a->rows, a->k_second);
+  f.w[0] = {(const T*)a->w, a->w_stride};
+  f.w[1] = {(const T*)a->w + a->k, a->w_stride};
+  f.bias = (const T*)a->bias;
+  f.y = (T*)a->y;
+  f.pre = (T*)a->pre;
+  f.y_stride = a->y_stride;
+  f.pre_stride = a->pre_stride;
+  f.rows = a->rows;
+  f.n = a->n;
+  f.act = a->act;
+  if (a->rows * round_up(a->n, 32) >= int64_t(1) << 20) {
+    auto tile = [&](auto nb) {
+      const int64_t tiles_n = cdiv(a->n, 32 * nb()), blocks = cdiv(a->rows, kTileRows) * tiles_n;
+      if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
+      return launch(what, k_gated_tile<T, nb()>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
+    };
+    return a->n <= 64 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>());
+  }
+  const int tiles_n = (int)cdiv(a->n, 32);
+  return launch(what, k_gated_few<T>, cdiv(a->rows, 32) * tiles_n, kFewNT, 0, stream, f, tiles_n);
+}
+
+// The backward pass's workspace: dz, the parts of db, and the layer's own.
+struct GatedPlan {
+  int64_t groups, part, parts, sums_at, layer_at, bytes;
+  massive_linear_grads layer;
+};
+int gated_plan(const massive_gated_grads* a, GatedPlan* p) {
+  const int size = size_of(a->type);
+  const bool dz = a->rows > 0 && (a->dx || a->dx_second || a->dw || a->dbias);
+  p->groups = cdiv(a->n, kGateUnits * (16 / size));
+  p->part = cdiv(a->rows, std::max<int64_t>(1, std::min(cdiv(a->rows, 4 * kGateWays), 2048 / std::min<int64_t>(2048, p->groups))));
+  p->parts = a->rows > 0 ? cdiv(a->rows, p->part) : 0;
+  p->sums_at = dz ? round_up(a->rows * 2 * a->n * size, 16) : 0;
+  p->layer_at = p->sums_at + (a->dbias ? round_up(p->parts * 2 * a->n * 4, 16) : 0);
+  massive_linear_grads& g = p->layer;
+  g = {};
+  g.x = a->x;
+  g.x_second = a->x_second;
+  g.w = a->w;
+  g.dx = a->dx;
+  g.dx_second = a->dx_second;
+  g.dw = a->dw;
+  g.dbias = a->rows > 0 ? nullptr : a->dbias;  // sums over no rows
+  g.rows = a->rows;
+  g.dy_stride = 2 * (int64_t)a->n;
+  g.x_stride = a->x_stride;
+  g.x_second_stride = a->x_second_stride;
+  g.w_stride = a->w_stride;
+  g.dx_stride = a->dx_stride;
+  g.dx_second_stride = a->dx_second_stride;
+  g.dw_stride = a->dw_stride;
+  g.n = 2 * a->n;
+  g.k = a->k;
+  g.k_second = a->k_second;
+  g.type = a->type;
+  g.act = MASSIVE_ACT_NONE;
+  int64_t layer = 0;
+  if (int rc = massive_linear_workspace(&g, &layer)) return rc;
+  p->bytes = p->layer_at + layer;
+  return MASSIVE_OK;
+}
+
+template <typename T>
+int gated_dz(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
+  GatedDz<T> f;
+  f.dy = (const T*)a->dy;
+  f.pre = (const T*)a->pre;
+  f.dz = (T*)workspace;
+  f.parts = a->dbias ? (float*)(workspace + p.sums_at) : nullptr;
+  f.rows = a->rows;
+  f.part = p.part;
+  f.dy_stride = a->dy_stride;
+  f.pre_stride = a->pre_stride;
+  f.dz_stride = 2 * (int64_t)a->n;
+  f.n = a->n;
+  f.act = a->act;
+  f.groups = (int)p.groups;
+  const char* what = "massive_gated_backward";
+  if (int rc = launch(what, k_gated_dz<T>, p.groups * p.parts, kGateNT, 0, stream, f)) return rc;
+  if (!a->dbias) return MASSIVE_OK;
+  return launch(what, k_rms_norm_join<T>, cdiv(2 * a->n, kNormNT / kNormJoinWays), kNormNT, 0, stream, (const float*)f.parts, p.parts, 2 * a->n, (T*)a->dbias);
+}
+
 }  // namespace
 
 extern "C" {
@@ -218,6 +325,62 @@ int massive_rms_norm_backward(const massive_norm_grads* a, void* workspace, int6
     if (!aligned(workspace, 16)) REFUSE("workspace is not 16-byte aligned");
   }
   return a->type == MASSIVE_F32 ? rms_norm_backward<float>(a, workspace, stream) : rms_norm_backward<bf16>(a, workspace, stream);
+}
+
+int massive_gated(const massive_gated_args* a, void* stream) {
+  if (!a) REFUSE("args is NULL");
+  if (int rc = check_gated(a->rows, a->n, a->k, a->k_second, a->type, a->act, a->x_second)) return rc;
+  if (a->rows == 0) return MASSIVE_OK;
+  if (!a->x || !a->w || !a->y) REFUSE("x / w / y are NULL");
+  if (a->x_stride < a->k || (a->x_second && a->x_second_stride < a->k_second) || a->w_stride < (int64_t)a->k + a->k_second ||
+      a->y_stride < a->n || (a->pre && a->pre_stride < 2 * (int64_t)a->n))
+    REFUSE("a stride is below its rows' length");
+  const int size = size_of(a->type);
+  for (const void* p : {a->x, a->x_second, a->w, a->bias, (const void*)a->y, (const void*)a->pre})
+    if (!aligned(p, size)) REFUSE("an array is not aligned");
+  return a->type == MASSIVE_F32 ? gated<float>(a, stream) : gated<bf16>(a, stream);
+}
+
+int massive_gated_workspace(const massive_gated_grads* a, int64_t* bytes) {
+  if (!bytes) REFUSE("bytes is NULL");
+  if (!a) REFUSE("args is NULL");
+  if (int rc = check_gated(a->rows, a->n, a->k, a->k_second, a->type, a->act, a->x_second)) return rc;
+  GatedPlan p;
+  if (int rc = gated_plan(a, &p)) return rc;
+  *bytes = a->rows > 0 ? p.bytes : 0;
+  return MASSIVE_OK;
+}
+
+int massive_gated_backward(const massive_gated_grads* a, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!a) REFUSE("args is NULL");
+  if (int rc = check_gated(a->rows, a->n, a->k, a->k_second, a->type, a->act, a->x_second)) return rc;
+  if (!a->dx && !a->dx_second && !a->dw && !a->dbias) return MASSIVE_OK;
+  if (a->dx_second && !a->k_second) REFUSE("dx_second without a second input");
+  const int64_t k = (int64_t)a->k + a->k_second;
+  if (a->dw && a->dw_stride < k) REFUSE("a stride is below its rows' length");
+  if (a->rows > 0) {
+    if (!a->dy || !a->pre) REFUSE("dy / pre are NULL");
+    if ((a->dx || a->dx_second) && !a->w) REFUSE("w is NULL");
+    if (a->dw && !a->x) REFUSE("x is NULL");
+    if (a->dy_stride < a->n || a->pre_stride < 2 * (int64_t)a->n || (a->x && a->x_stride < a->k) ||
+        (a->x_second && a->x_second_stride < a->k_second) || (a->w && a->w_stride < k) || (a->dx && a->dx_stride < a->k) ||
+        (a->dx_second && a->dx_second_stride < a->k_second))
+      REFUSE("a stride is below its rows' length");
+  }
+  const int size = size_of(a->type);
+  for (const void* p : {a->dy, a->pre, a->x, a->x_second, a->w, (const void*)a->dx, (const void*)a->dx_second, (const void*)a->dw, (const void*)a->dbias})
+    if (!aligned(p, size)) REFUSE("an array is not aligned");
+  GatedPlan p;
+  if (int rc = gated_plan(a, &p)) return rc;
+  if (a->rows == 0) return massive_linear_backward(&p.layer, nullptr, 0, stream);
+  if (p.groups * p.parts > kMostBlocks) REFUSE("too many rows and columns for one call");
+  if (!workspace || workspace_bytes < p.bytes)
+    return call_error(MASSIVE_ECAPACITY, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)p.bytes);
+  if (!aligned(workspace, 16)) REFUSE("workspace is not 16-byte aligned");
+  char* w = (char*)workspace;
+  p.layer.dy = w;
+  if (int rc = a->type == MASSIVE_F32 ? gated_dz<float>(a, p, w, stream) : gated_dz<bf16>(a, p, w, stream)) return rc;
+  return massive_linear_backward(&p.layer, w + p.layer_at, p.bytes - p.layer_at, stream);
 }
 
 }  // extern "C"

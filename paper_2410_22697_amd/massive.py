@@ -28,7 +28,8 @@ EXPORTS = ("massive_init", "massive_output_bounds", "massive_sample", "massive_s
            "massive_row_layout", "massive_pack_rows", "massive_unpack_rows", "massive_block_mean",
            "massive_block_mean_workspace", "massive_block_mean_backward", "massive_linear", "massive_linear_workspace",
            "massive_linear_backward", "massive_adamw", "massive_adamw_states", "massive_dropout", "massive_rms_norm",
-           "massive_rms_norm_workspace", "massive_rms_norm_backward")
+           "massive_rms_norm_workspace", "massive_rms_norm_backward", "massive_gated", "massive_gated_workspace",
+           "massive_gated_backward")
 
 
 class MassiveError(RuntimeError):

@@ -71,6 +71,16 @@ class _NormGrads(ctypes.Structure):
         [("eps", ctypes.c_double), ("d", _i32), ("type", _i32)]
 
 
+class _GatedArgs(ctypes.Structure):
+    _fields_ = [(f, _vp) for f in ("x", "x_second", "w", "bias", "y", "pre")] + [("rows", _i64)] + \
+        [(f, _i64) for f in ("x_stride", "x_second_stride", "w_stride", "y_stride", "pre_stride")] + \
+        [(f, _i32) for f in ("n", "k", "k_second", "type", "act")]
+
+
+class _GatedGrads(ctypes.Structure):
+    _fields_ = _LinearGrads._fields_
+
+
 class _AdamwTensor(ctypes.Structure):
     _fields_ = [(f, _vp) for f in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", _i64)]
 
@@ -104,6 +114,9 @@ def _load():
         lib.massive_rms_norm.argtypes = [p(_NormArgs), _vp]
         lib.massive_rms_norm_workspace.argtypes = [p(_NormGrads), p(_i64)]
         lib.massive_rms_norm_backward.argtypes = [p(_NormGrads), _vp, _i64, _vp]
+        lib.massive_gated.argtypes = [p(_GatedArgs), _vp]
+        lib.massive_gated_workspace.argtypes = [p(_GatedGrads), p(_i64)]
+        lib.massive_gated_backward.argtypes = [p(_GatedGrads), _vp, _i64, _vp]
         lib.massive_adamw.argtypes = [p(_AdamwTensor), _i64, p(_AdamwArgs), _vp]
         lib.massive_adamw_states.argtypes = [_vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp]
         _lib = lib
@@ -625,6 +638,90 @@ def rms_norm_backward(dy, s, weight=None, eps: float = 1e-6, ds=None, need_dx: b
         work = torch.empty(need.value, dtype=torch.uint8, device="cuda") if need.value else None
         _check(lib.massive_rms_norm_backward(ctypes.byref(g), _ptr(work), need.value, _stream(here)))
     return dx, dw
+
+
+# ------------------------------------------------------------------ gated layer
+def _gated_layer(x, weight, x2):
+    """_layer()'s, with n the outputs of a half."""
+    rows, both, *rest = _layer(x, weight, x2)
+    if both % 2 or not both:
+        raise ValueError("weight has %d rows, and must have two for each output" % both)
+    return rows, both // 2, *rest
+
+
+def _gated(x, weight, bias, act, x2, save_pre):
+    code = _activation(act)
+    rows, n, k, k2, x_stride, x2_stride, w_stride = _gated_layer(x, weight, x2)
+    here = _on_gpu(x, weight, bias, x2)
+    dtype = x.dtype
+    if bias is not None:
+        _vector(bias, "bias", 2 * n, dtype)
+    y = torch.empty((rows, n), dtype=dtype, device="cuda")
+    pre = torch.empty((rows, 2 * n), dtype=dtype, device="cuda") if save_pre else None
+    a = _GatedArgs(x.data_ptr(), _ptr(x2), weight.data_ptr(), _ptr(bias), y.data_ptr(), _ptr(pre), rows, x_stride, x2_stride, w_stride, n, 2 * n,
+                   n, k, k2, _TYPES[dtype], code)
+    _check(_load().massive_gated(ctypes.byref(a), _stream(here)))
+    return y, pre
+
+
+class _Gated(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, act, x2):
+        y, pre = _gated(x, weight, bias, act, x2, True)
+        ctx.save_for_backward(x, weight, x2, pre)
+        ctx.act, ctx.bias = act, bias is not None
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, weight, x2, pre = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx, dx2, dw, db = gated_backward(dy.contiguous(), x, weight, pre, ctx.act, x2, bias=ctx.bias and need[2], need_dx=need[0],
+                                         need_dx2=need[4], need_dw=need[1])
+        return dx, dw, db, None, dx2
+
+
+def gated(x, weight, bias=None, act: str = "silu", x2=None, save_pre: bool = False):
+    """act(g) * u, [g | u] = [x | x2] weight^T + bias, with linear's activations.
+    x [rows, k], x2 [rows, k2], weight [2 n, k + k2], its first n rows the
+    gate's, bias [2 n]; all of one type, float32 or bfloat16, rows of any
+    stride. With save_pre, returns [g | u] too, for gated_backward."""
+    _no_tangent(x, weight, bias, x2)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, x2)):
+        if save_pre:
+            raise ValueError("save_pre is for calls outside autograd")
+        return _Gated.apply(x, weight, bias, act, x2)
+    y, pre = _gated(x, weight, bias, act, x2, save_pre)
+    return (y, pre) if save_pre else y
+
+
+def gated_backward(dy, x, weight, pre, act: str = "silu", x2=None, bias: bool = True, need_dx: bool = True, need_dx2: bool = True,
+                   need_dw: bool = True):
+    """(dx, dx2, dweight, dbias) of `gated`, None for those not asked for or not
+    there. pre is what gated returned with save_pre. In bfloat16, the gradients
+    of g and u are rounded to bfloat16 before they are multiplied by the
+    weights and by the inputs; dbias sums them unrounded."""
+    _no_tangent(dy, x, weight, pre, x2)
+    code = _activation(act)
+    rows, n, k, k2, x_stride, x2_stride, w_stride = _gated_layer(x, weight, x2)
+    here = _on_gpu(dy, x, weight, x2, pre)
+    dtype = x.dtype
+    dy_stride = _matrix(dy, "dy", cols=n, rows=rows, dtype=dtype)
+    pre_stride = _matrix(pre, "pre", cols=2 * n, rows=rows, dtype=dtype)
+    new = lambda *shape: torch.empty(shape, dtype=dtype, device="cuda")  # noqa: E731
+    dx = new(rows, k) if need_dx else None
+    dx2 = new(rows, k2) if need_dx2 and x2 is not None else None
+    dw = new(2 * n, k + k2) if need_dw else None
+    db = new(2 * n) if bias else None
+    g = _GatedGrads(dy.data_ptr(), pre.data_ptr(), x.data_ptr(), _ptr(x2), weight.data_ptr(), _ptr(dx), _ptr(dx2), _ptr(dw), _ptr(db),
+                    rows, dy_stride, pre_stride, x_stride, x2_stride, w_stride, k, k2, k + k2, n, k, k2, _TYPES[dtype], code)
+    lib = _load()
+    need = _i64()
+    _check(lib.massive_gated_workspace(ctypes.byref(g), ctypes.byref(need)))
+    work = torch.empty(need.value, dtype=torch.uint8, device="cuda") if need.value else None
+    _check(lib.massive_gated_backward(ctypes.byref(g), _ptr(work), need.value, _stream(here)))
+    return dx, dx2, dw, db
 
 
 # ------------------------------------------------------------------------ AdamW

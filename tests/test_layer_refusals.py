@@ -92,12 +92,56 @@ def test_workspaces_and_calls_with_nothing_to_do():
     refused(lib().massive_rms_norm_backward(None, None, 0, None), "NULL")
 
 
+def layer(**more):
+    a = dict(x=P, w=P, y=P, rows=4, x_stride=6, w_stride=6, y_stride=5, n=5, k=6, k_second=0, type=0, act=3)
+    return operators._GatedArgs(**{**a, **more})
+
+
+@pytest.mark.parametrize("bad,word", [(dict(type=2), "type"), (dict(act=4), "act"), (dict(act=-1), "act"), (dict(rows=-1), "rows"), (dict(n=0), "n must"),
+                                      (dict(n=(1 << 19) + 1), "n must"), (dict(k=0), "n must"), (dict(k_second=-1), "k_second"), (dict(x=None), "NULL"),
+                                      (dict(w=None), "NULL"), (dict(y=None), "NULL"), (dict(x_stride=5), "stride"), (dict(w_stride=5), "stride"),
+                                      (dict(y_stride=4), "stride"), (dict(k_second=2), "go together"), (dict(x_second=P), "go together"),
+                                      (dict(pre=P, pre_stride=9), "stride"), (dict(bias=P + 2), "aligned"), (dict(rows=1 << 30), "rows")])
+def test_gated(bad, word):
+    a = layer(**bad)
+    refused(lib().massive_gated(ctypes.byref(a), None), word)
+
+
+def gated_grads(**more):
+    a = dict(dy=P, pre=P, x=P, w=P, dx=P, dw=P, dbias=P, rows=4, dy_stride=5, pre_stride=10, x_stride=6, w_stride=6, dx_stride=6, dw_stride=6, n=5, k=6,
+             type=0, act=3)
+    return operators._GatedGrads(**{**a, **more})
+
+
+@pytest.mark.parametrize("bad,word", [(dict(type=3), "type"), (dict(act=9), "act"), (dict(dy=None), "NULL"), (dict(pre=None), "pre"), (dict(w=None), "w is"),
+                                      (dict(x=None), "x is"), (dict(dy_stride=4), "stride"), (dict(pre_stride=9), "stride"), (dict(dw_stride=5), "stride"),
+                                      (dict(dx_stride=5), "stride"), (dict(dx_second=P), "second"), (dict(dw=P + 1), "aligned"), (dict(n=0), "n must")])
+def test_gated_backward(bad, word):
+    a = gated_grads(**bad)
+    refused(lib().massive_gated_backward(ctypes.byref(a), P, 1 << 40, None), word)
+
+
+def test_gated_workspace():
+    a, size = gated_grads(), ctypes.c_int64()
+    assert lib().massive_gated_workspace(ctypes.byref(a), ctypes.byref(size)) == OK and size.value > 0
+    refused(lib().massive_gated_backward(ctypes.byref(a), P, size.value - 1, None), "workspace", ECAPACITY)
+    refused(lib().massive_gated_backward(ctypes.byref(a), None, size.value, None), "workspace", ECAPACITY)
+    refused(lib().massive_gated_backward(ctypes.byref(a), P + 8, size.value, None), "aligned")
+    refused(lib().massive_gated_workspace(ctypes.byref(a), None), "NULL")
+    refused(lib().massive_gated_workspace(None, ctypes.byref(size)), "NULL")
+    assert lib().massive_gated_backward(ctypes.byref(gated_grads(dx=None, dw=None, dbias=None)), None, 0, None) == OK
+    assert lib().massive_gated(ctypes.byref(layer(rows=0, x=None, y=None)), None) == OK
+    refused(lib().massive_gated(None, None), "NULL")
+    refused(lib().massive_gated_backward(None, None, 0, None), "NULL")
+
+
 def test_struct_layouts_match_the_binding(tmp_path):
     """Every field of the structs, as a C99 compiler sees the header."""
     if shutil.which("gcc") is None:
         pytest.skip("needs gcc")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    structs = {"massive_dropout_args": operators._DropoutArgs, "massive_norm_args": operators._NormArgs, "massive_norm_grads": operators._NormGrads}
+    structs = {"massive_dropout_args": operators._DropoutArgs, "massive_norm_args": operators._NormArgs, "massive_norm_grads": operators._NormGrads,
+               "massive_gated_args": operators._GatedArgs, "massive_gated_grads": operators._GatedGrads}
     lines = ["#include <stddef.h>", "#include <stdio.h>", '#include "massive.h"', "int main(void) {"]
     want = []
     for name, s in structs.items():
@@ -122,6 +166,9 @@ X = torch.randn(6, 16)
     (lambda: operators.dropout(X, 0.5, 1, draw=2 ** 32), "draw"), (lambda: operators.dropout(X, 0.5, torch.zeros(2, dtype=torch.int64)), "one int64"),
     (lambda: operators.dropout(X, 0.5, torch.zeros(1)), "one int64"), (lambda: operators.dropout(X.t(), 0.5, 1), "contiguous rows"),
     (lambda: operators.dropout_backward(X.expand(1, 6, 16)[0].expand(6, 16)[:1].expand(6, 16), 0.5, 1), "overlap"),
+    (lambda: operators.gated(X, torch.randn(10, 16)), "device"),
+    (lambda: operators.gated(X, torch.randn(9, 16)), "two for each"), (lambda: operators.gated(X, torch.randn(10, 15)), "shape"),
+    (lambda: operators.gated(X, torch.randn(10, 16), act="tanh"), "act must"), (lambda: operators.gated_backward(X, X, torch.randn(32, 16), X), "device"),
     (lambda: operators.rms_norm(X), "device"), (lambda: operators.rms_norm(X[0]), "2-d"), (lambda: operators.rms_norm_backward(X, X), "device")])
 def test_the_binding_refuses(call, word):
     with pytest.raises(ValueError, match=word):
@@ -132,6 +179,7 @@ def test_tangents_are_refused():
     with forward_ad.dual_level():
         dual = forward_ad.make_dual(X, torch.ones_like(X))
         for bad in (lambda: operators.dropout(dual, 0.5, 1), lambda: operators.dropout(X, 0.5, 1, residual=dual), lambda: operators.rms_norm(dual),
-                    lambda: operators.rms_norm(X, residual=dual), lambda: operators.rms_norm_backward(dual, X), lambda: operators.dropout_backward(dual, 0.5, 1)):
+                    lambda: operators.rms_norm(X, residual=dual), lambda: operators.rms_norm_backward(dual, X), lambda: operators.dropout_backward(dual, 0.5, 1),
+                    lambda: operators.gated(dual, X), lambda: operators.gated_backward(X, X, X, dual)):
             with pytest.raises(ValueError, match="tangent"):
                 bad()
