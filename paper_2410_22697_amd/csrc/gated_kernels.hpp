@@ -33,35 +33,53 @@ __device__ __forceinline__ void with_act(int act, F f) {
   else f(std::integral_constant<int, kActNone>());
 }
 
-// Many rows: 128 rows by 32 NB outputs of both halves a block.
+// Many rows: 128 rows by 32 NB outputs of both halves a block; a wave has 16 NB
+// outputs of the gate and the same of the other half.
 template <typename T, int NB>
 __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles_n, int64_t blocks) {
-  using P = TileProduct<T, NB, false>;
-  constexpr int kOut = 16 * NB;  // outputs of a wave
-  constexpr int kTurns = 4 * 32 * P::template turn_pitch<kOut>();
-  __shared__ __align__(16) char lds[P::kLds > kTurns ? P::kLds : kTurns];
+  typedef TileAlong<T, 64 * NB> A;
+  typedef TileAlong<T, kTileSecond> B;
+  typedef TileTurn<T, 16 * NB> Turn;
+  constexpr int kOut = 16 * NB;
+  constexpr int kLds = tile_lds<A, B>() > 4 * Turn::kBytes ? tile_lds<A, B>() : 4 * Turn::kBytes;
+  __shared__ __align__(16) char lds[kLds];
   __shared__ __align__(16) float bias[2][32 * NB];
   const int64_t tile = tile_of_block(blockIdx.x, blocks);
-  const int64_t r0 = tile / tiles_n * kTileRows;
+  const int64_t r0 = tile / tiles_n * kTileSecond;
   const int n0 = (int)(tile % tiles_n) * (32 * NB);
   if ((int)threadIdx.x < 64 * NB) {
     const int h = threadIdx.x / (32 * NB), c = n0 + threadIdx.x % (32 * NB);
     bias[h][threadIdx.x % (32 * NB)] = a.bias && c < a.n ? (float)a.bias[h * a.n + c] : 0.0f;
   }
+  A weights;
+  B rows;
+  auto segment = [&](int g) {
+    weights.begin([&](int c) {
+      const int square = c / 32 % NB, out = n0 + c / (32 * NB) * kOut + square % (NB / 2) * 32 + c % 32;
+      return a.w[g].p + (int64_t)((square >= NB / 2 ? a.n : 0) + min(out, a.n - 1)) * a.w[g].stride;
+    });
+    rows.begin([&](int r) { return a.x[g].p + min(r0 + r, a.rows - 1) * a.x[g].stride; });  // those that are not there repeat the last one
+  };
+  constexpr int kStep = tile_step<T>();
+  const int first = (int)((a.x[0].K + kStep - 1) / kStep), steps = first + (int)((a.x[1].K + kStep - 1) / kStep);
   f32x16 acc[NB][2] = {};
-  // a wave's squares: NB / 2 of the gate, and those of the other half
-  P::run(a.x, a.w, r0, a.rows, 0, 0,
-         [&](int c) {
-           const int square = c / 32 % NB, out = n0 + c / (32 * NB) * kOut + square % (NB / 2) * 32 + c % 32;
-           return (square >= NB / 2 ? a.n : 0) + min(out, a.n - 1);
-         },
-         lds, acc);
+  segment(0);
+  tile_product<T, NB>(
+      weights, rows, steps,
+      [&](int step) {
+        if (step == first) segment(1);
+        const int g = step < first ? 0 : 1;
+        const int64_t k0 = (int64_t)(step - (g ? first : 0)) * kStep;
+        weights.load(k0, a.x[g].K);
+        rows.load(k0, a.x[g].K);
+      },
+      lds, acc);
   const int lane = lane_id();
   const int wave = wave_uniform((int32_t)wave_id());
-  char* turn = lds + wave * 32 * P::template turn_pitch<kOut>();
+  const Turn turn = {lds + wave * Turn::kBytes};
   const int c0 = wave % 2 * kOut;
-  // f(gate, other half, results) for four outputs at a time, all of which then go to out
-  auto each = [&](T* out, int64_t stride, int at, auto f) {
+  // f(gate, other half) for every output, to out
+  auto each = [&](T* out, int64_t stride, auto f) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -73,16 +91,16 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = f(acc[i][j][4 * q + e] + bg[e], acc[i + NB / 2][j][4 * q + e] + bu[e]);
-          P::template turn_in<kOut>(turn, 32 * i, q, v);
+          turn.in(32 * i, q, v);
         }
-      P::template turn_out<kOut>(turn, out + at, stride, r0 + wave / 2 * 64 + 32 * j, a.rows, n0 + c0, a.n);
+      turn.out(out, stride, r0 + wave / 2 * 64 + 32 * j, a.rows, n0 + c0, a.n);
     }
   };
   if (a.pre) {
-    each(a.pre, a.pre_stride, 0, [](float g, float) { return g; });
-    each(a.pre, a.pre_stride, a.n, [](float, float u) { return u; });
+    each(a.pre, a.pre_stride, [](float g, float) { return g; });
+    each(a.pre + a.n, a.pre_stride, [](float, float u) { return u; });
   }
-  with_act(a.act, [&](auto act) { each(a.y, a.y_stride, 0, [&](float g, float u) { return act_value(g, act()) * u; }); });
+  with_act(a.act, [&](auto act) { each(a.y, a.y_stride, [&](float g, float u) { return act_value(g, act()) * u; }); });
 }
 
 // Few rows: 32 rows by 32 outputs of both halves a block, its eight waves share
@@ -92,6 +110,7 @@ __global__ __launch_bounds__(kFewNT) void k_gated_few(Gated<T> a, int tiles_n) {
   __shared__ float halves[2][32 * 32];
   const int64_t r0 = (int64_t)(blockIdx.x / tiles_n) * 32;
   const int n0 = (int)(blockIdx.x % tiles_n) * 32;
+#pragma unroll 1
   for (int h = 0; h < 2; ++h) {
     const Weights<T> w[2] = {{a.w[0].p + (int64_t)h * a.n * a.w[0].stride, a.w[0].stride}, {a.w[1].p + (int64_t)h * a.n * a.w[1].stride, a.w[1].stride}};
     few_product<T, false, false, 2>(a.x, w, r0, a.rows, n0, a.n, [&](int64_t row, int col, float z) {
@@ -174,6 +193,146 @@ __global__ __launch_bounds__(kGateNT) void k_gated_dz(GatedDz<T> a) {
     for (int v = 0; v < kGateWays; ++v) t += joined[v][h][j];
     if (col < a.n) a.parts[(int64_t)(blockIdx.x / a.groups) * 2 * a.n + h * a.n + col] = t;
   }
+}
+
+// dx = dz w over many rows: 128 rows by 64 NB columns a block.
+template <typename T, int NB>
+__global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tiles_n, int64_t blocks) {
+  typedef TileAcross<T, 64 * NB> A;
+  typedef TileAlong<T, kTileSecond> B;
+  typedef TileTurn<T, 32 * NB> Turn;
+  constexpr int kLds = tile_lds<A, B>() > 4 * Turn::kBytes ? tile_lds<A, B>() : 4 * Turn::kBytes;
+  __shared__ __align__(16) char lds[kLds];
+  const int64_t tile = tile_of_block(blockIdx.x, blocks);
+  const int64_t r0 = tile / tiles_n * kTileSecond;
+  const int n0 = (int)(tile % tiles_n) * (64 * NB);
+  A weights;
+  B rows;
+  weights.begin([&](int c, int& columns, int64_t& stride) {
+    columns = a.cols - (n0 + c);
+    stride = a.w.stride;
+    return a.w.p + n0 + c;
+  });
+  rows.begin([&](int r) { return a.dz.p + min(r0 + r, a.rows - 1) * a.dz.stride; });
+  f32x16 acc[NB][2] = {};
+  tile_product<T, NB>(
+      weights, rows, (int)((a.dz.K + tile_step<T>() - 1) / tile_step<T>()),
+      [&](int step) {
+        weights.load((int64_t)step * tile_step<T>(), a.dz.K);
+        rows.load((int64_t)step * tile_step<T>(), a.dz.K);
+      },
+      lds, acc);
+  const int wave = wave_uniform((int32_t)wave_id());
+  const Turn turn = {lds + wave * Turn::kBytes};
+  const int c0 = n0 + wave % 2 * (32 * NB);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        turn.in(32 * i, q, v);
+      }
+    const int64_t at = r0 + wave / 2 * 64 + 32 * j;
+    constexpr int kV = 16 / sizeof(T);
+    turn.units([&](int r, int c, cols_t<T, kV> v) {
+      const int64_t row = at + r;
+      const int col = c0 + c;
+      if (row >= a.rows) return;
+      const int s = col >= a.split ? 1 : 0, end = s ? a.cols : a.split;
+      if (col + kV <= end) {
+        *reinterpret_cast<cols_t<T, kV>*>(a.dx[s] + row * a.dx_stride[s] + col - (s ? a.split : 0)) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < kV; ++e)
+          if (col + e < a.cols) linear_dx_store(a, row, col + e, (float)v[e]);
+      }
+    });
+  }
+}
+
+// dw = dz^T [x | x2], one part of the rows a block: 128 outputs by 64 NB columns.
+// Columns are placed in whole units, the second input's from `second` on.
+template <typename T, int NB>
+__global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(LinearDw<T> a, int64_t blocks) {
+  typedef TileAcross<T, 64 * NB> A;
+  typedef TileAcross<T, kTileSecond> B;
+  typedef TileTurn<float, 32 * NB> Turn;
+  constexpr int kLds = tile_lds<A, B>() > 4 * Turn::kBytes ? tile_lds<A, B>() : 4 * Turn::kBytes;
+  __shared__ __align__(16) char lds[kLds];
+  const int64_t tile = tile_of_block(blockIdx.x, blocks);
+  const int64_t part = tile / (a.tiles_n * a.tiles_k);
+  const int in = (int)(tile % (a.tiles_n * a.tiles_k));
+  const int n0 = in / a.tiles_k * kTileSecond, k0 = in % a.tiles_k * (64 * NB);
+  const int64_t from = part * a.part, rows = min(a.part, a.rows - from);
+  A xs;
+  B dzs;
+  xs.begin([&](int c, int& columns, int64_t& stride) {
+    const int at = k0 + c, s = at >= a.second ? 1 : 0, col = at - (s ? a.second : 0);
+    columns = a.k[s] - col;
+    stride = a.x[s].stride;
+    return a.x[s].p + from * stride + col;
+  });
+  dzs.begin([&](int c, int& columns, int64_t& stride) {
+    columns = a.n - (n0 + c);
+    stride = a.dz.stride;
+    return a.dz.p + from * stride + n0 + c;
+  });
+  f32x16 acc[NB][2] = {};
+  tile_product<T, NB>(
+      xs, dzs, (int)((rows + tile_step<T>() - 1) / tile_step<T>()),
+      [&](int step) {
+        xs.load((int64_t)step * tile_step<T>(), rows);
+        dzs.load((int64_t)step * tile_step<T>(), rows);
+      },
+      lds, acc);
+  const int wave = wave_uniform((int32_t)wave_id());
+  const Turn turn = {lds + wave * Turn::kBytes};
+  const int all = a.k[0] + a.k[1], c0 = k0 + wave % 2 * (32 * NB);
+  float* dw = a.dw + part * a.n * (int64_t)all;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        turn.in(32 * i, q, v);
+      }
+    const int out = n0 + wave / 2 * 64 + 32 * j;
+    turn.units([&](int r, int c, cols_t<float, 4> v) {
+      if (out + r >= a.n) return;
+      const int at = c0 + c, s = at >= a.second ? 1 : 0, col = at - (s ? a.second : 0);
+      float* p = dw + (int64_t)(out + r) * all + (s ? a.k[0] : 0) + col;
+      if (col + 4 <= a.k[s]) {
+        *reinterpret_cast<cols_t<float, 4>*>(p) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + e < a.k[s]) p[e] = v[e];
+      }
+    });
+  }
+}
+
+// Adds the parts of dw, four values a thread.
+template <typename T>
+__global__ __launch_bounds__(kGateNT) void k_gated_join(const float* __restrict__ parts, int64_t count, int64_t values, int cols, T* __restrict__ dw, int64_t stride) {
+  const int64_t i = ((int64_t)blockIdx.x * kGateNT + threadIdx.x) * 4;
+  if (i >= values) return;
+  const int valid = (int)min(values - i, (int64_t)4);
+  float sum[4] = {};
+#pragma unroll 8
+  for (int64_t p = 0; p < count; ++p) {
+    float v[4];
+    load_cols<float, 4>(parts + p * values + i, valid, v);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] += v[q];
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (q < valid) dw[(i + q) / cols * stride + (i + q) % cols] = (T)sum[q];
 }
 
 }  // namespace ms

@@ -182,7 +182,7 @@ int gated(const massive_gated_args* a, void* stream) {
   f.act = a->act;
   if (a->rows * round_up(a->n, 32) >= int64_t(1) << 20) {
     auto tile = [&](auto nb) {
-      const int64_t tiles_n = cdiv(a->n, 32 * nb()), blocks = cdiv(a->rows, kTileRows) * tiles_n;
+      const int64_t tiles_n = cdiv(a->n, 32 * nb()), blocks = cdiv(a->rows, kTileSecond) * tiles_n;
       if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
       return launch(what, k_gated_tile<T, nb()>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
     };
@@ -192,45 +192,43 @@ int gated(const massive_gated_args* a, void* stream) {
   return launch(what, k_gated_few<T>, cdiv(a->rows, 32) * tiles_n, kFewNT, 0, stream, f, tiles_n);
 }
 
-// The backward pass's workspace: dz, the parts of db, and the layer's own.
-struct GatedPlan {
-  int64_t groups, part, parts, sums_at, layer_at, bytes;
-  massive_linear_grads layer;
+// Parts of dw's rows: as many blocks as the chip holds twice over, none of less
+// than eight steps of rows where there are more.
+struct GatedDwPlan {
+  int nb, second;
+  int64_t tiles_n, tiles_k, part, parts, floats;
 };
-int gated_plan(const massive_gated_grads* a, GatedPlan* p) {
+GatedDwPlan gated_dw_plan(const massive_gated_grads* a) {
+  GatedDwPlan p;
+  const int vector = 16 / size_of(a->type), step = kTileStepBytes / size_of(a->type);
+  p.second = (int)round_up(a->k, vector);
+  const int64_t cols = p.second + a->k_second, n = 2 * (int64_t)a->n;
+  p.nb = cols <= 128 ? 2 : 4;
+  p.tiles_n = cdiv(n, kTileSecond);
+  p.tiles_k = cdiv(cols, 64 * p.nb);
+  const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 8 * step));
+  p.part = std::max<int64_t>(1, round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, 512 / (p.tiles_n * p.tiles_k)))), step));
+  p.parts = cdiv(a->rows, p.part);
+  p.floats = a->dw ? p.parts * n * ((int64_t)a->k + a->k_second) : 0;
+  return p;
+}
+
+// The backward pass's workspace: dz, the parts of db, those of dw.
+struct GatedPlan {
+  int64_t groups, part, parts, sums_at, dw_at, bytes;
+  GatedDwPlan dw;
+};
+GatedPlan gated_plan(const massive_gated_grads* a) {
+  GatedPlan p;
   const int size = size_of(a->type);
-  const bool dz = a->rows > 0 && (a->dx || a->dx_second || a->dw || a->dbias);
-  p->groups = cdiv(a->n, kGateUnits * (16 / size));
-  p->part = cdiv(a->rows, std::max<int64_t>(1, std::min(cdiv(a->rows, 4 * kGateWays), 2048 / std::min<int64_t>(2048, p->groups))));
-  p->parts = a->rows > 0 ? cdiv(a->rows, p->part) : 0;
-  p->sums_at = dz ? round_up(a->rows * 2 * a->n * size, 16) : 0;
-  p->layer_at = p->sums_at + (a->dbias ? round_up(p->parts * 2 * a->n * 4, 16) : 0);
-  massive_linear_grads& g = p->layer;
-  g = {};
-  g.x = a->x;
-  g.x_second = a->x_second;
-  g.w = a->w;
-  g.dx = a->dx;
-  g.dx_second = a->dx_second;
-  g.dw = a->dw;
-  g.dbias = a->rows > 0 ? nullptr : a->dbias;  // sums over no rows
-  g.rows = a->rows;
-  g.dy_stride = 2 * (int64_t)a->n;
-  g.x_stride = a->x_stride;
-  g.x_second_stride = a->x_second_stride;
-  g.w_stride = a->w_stride;
-  g.dx_stride = a->dx_stride;
-  g.dx_second_stride = a->dx_second_stride;
-  g.dw_stride = a->dw_stride;
-  g.n = 2 * a->n;
-  g.k = a->k;
-  g.k_second = a->k_second;
-  g.type = a->type;
-  g.act = MASSIVE_ACT_NONE;
-  int64_t layer = 0;
-  if (int rc = massive_linear_workspace(&g, &layer)) return rc;
-  p->bytes = p->layer_at + layer;
-  return MASSIVE_OK;
+  p.groups = cdiv(a->n, kGateUnits * (16 / size));
+  p.part = std::max<int64_t>(1, cdiv(a->rows, std::max<int64_t>(1, std::min(cdiv(a->rows, 4 * kGateWays), 2048 / std::min<int64_t>(2048, p.groups)))));
+  p.parts = cdiv(a->rows, p.part);
+  p.dw = gated_dw_plan(a);
+  p.sums_at = round_up(a->rows * 2 * a->n * size, 16);
+  p.dw_at = p.sums_at + (a->dbias ? round_up(p.parts * 2 * a->n * 4, 16) : 0);
+  p.bytes = p.dw_at + p.dw.floats * 4;
+  return p;
 }
 
 template <typename T>
@@ -252,6 +250,52 @@ int gated_dz(const massive_gated_grads* a, const GatedPlan& p, char* workspace, 
   if (int rc = launch(what, k_gated_dz<T>, p.groups * p.parts, kGateNT, 0, stream, f)) return rc;
   if (!a->dbias) return MASSIVE_OK;
   return launch(what, k_rms_norm_join<T>, cdiv(2 * a->n, kNormNT / kNormJoinWays), kNormNT, 0, stream, (const float*)f.parts, p.parts, 2 * a->n, (T*)a->dbias);
+}
+
+template <typename T>
+int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
+  const char* what = "massive_gated_backward";
+  if (int rc = gated_dz<T>(a, p, workspace, stream)) return rc;
+  const int n = 2 * a->n;
+  const Operand<T> dz = rows_of<T>(workspace, n, a->rows, n);
+  if (a->dx || a->dx_second) {
+    LinearDx<T> f;
+    f.dz = dz;
+    const int k0 = a->dx ? a->k : 0, k1 = a->dx_second ? a->k_second : 0;
+    f.w = {(const T*)a->w + (a->dx ? 0 : a->k), a->w_stride};
+    f.dx[0] = (T*)a->dx;
+    f.dx[1] = (T*)a->dx_second;
+    f.dx_stride[0] = a->dx_stride;
+    f.dx_stride[1] = a->dx_second_stride;
+    f.rows = a->rows;
+    f.cols = k0 + k1;
+    f.split = k0;
+    auto tile = [&](auto nb) {
+      const int64_t tiles_n = cdiv(f.cols, 64 * nb()), blocks = cdiv(a->rows, kTileSecond) * tiles_n;
+      return launch(what, k_gated_dx<T, nb()>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
+    };
+    if (int rc = f.cols <= 128 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
+  }
+  if (!a->dw) return MASSIVE_OK;
+  LinearDw<T> f;
+  f.dz = dz;
+  f.x[0] = rows_of<T>(a->x, a->x_stride, a->rows, a->k);
+  f.x[1] = rows_of<T>(a->x_second, a->x_second_stride, a->rows, a->k_second);
+  f.dw = (float*)(workspace + p.dw_at);
+  f.dbias = nullptr;
+  f.rows = a->rows;
+  f.part = p.dw.part;
+  f.n = n;
+  f.k[0] = a->k;
+  f.k[1] = a->k_second;
+  f.second = p.dw.second;
+  f.tiles_n = (int)p.dw.tiles_n;
+  f.tiles_k = (int)p.dw.tiles_k;
+  const int64_t blocks = p.dw.parts * p.dw.tiles_n * p.dw.tiles_k;
+  if (int rc = launch(what, p.dw.nb == 2 ? k_gated_dw<T, 2> : k_gated_dw<T, 4>, blocks, kTileNT, 0, stream, f, blocks)) return rc;
+  const int cols = a->k + a->k_second;
+  const int64_t values = (int64_t)n * cols;
+  return launch(what, k_gated_join<T>, cdiv(values, 4 * kGateNT), kGateNT, 0, stream, (const float*)f.dw, p.dw.parts, values, cols, (T*)a->dw, a->dw_stride);
 }
 
 }  // namespace
@@ -345,9 +389,7 @@ int massive_gated_workspace(const massive_gated_grads* a, int64_t* bytes) {
   if (!bytes) REFUSE("bytes is NULL");
   if (!a) REFUSE("args is NULL");
   if (int rc = check_gated(a->rows, a->n, a->k, a->k_second, a->type, a->act, a->x_second)) return rc;
-  GatedPlan p;
-  if (int rc = gated_plan(a, &p)) return rc;
-  *bytes = a->rows > 0 ? p.bytes : 0;
+  *bytes = a->rows > 0 ? gated_plan(a).bytes : 0;
   return MASSIVE_OK;
 }
 
@@ -370,17 +412,26 @@ int massive_gated_backward(const massive_gated_grads* a, void* workspace, int64_
   const int size = size_of(a->type);
   for (const void* p : {a->dy, a->pre, a->x, a->x_second, a->w, (const void*)a->dx, (const void*)a->dx_second, (const void*)a->dw, (const void*)a->dbias})
     if (!aligned(p, size)) REFUSE("an array is not aligned");
-  GatedPlan p;
-  if (int rc = gated_plan(a, &p)) return rc;
-  if (a->rows == 0) return massive_linear_backward(&p.layer, nullptr, 0, stream);
-  if (p.groups * p.parts > kMostBlocks) REFUSE("too many rows and columns for one call");
+  const GatedPlan p = gated_plan(a);
+  const int64_t values = a->dw ? 2 * a->n * k : 0;
+  if (p.groups * p.parts > kMostBlocks || p.dw.parts * p.dw.tiles_n * p.dw.tiles_k > kMostBlocks || cdiv(values, 4 * kGateNT) > kMostBlocks ||
+      cdiv(a->rows, kTileSecond) * cdiv(k, 128) > kMostBlocks)
+    REFUSE("too many rows and columns for one call");
+  if (a->rows == 0) {  // sums over no rows
+    const char* what = "massive_gated_backward";
+    return with_type(a->type, [&](auto* t) {
+      using T = std::remove_pointer_t<decltype(t)>;
+      if (a->dw)
+        if (int rc = launch(what, k_gated_join<T>, cdiv(values, 4 * kGateNT), kGateNT, 0, stream, (const float*)nullptr, int64_t(0), values, (int)k, (T*)a->dw, a->dw_stride))
+          return rc;
+      if (!a->dbias) return MASSIVE_OK;
+      return launch(what, k_rms_norm_join<T>, cdiv(2 * a->n, kNormNT / kNormJoinWays), kNormNT, 0, stream, (const float*)nullptr, int64_t(0), 2 * a->n, (T*)a->dbias);
+    });
+  }
   if (!workspace || workspace_bytes < p.bytes)
     return call_error(MASSIVE_ECAPACITY, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)p.bytes);
   if (!aligned(workspace, 16)) REFUSE("workspace is not 16-byte aligned");
-  char* w = (char*)workspace;
-  p.layer.dy = w;
-  if (int rc = a->type == MASSIVE_F32 ? gated_dz<float>(a, p, w, stream) : gated_dz<bf16>(a, p, w, stream)) return rc;
-  return massive_linear_backward(&p.layer, w + p.layer_at, p.bytes - p.layer_at, stream);
+  return a->type == MASSIVE_F32 ? gated_backward<float>(a, p, (char*)workspace, stream) : gated_backward<bf16>(a, p, (char*)workspace, stream);
 }
 
 }  // extern "C"
