@@ -24,6 +24,11 @@ struct Gated {
   int n, act;
 };
 
+template <int V>
+__device__ __forceinline__ int round_up_to(int x) {
+  return (x + V - 1) / V * V;
+}
+
 // Calls f(act) with the activation as a type.
 template <typename F>
 __device__ __forceinline__ void with_act(int act, F f) {
@@ -53,25 +58,18 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles
   }
   A weights;
   B rows;
-  auto segment = [&](int g) {
-    weights.begin([&](int c) {
-      const int square = c / 32 % NB, out = n0 + c / (32 * NB) * kOut + square % (NB / 2) * 32 + c % 32;
-      return a.w[g].p + (int64_t)((square >= NB / 2 ? a.n : 0) + min(out, a.n - 1)) * a.w[g].stride;
-    });
-    rows.begin([&](int r) { return a.x[g].p + min(r0 + r, a.rows - 1) * a.x[g].stride; });  // those that are not there repeat the last one
-  };
-  constexpr int kStep = tile_step<T>();
-  const int first = (int)((a.x[0].K + kStep - 1) / kStep), steps = first + (int)((a.x[1].K + kStep - 1) / kStep);
   f32x16 acc[NB][2] = {};
-  segment(0);
+  const TileSegment segments[2] = {{a.x[0].K, true}, {a.x[1].K, true}};
   tile_product<T, NB>(
-      weights, rows, steps,
-      [&](int step) {
-        if (step == first) segment(1);
-        const int g = step < first ? 0 : 1;
-        const int64_t k0 = (int64_t)(step - (g ? first : 0)) * kStep;
-        weights.load(k0, a.x[g].K);
-        rows.load(k0, a.x[g].K);
+      weights, rows, segments,
+      [&](int g) {
+        const T *xp = g ? a.x[1].p : a.x[0].p, *wp = g ? a.w[1].p : a.w[0].p;
+        const int64_t x_stride = g ? a.x[1].stride : a.x[0].stride;
+        weights.begin([&](int c) {
+          const int square = c / 32 % NB, out = n0 + c / (32 * NB) * kOut + square % (NB / 2) * 32 + c % 32;
+          return wp + (int64_t)((square >= NB / 2 ? a.n : 0) + min(out, a.n - 1)) * a.w[0].stride;
+        });
+        rows.begin([&](int r) { return xp + min(r0 + r, a.rows - 1) * x_stride; });  // those that are not there repeat the last one
       },
       lds, acc);
   const int lane = lane_id();
@@ -208,18 +206,18 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tile
   const int n0 = (int)(tile % tiles_n) * (64 * NB);
   A weights;
   B rows;
-  weights.begin([&](int c, int& columns, int64_t& stride) {
-    columns = a.cols - (n0 + c);
-    stride = a.w.stride;
-    return a.w.p + n0 + c;
-  });
-  rows.begin([&](int r) { return a.dz.p + min(r0 + r, a.rows - 1) * a.dz.stride; });
   f32x16 acc[NB][2] = {};
+  const TileSegment segments[1] = {{a.dz.K, a.cols >= 16 / (int)sizeof(T)}};
   tile_product<T, NB>(
-      weights, rows, (int)((a.dz.K + tile_step<T>() - 1) / tile_step<T>()),
-      [&](int step) {
-        weights.load((int64_t)step * tile_step<T>(), a.dz.K);
-        rows.load((int64_t)step * tile_step<T>(), a.dz.K);
+      weights, rows, segments,
+      [&](int) {
+        weights.begin([&](int c, int& at, int& columns, int64_t& stride) {
+          at = n0 + c;
+          columns = a.cols;
+          stride = a.w.stride;
+          return a.w.p;
+        });
+        rows.begin([&](int r) { return a.dz.p + min(r0 + r, a.rows - 1) * a.dz.stride; });
       },
       lds, acc);
   const int wave = wave_uniform((int32_t)wave_id());
@@ -238,10 +236,9 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tile
     constexpr int kV = 16 / sizeof(T);
     turn.units([&](int r, int c, cols_t<T, kV> v) {
       const int64_t row = at + r;
-      const int col = c0 + c;
-      if (row >= a.rows) return;
-      const int s = col >= a.split ? 1 : 0, end = s ? a.cols : a.split;
-      if (col + kV <= end) {
+      if (row >= a.rows || c0 + c >= a.cols) return;
+      const int col = tile_column<T>(c0 + c, a.cols), s = col >= a.split ? 1 : 0;
+      if (col + kV <= (s ? a.cols : a.split)) {
         *reinterpret_cast<cols_t<T, kV>*>(a.dx[s] + row * a.dx_stride[s] + col - (s ? a.split : 0)) = v;
       } else {
 #pragma unroll
@@ -268,23 +265,25 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(LinearDw<T> a, int64_t 
   const int64_t from = part * a.part, rows = min(a.part, a.rows - from);
   A xs;
   B dzs;
-  xs.begin([&](int c, int& columns, int64_t& stride) {
-    const int at = k0 + c, s = at >= a.second ? 1 : 0, col = at - (s ? a.second : 0);
-    columns = a.k[s] - col;
-    stride = a.x[s].stride;
-    return a.x[s].p + from * stride + col;
-  });
-  dzs.begin([&](int c, int& columns, int64_t& stride) {
-    columns = a.n - (n0 + c);
-    stride = a.dz.stride;
-    return a.dz.p + from * stride + n0 + c;
-  });
   f32x16 acc[NB][2] = {};
+  constexpr int kV = 16 / sizeof(T);
+  const TileSegment segments[1] = {{rows, a.n >= kV && a.k[0] >= kV && (a.k[1] == 0 || a.k[1] >= kV)}};
   tile_product<T, NB>(
-      xs, dzs, (int)((rows + tile_step<T>() - 1) / tile_step<T>()),
-      [&](int step) {
-        xs.load((int64_t)step * tile_step<T>(), rows);
-        dzs.load((int64_t)step * tile_step<T>(), rows);
+      xs, dzs, segments,
+      [&](int) {
+        xs.begin([&](int c, int& at, int& columns, int64_t& stride) {
+          const int s = k0 + c >= a.second && a.k[1] > 0 ? 1 : 0;
+          at = k0 + c - (s ? a.second : 0);
+          columns = s ? a.k[1] : a.k[0];
+          stride = s ? a.x[1].stride : a.x[0].stride;
+          return (s ? a.x[1].p : a.x[0].p) + from * stride;
+        });
+        dzs.begin([&](int c, int& at, int& columns, int64_t& stride) {
+          at = n0 + c;
+          columns = a.n;
+          stride = a.dz.stride;
+          return a.dz.p + from * stride;
+        });
       },
       lds, acc);
   const int wave = wave_uniform((int32_t)wave_id());
@@ -302,15 +301,17 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(LinearDw<T> a, int64_t 
       }
     const int out = n0 + wave / 2 * 64 + 32 * j;
     turn.units([&](int r, int c, cols_t<float, 4> v) {
-      if (out + r >= a.n) return;
-      const int at = c0 + c, s = at >= a.second ? 1 : 0, col = at - (s ? a.second : 0);
-      float* p = dw + (int64_t)(out + r) * all + (s ? a.k[0] : 0) + col;
-      if (col + 4 <= a.k[s]) {
+      const int at = c0 + c, s = at >= a.second ? 1 : 0, c1 = at - (s ? a.second : 0), columns = s ? a.k[1] : a.k[0];
+      if (out + r >= round_up_to<kV>(a.n) || c1 >= round_up_to<kV>(columns)) return;
+      const int row = tile_column<T>(out + r, a.n), col = tile_column<T>(c1, columns);
+      if (row >= a.n) return;
+      float* p = dw + (int64_t)row * all + (s ? a.k[0] : 0) + col;
+      if (col + 4 <= columns) {
         *reinterpret_cast<cols_t<float, 4>*>(p) = v;
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (col + e < a.k[s]) p[e] = v[e];
+          if (col + e < columns) p[e] = v[e];
       }
     });
   }

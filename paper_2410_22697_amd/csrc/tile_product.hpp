@@ -30,6 +30,11 @@ constexpr int tile_step() {
   return kTileStepBytes / sizeof(T);
 }
 
+// Both kinds of operand hold what a thread takes of a step: whole() asks for it
+// where the step's k are all there, and ragged() where some lie behind the last
+// one (left out as k_along() leaves them out); either goes on to the next step.
+// A loop of whole() has no branch that would wait for a load.
+
 // An operand along k, COLS columns of it: column c's row of k begins at
 // where(c). In LDS the units of a column change places, so that eight columns'
 // same units lie in distinct banks.
@@ -43,17 +48,22 @@ struct TileAlong {
   template <typename F>
   __device__ __forceinline__ void begin(F where) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) p[i] = where((int)threadIdx.x / 4 + i * (kTileNT / 4));
+    for (int i = 0; i < kPer; ++i) p[i] = where((int)threadIdx.x / 4 + i * (kTileNT / 4)) + threadIdx.x % 4 * kV;
+  }
+  __device__ __forceinline__ void whole() {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      v[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(p[i]));
+      p[i] += tile_step<T>();
+    }
   }
   // k0: the step's first k, of K
-  __device__ __forceinline__ void load(int64_t k0, int64_t K) {
+  __device__ __forceinline__ void ragged(int64_t k0, int64_t K) {
     const int64_t k = k0 + threadIdx.x % 4 * kV;
-    if (k0 + tile_step<T>() <= K) {
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) v[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(p[i] + k));
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) v[i] = k_along(p[i], k, K);
+    for (int i = 0; i < kPer; ++i) {
+      v[i] = k_along(p[i] - k, k, K);
+      p[i] += tile_step<T>();
     }
   }
   __device__ __forceinline__ void put(char* to) const {
@@ -67,75 +77,100 @@ struct TileAlong {
   }
 };
 
-// An operand across k: the columns of a unit begin at where(c, columns), which
-// also says how many of them and those after them there are (none: where() is
-// not followed).
+// An operand across k. Its columns are read in units of 16 bytes that are all
+// there: the last one ends with the row (tile_column() says which columns it
+// holds), one behind it repeats it, and its results go nowhere or are stored
+// twice. Rows of less than 16 bytes are read value by value, by ragged() alone.
 template <typename T, int COLS>
 struct TileAcross {
   static constexpr int kV = 16 / sizeof(T), kPer = COLS * 4 / kTileNT, kColUnits = COLS / kV;
   static constexpr int kBytes = tile_step<T>() * dw_pitch<T, COLS>();
-  const T* p[kPer];
-  int64_t stride[kPer];
-  int columns[kPer];
+  static constexpr int kRows = kTileNT / kColUnits;  // that the block takes at a time: a thread's columns are the same in all of them
+  static_assert(kTileNT % kColUnits == 0, "");
+  const T* p;
+  int64_t stride;
+  int narrow;  // columns, where there are less than a unit's
   u32x4 v[kPer];
 
+  // where(c, first, columns, stride): the row of k = 0, which of its columns position c is, how many there are
   template <typename F>
   __device__ __forceinline__ void begin(F where) {
+    int c, columns;
+    const T* row = where((int)threadIdx.x % kColUnits * kV, c, columns, stride);
+    narrow = columns < kV ? columns : 0;
+    p = row + (columns < kV ? 0 : min(c, columns - kV)) + (int64_t)(threadIdx.x / kColUnits) * stride;
+  }
+  __device__ __forceinline__ void whole() {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int id = threadIdx.x + i * kTileNT;
-      p[i] = where(id % kColUnits * kV, columns[i], stride[i]) + (int64_t)(id / kColUnits) * stride[i];
+      v[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(p));
+      p += kRows * stride;
     }
   }
-  __device__ __forceinline__ void load(int64_t k0, int64_t K) {
+  __device__ __forceinline__ void ragged(int64_t k0, int64_t K) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      // (a ragged end is read as k_along() reads it: the last kV of k, those before k left out)
-      const int r = ((int)threadIdx.x + i * kTileNT) / kColUnits, in = r % kV;
+      const int r = (int)threadIdx.x / kColUnits + i * kRows, in = r % kV;
       const int64_t unit = k0 + (r - in);
       const int skip = K >= kV ? skipped<T>(unit, K) : (unit + in < K ? 0 : kV);
-      const T* from = p[i] + (skip && K >= kV ? K - kV - (r - in) : k0) * stride[i];
+      const T* from = p + (skip && K >= kV ? K - kV - unit : 0) * stride;
       v[i] = (u32x4)0u;
-      if (columns[i] > 0 && in >= skip) {
-        if (columns[i] >= kV) {
-          v[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(from));
-        } else {
+      if (in >= skip) {
+        if (narrow) {
           cols_t<T, kV> t;
 #pragma unroll
-          for (int q = 0; q < kV; ++q) t[q] = q < columns[i] ? from[q] : (T)0.0f;
+          for (int q = 0; q < kV; ++q) t[q] = q < narrow ? from[q] : (T)0.0f;
           v[i] = __builtin_bit_cast(u32x4, t);
+        } else {
+          v[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(from));
         }
       }
+      p += kRows * stride;
     }
   }
   __device__ __forceinline__ void put(char* to) const {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int id = threadIdx.x + i * kTileNT;
-      *reinterpret_cast<u32x4*>(to + id / kColUnits * dw_pitch<T, COLS>() + id % kColUnits * 16) = v[i];
-    }
+    for (int i = 0; i < kPer; ++i)
+      *reinterpret_cast<u32x4*>(to + (threadIdx.x / kColUnits + i * kRows) * dw_pitch<T, COLS>() + threadIdx.x % kColUnits * 16) = v[i];
   }
   static __device__ __forceinline__ u32x4 fragment(const char* from, int c0, int s) { return dw_fragment<T, COLS>(from, c0, s); }
 };
+
+// The first column of the V that an operand across k has from column c on (c a
+// multiple of a unit's; V columns of a unit at most): c, or less where that unit
+// was moved to end with the row.
+template <typename T>
+__device__ __forceinline__ int tile_column(int c, int columns) {
+  constexpr int kV = 16 / sizeof(T);
+  const int unit = c / kV * kV;
+  return c - (columns >= kV && unit + kV > columns ? unit + kV - columns : 0);
+}
 
 template <typename A, typename B>
 constexpr int tile_lds() {
   return 2 * (A::kBytes + B::kBytes);
 }
 
+// A segment of the reduction: K of it, of which the steps all there are taken by
+// whole() if `plain` (by ragged() else).
+struct TileSegment {
+  int64_t K;
+  bool plain;
+};
+
 // acc[i][j] += the products of the first operand's columns wave % 2 * 32 NB + 32 i
-// on and the second's wave / 2 * 64 + 32 j on, over `steps` steps; load(step)
-// asks for both operands' part of a step.
-template <typename T, int NB, typename A, typename B, typename L>
-__device__ __forceinline__ void tile_product(A& first, B& second, int steps, L load, char* lds, f32x16 (&acc)[NB][2]) {
-  constexpr int kBuffer = A::kBytes + B::kBytes;
+// on and the second's wave / 2 * 64 + 32 j on, over SEGMENTS segments, none of
+// them before the first empty; begin(g) begins segment g of both operands.
+template <typename T, int NB, int SEGMENTS, typename A, typename B, typename F>
+__device__ __forceinline__ void tile_product(A& first, B& second, const TileSegment (&segments)[SEGMENTS], F begin, char* lds, f32x16 (&acc)[NB][2]) {
+  constexpr int kBuffer = A::kBytes + B::kBytes, kStep = tile_step<T>();
   const int wave = wave_uniform((int32_t)wave_id());
   auto put = [&](int buffer) {
-    first.put(lds + buffer * kBuffer);
-    second.put(lds + buffer * kBuffer + A::kBytes);
+    first.put(lds + buffer);
+    second.put(lds + buffer + A::kBytes);
   };
   auto multiply = [&](int buffer) {
-    const char *fa = lds + buffer * kBuffer, *fb = fa + A::kBytes;
+    const char *fa = lds + buffer, *fb = fa + A::kBytes;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       u32x4 a[NB], b[2];
@@ -157,17 +192,53 @@ __device__ __forceinline__ void tile_product(A& first, B& second, int steps, L l
         }
     }
   };
-  if (steps > 0) {
-    load(0);
-    put(0);
-  }
-  __syncthreads();
-  for (int s = 0; s < steps; ++s) {
-    if (s + 1 < steps) load(s + 1);
-    multiply(s % 2);
-    if (s + 1 < steps) put((s + 1) % 2);
+  // the step that was asked for is put beside the one before it, which is multiplied meanwhile
+  int buffer = 0;
+  auto step = [&] {
+    __builtin_amdgcn_sched_barrier(0);  // the step's loads stay ahead of the products that they run beside, and its stores behind them
+    multiply(buffer);
+    __builtin_amdgcn_sched_barrier(0);
+    buffer = kBuffer - buffer;
+    put(buffer);
     __syncthreads();
+  };
+  begin(0);
+  int64_t k0 = 0;
+  if (segments[0].plain && kStep <= segments[0].K) {
+    first.whole();
+    second.whole();
+  } else {
+    first.ragged(0, segments[0].K);
+    second.ragged(0, segments[0].K);
   }
+  put(0);
+  __syncthreads();
+  k0 = kStep;
+#pragma unroll 1
+  for (int g = 0; g < SEGMENTS; ++g) {
+    if (g > 0) {
+      if (segments[SEGMENTS - 1].K <= 0) break;
+      begin(g);
+      k0 = 0;
+    }
+    const int64_t K = SEGMENTS > 1 && g ? segments[SEGMENTS - 1].K : segments[0].K;
+    if (SEGMENTS > 1 && g ? segments[SEGMENTS - 1].plain : segments[0].plain) {
+#pragma unroll 1
+      for (; k0 + kStep <= K; k0 += kStep) {
+        first.whole();
+        second.whole();
+        step();
+      }
+    }
+#pragma unroll 1
+    for (; k0 < K; k0 += kStep) {
+      first.ragged(k0, K);
+      second.ragged(k0, K);
+      step();
+    }
+  }
+  multiply(buffer);
+  __syncthreads();
 }
 
 // A wave's way out: 32 of the second operand's columns, OUT of the first's for
