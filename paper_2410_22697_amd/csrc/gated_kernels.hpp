@@ -40,15 +40,16 @@ __device__ __forceinline__ void with_act(int act, F f) {
 
 // Many rows: 128 rows by 32 NB outputs of both halves a block; a wave has 16 NB
 // outputs of the gate and the same of the other half.
-template <typename T, int NB>
+template <typename T, int NB, bool DIRECT>
 __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles_n, int64_t blocks) {
   typedef TileAlong<T, 64 * NB> A;
   typedef TileAlong<T, kTileSecond> B;
   typedef TileTurn<T, 16 * NB> Turn;
   constexpr int kOut = 16 * NB;
-  constexpr int kLds = tile_lds<A, B>() > 4 * Turn::kBytes ? tile_lds<A, B>() : 4 * Turn::kBytes;
-  __shared__ __align__(16) char lds[kLds];
-  __shared__ __align__(16) float bias[2][32 * NB];
+  constexpr int kLds = tile_lds<A, B>(DIRECT) > 4 * Turn::kBytes ? tile_lds<A, B>(DIRECT) : 4 * Turn::kBytes;
+  // (all in one array: between two, the compiler would have LDS reads wait for whatever is on its way to the other)
+  __shared__ __align__(16) char lds[kLds + 64 * NB * sizeof(float)];
+  float(*bias)[32 * NB] = reinterpret_cast<float(*)[32 * NB]>(lds + kLds);
   const int64_t tile = tile_of_block(blockIdx.x, blocks);
   const int64_t r0 = tile / tiles_n * kTileSecond;
   const int n0 = (int)(tile % tiles_n) * (32 * NB);
@@ -60,9 +61,7 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles
   B rows;
   f32x16 acc[NB][2] = {};
   const TileSegment segments[2] = {{a.x[0].K, true}, {a.x[1].K, true}};
-  tile_product<T, NB>(
-      weights, rows, segments,
-      [&](int g) {
+  auto begin = [&](int g) {
         const T *xp = g ? a.x[1].p : a.x[0].p, *wp = g ? a.w[1].p : a.w[0].p;
         const int64_t x_stride = g ? a.x[1].stride : a.x[0].stride;
         weights.begin([&](int c) {
@@ -70,8 +69,9 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles
           return wp + (int64_t)((square >= NB / 2 ? a.n : 0) + min(out, a.n - 1)) * a.w[0].stride;
         });
         rows.begin([&](int r) { return xp + min(r0 + r, a.rows - 1) * x_stride; });  // those that are not there repeat the last one
-      },
-      lds, acc);
+  };
+  if constexpr (DIRECT) tile_product_direct<T, NB>(weights, rows, segments, begin, lds, acc);
+  else tile_product<T, NB>(weights, rows, segments, begin, lds, acc);
   const int lane = lane_id();
   const int wave = wave_uniform((int32_t)wave_id());
   const Turn turn = {lds + wave * Turn::kBytes};
@@ -194,12 +194,12 @@ __global__ __launch_bounds__(kGateNT) void k_gated_dz(GatedDz<T> a) {
 }
 
 // dx = dz w over many rows: 128 rows by 64 NB columns a block.
-template <typename T, int NB>
+template <typename T, int NB, bool DIRECT>
 __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tiles_n, int64_t blocks) {
   typedef TileAcross<T, 64 * NB> A;
   typedef TileAlong<T, kTileSecond> B;
   typedef TileTurn<T, 32 * NB> Turn;
-  constexpr int kLds = tile_lds<A, B>() > 4 * Turn::kBytes ? tile_lds<A, B>() : 4 * Turn::kBytes;
+  constexpr int kLds = tile_lds<A, B>(DIRECT) > 4 * Turn::kBytes ? tile_lds<A, B>(DIRECT) : 4 * Turn::kBytes;
   __shared__ __align__(16) char lds[kLds];
   const int64_t tile = tile_of_block(blockIdx.x, blocks);
   const int64_t r0 = tile / tiles_n * kTileSecond;
@@ -208,9 +208,7 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tile
   B rows;
   f32x16 acc[NB][2] = {};
   const TileSegment segments[1] = {{a.dz.K, a.cols >= 16 / (int)sizeof(T)}};
-  tile_product<T, NB>(
-      weights, rows, segments,
-      [&](int) {
+  auto begin = [&](int) {
         weights.begin([&](int c, int& at, int& columns, int64_t& stride) {
           at = n0 + c;
           columns = a.cols;
@@ -218,8 +216,9 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tile
           return a.w.p;
         });
         rows.begin([&](int r) { return a.dz.p + min(r0 + r, a.rows - 1) * a.dz.stride; });
-      },
-      lds, acc);
+  };
+  if constexpr (DIRECT) tile_product_direct<T, NB>(weights, rows, segments, begin, lds, acc);
+  else tile_product<T, NB>(weights, rows, segments, begin, lds, acc);
   const int wave = wave_uniform((int32_t)wave_id());
   const Turn turn = {lds + wave * Turn::kBytes};
   const int c0 = n0 + wave % 2 * (32 * NB);
@@ -251,12 +250,12 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tile
 
 // dw = dz^T [x | x2], one part of the rows a block: 128 outputs by 64 NB columns.
 // Columns are placed in whole units, the second input's from `second` on.
-template <typename T, int NB>
+template <typename T, int NB, bool DIRECT>
 __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(LinearDw<T> a, int64_t blocks) {
   typedef TileAcross<T, 64 * NB> A;
   typedef TileAcross<T, kTileSecond> B;
   typedef TileTurn<float, 32 * NB> Turn;
-  constexpr int kLds = tile_lds<A, B>() > 4 * Turn::kBytes ? tile_lds<A, B>() : 4 * Turn::kBytes;
+  constexpr int kLds = tile_lds<A, B>(DIRECT) > 4 * Turn::kBytes ? tile_lds<A, B>(DIRECT) : 4 * Turn::kBytes;
   __shared__ __align__(16) char lds[kLds];
   const int64_t tile = tile_of_block(blockIdx.x, blocks);
   const int64_t part = tile / (a.tiles_n * a.tiles_k);
@@ -268,9 +267,7 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(LinearDw<T> a, int64_t 
   f32x16 acc[NB][2] = {};
   constexpr int kV = 16 / sizeof(T);
   const TileSegment segments[1] = {{rows, a.n >= kV && a.k[0] >= kV && (a.k[1] == 0 || a.k[1] >= kV)}};
-  tile_product<T, NB>(
-      xs, dzs, segments,
-      [&](int) {
+  auto begin = [&](int) {
         xs.begin([&](int c, int& at, int& columns, int64_t& stride) {
           const int s = k0 + c >= a.second && a.k[1] > 0 ? 1 : 0;
           at = k0 + c - (s ? a.second : 0);
@@ -284,8 +281,9 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(LinearDw<T> a, int64_t 
           stride = a.dz.stride;
           return a.dz.p + from * stride;
         });
-      },
-      lds, acc);
+  };
+  if constexpr (DIRECT) tile_product_direct<T, NB>(xs, dzs, segments, begin, lds, acc);
+  else tile_product<T, NB>(xs, dzs, segments, begin, lds, acc);
   const int wave = wave_uniform((int32_t)wave_id());
   const Turn turn = {lds + wave * Turn::kBytes};
   const int all = a.k[0] + a.k[1], c0 = k0 + wave % 2 * (32 * NB);

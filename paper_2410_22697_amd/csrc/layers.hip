@@ -164,6 +164,12 @@ Operand<T> rows_of(const void* p, int64_t stride, int64_t rows, int64_t k) {
   return Operand<T>{(const T*)p, nullptr, stride, 0, rows, k, MASSIVE_ACT_NONE};
 }
 
+// Whether rows begin at multiples of 16 bytes (NULL counts as such).
+template <typename T>
+bool in_units(const void* p, int64_t stride) {
+  return !p || (aligned(p, 16) && stride * (int64_t)sizeof(T) % 16 == 0);
+}
+
 template <typename T>
 int gated(const massive_gated_args* a, void* stream) {
   const char* what = "massive_gated";
@@ -181,10 +187,12 @@ int gated(const massive_gated_args* a, void* stream) {
   f.n = a->n;
   f.act = a->act;
   if (a->rows * round_up(a->n, 32) >= int64_t(1) << 20) {
+    const bool direct = in_units<T>(a->x, a->x_stride) && in_units<T>(a->x_second, a->x_second_stride) && in_units<T>(a->w, a->w_stride) &&
+                        (!a->x_second || a->k * sizeof(T) % 16 == 0);
     auto tile = [&](auto nb) {
       const int64_t tiles_n = cdiv(a->n, 32 * nb()), blocks = cdiv(a->rows, kTileSecond) * tiles_n;
       if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
-      return launch(what, k_gated_tile<T, nb()>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
+      return launch(what, direct ? k_gated_tile<T, nb(), true> : k_gated_tile<T, nb(), false>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
     };
     return a->n <= 64 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>());
   }
@@ -256,6 +264,7 @@ template <typename T>
 int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
   const char* what = "massive_gated_backward";
   if (int rc = gated_dz<T>(a, p, workspace, stream)) return rc;
+  constexpr int kV = 16 / sizeof(T);
   const int n = 2 * a->n;
   const Operand<T> dz = rows_of<T>(workspace, n, a->rows, n);
   if (a->dx || a->dx_second) {
@@ -270,9 +279,10 @@ int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* works
     f.rows = a->rows;
     f.cols = k0 + k1;
     f.split = k0;
+    const bool direct = n % kV == 0 && in_units<T>(f.w.p, f.w.stride) && f.cols % kV == 0;
     auto tile = [&](auto nb) {
       const int64_t tiles_n = cdiv(f.cols, 64 * nb()), blocks = cdiv(a->rows, kTileSecond) * tiles_n;
-      return launch(what, k_gated_dx<T, nb()>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
+      return launch(what, direct ? k_gated_dx<T, nb(), true> : k_gated_dx<T, nb(), false>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
     };
     if (int rc = f.cols <= 128 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
   }
@@ -292,7 +302,9 @@ int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* works
   f.tiles_n = (int)p.dw.tiles_n;
   f.tiles_k = (int)p.dw.tiles_k;
   const int64_t blocks = p.dw.parts * p.dw.tiles_n * p.dw.tiles_k;
-  if (int rc = launch(what, p.dw.nb == 2 ? k_gated_dw<T, 2> : k_gated_dw<T, 4>, blocks, kTileNT, 0, stream, f, blocks)) return rc;
+  const bool direct = n % kV == 0 && a->k % kV == 0 && a->k_second % kV == 0 && in_units<T>(a->x, a->x_stride) && in_units<T>(a->x_second, a->x_second_stride);
+  auto tile = [&](auto nb) { return launch(what, direct ? k_gated_dw<T, nb(), true> : k_gated_dw<T, nb(), false>, blocks, kTileNT, 0, stream, f, blocks); };
+  if (int rc = p.dw.nb == 2 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
   const int cols = a->k + a->k_second;
   const int64_t values = (int64_t)n * cols;
   return launch(what, k_gated_join<T>, cdiv(values, 4 * kGateNT), kGateNT, 0, stream, (const float*)f.dw, p.dw.parts, values, cols, (T*)a->dw, a->dw_stride);

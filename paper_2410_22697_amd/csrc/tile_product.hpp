@@ -32,8 +32,25 @@ constexpr int tile_step() {
 
 // Both kinds of operand hold what a thread takes of a step: whole() asks for it
 // where the step's k are all there, and ragged() where some lie behind the last
-// one (left out as k_along() leaves them out); either goes on to the next step.
-// A loop of whole() has no branch that would wait for a load.
+// one (left out as k_along() leaves them out); either goes on to the next step,
+// and put() gives it to LDS. direct() is whole() and put() without the registers
+// between, for rows whose units are aligned. A thread's units lie in LDS at
+// 16 bytes times its number, for that reason; what is where is settled by which
+// units it reads.
+typedef __attribute__((address_space(1))) const void global_void;
+typedef __attribute__((address_space(3))) void lds_void;
+__device__ __forceinline__ void tile_direct(const void* from, char* to) {
+  __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)(to + threadIdx.x / MS_WAVE * (MS_WAVE * 16)), 16, 0, 0);
+}
+
+// Four rows' 16-bit values of a column, for 16 lanes: their own 4 columns of 16,
+// row by row. (The qualifier is what tells the compiler that the read need not
+// wait for what direct() has on its way; tile_sync() has waited for what counts.)
+__device__ __forceinline__ uint2 tile_turned(const char* __restrict__ p) {
+  typedef short short4v __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) short4v* lds_ptr;
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p));
+}
 
 // An operand along k, COLS columns of it: column c's row of k begins at
 // where(c). In LDS the units of a column change places, so that eight columns'
@@ -44,11 +61,18 @@ struct TileAlong {
   const T* p[kPer];
   u32x4 v[kPer];
 
-  static __device__ __forceinline__ int place(int c, int u) { return (c * 4 + (u ^ ((c >> 1) & 3))) * 16; }
+  static __device__ __forceinline__ int unit() { return (threadIdx.x % 4) ^ (threadIdx.x / 8 % 4); }
   template <typename F>
   __device__ __forceinline__ void begin(F where) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) p[i] = where((int)threadIdx.x / 4 + i * (kTileNT / 4)) + threadIdx.x % 4 * kV;
+    for (int i = 0; i < kPer; ++i) p[i] = where((int)threadIdx.x / 4 + i * (kTileNT / 4)) + unit() * kV;
+  }
+  __device__ __forceinline__ void direct(char* to) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      tile_direct(p[i], to + i * (kTileNT * 16));
+      p[i] += tile_step<T>();
+    }
   }
   __device__ __forceinline__ void whole() {
 #pragma unroll
@@ -59,7 +83,7 @@ struct TileAlong {
   }
   // k0: the step's first k, of K
   __device__ __forceinline__ void ragged(int64_t k0, int64_t K) {
-    const int64_t k = k0 + threadIdx.x % 4 * kV;
+    const int64_t k = k0 + unit() * kV;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       v[i] = k_along(p[i] - k, k, K);
@@ -68,12 +92,12 @@ struct TileAlong {
   }
   __device__ __forceinline__ void put(char* to) const {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) *reinterpret_cast<u32x4*>(to + place(threadIdx.x / 4 + i * (kTileNT / 4), threadIdx.x % 4)) = v[i];
+    for (int i = 0; i < kPer; ++i) *reinterpret_cast<u32x4*>(to + (threadIdx.x + i * kTileNT) * 16) = v[i];
   }
   // the columns c0 to c0 + 31 in the step's half s
   static __device__ __forceinline__ u32x4 fragment(const char* from, int c0, int s) {
-    const int lane = lane_id();
-    return *reinterpret_cast<const u32x4*>(from + place(c0 + lane % 32, 2 * s + lane / 32));
+    const int lane = lane_id(), c = c0 + lane % 32, u = 2 * s + lane / 32;
+    return *reinterpret_cast<const u32x4*>(from + (c * 4 + (u ^ ((c >> 1) & 3))) * 16);
   }
 };
 
@@ -81,12 +105,14 @@ struct TileAlong {
 // there: the last one ends with the row (tile_column() says which columns it
 // holds), one behind it repeats it, and its results go nowhere or are stored
 // twice. Rows of less than 16 bytes are read value by value, by ragged() alone.
+// In LDS 32 bytes change places within their row, so that four rows' same ones
+// (what 16 lanes read transposed) lie in distinct banks.
 template <typename T, int COLS>
 struct TileAcross {
-  static constexpr int kV = 16 / sizeof(T), kPer = COLS * 4 / kTileNT, kColUnits = COLS / kV;
-  static constexpr int kBytes = tile_step<T>() * dw_pitch<T, COLS>();
+  static constexpr int kV = 16 / sizeof(T), kPer = COLS * 4 / kTileNT, kColUnits = COLS / kV, kPitch = COLS * sizeof(T);
+  static constexpr int kBytes = tile_step<T>() * kPitch;
   static constexpr int kRows = kTileNT / kColUnits;  // that the block takes at a time: a thread's columns are the same in all of them
-  static_assert(kTileNT % kColUnits == 0, "");
+  static_assert(kTileNT % kColUnits == 0 && kRows % 4 == 0, "");
   const T* p;
   int64_t stride;
   int narrow;  // columns, where there are less than a unit's
@@ -96,9 +122,16 @@ struct TileAcross {
   template <typename F>
   __device__ __forceinline__ void begin(F where) {
     int c, columns;
-    const T* row = where((int)threadIdx.x % kColUnits * kV, c, columns, stride);
+    const T* row = where((((int)threadIdx.x % kColUnits) ^ ((int)threadIdx.x / kColUnits % 4 * 2)) * kV, c, columns, stride);
     narrow = columns < kV ? columns : 0;
     p = row + (columns < kV ? 0 : min(c, columns - kV)) + (int64_t)(threadIdx.x / kColUnits) * stride;
+  }
+  __device__ __forceinline__ void direct(char* to) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      tile_direct(p, to + i * (kTileNT * 16));
+      p += kRows * stride;
+    }
   }
   __device__ __forceinline__ void whole() {
 #pragma unroll
@@ -130,10 +163,25 @@ struct TileAcross {
   }
   __device__ __forceinline__ void put(char* to) const {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      *reinterpret_cast<u32x4*>(to + (threadIdx.x / kColUnits + i * kRows) * dw_pitch<T, COLS>() + threadIdx.x % kColUnits * 16) = v[i];
+    for (int i = 0; i < kPer; ++i) *reinterpret_cast<u32x4*>(to + (threadIdx.x + i * kTileNT) * 16) = v[i];
   }
-  static __device__ __forceinline__ u32x4 fragment(const char* from, int c0, int s) { return dw_fragment<T, COLS>(from, c0, s); }
+  // the columns c0 to c0 + 31 in the step's half s
+  static __device__ __forceinline__ u32x4 fragment(const char* from, int c0, int s) {
+    const int lane = lane_id();
+    if constexpr (sizeof(T) == 2) {
+      const int group = lane / 16, i = lane % 16, r = 16 * s + 8 * (group / 2) + i / 4, chunk = c0 / 16 + group % 2;
+      const char* p = from + r * kPitch + (chunk ^ (i / 4)) * 32 + i % 4 * 8;
+      const uint2 a = tile_turned(p), b = tile_turned(p + 4 * kPitch);
+      return u32x4{a.x, a.y, b.x, b.y};
+    } else {
+      const int c = c0 + lane % 32;
+      const char* p = from + (8 * s + 4 * (lane / 32)) * kPitch + c % 8 * 4;
+      u32x4 v;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const uint32_t*>(p + q * kPitch + (c / 8 ^ q) * 32);
+      return v;
+    }
+  }
 };
 
 // The first column of the V that an operand across k has from column c on (c a
@@ -146,64 +194,66 @@ __device__ __forceinline__ int tile_column(int c, int columns) {
   return c - (columns >= kV && unit + kV > columns ? unit + kV - columns : 0);
 }
 
+constexpr int kTileBuffers[2] = {2, 3};  // of the two ways through registers and direct
 template <typename A, typename B>
-constexpr int tile_lds() {
-  return 2 * (A::kBytes + B::kBytes);
+constexpr int tile_lds(bool direct) {
+  return kTileBuffers[direct] * (A::kBytes + B::kBytes);
 }
 
 // A segment of the reduction: K of it, of which the steps all there are taken by
-// whole() if `plain` (by ragged() else).
+// whole() if `plain` (by ragged() else; direct() is for plain ones).
 struct TileSegment {
   int64_t K;
   bool plain;
 };
 
 // acc[i][j] += the products of the first operand's columns wave % 2 * 32 NB + 32 i
-// on and the second's wave / 2 * 64 + 32 j on, over SEGMENTS segments, none of
-// them before the first empty; begin(g) begins segment g of both operands.
+// on and the second's wave / 2 * 64 + 32 j on, in the step at `from`.
+template <typename T, int NB, typename A, typename B>
+__device__ __forceinline__ void tile_multiply(const char* from, f32x16 (&acc)[NB][2]) {
+  const int wave = wave_uniform((int32_t)wave_id());
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    u32x4 a[NB], b[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) b[j] = B::fragment(from + A::kBytes, wave / 2 * 64 + 32 * j, s);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) a[i] = A::fragment(from, wave % 2 * (32 * NB) + 32 * i, s);
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if constexpr (sizeof(T) == 2) {
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, b[j]), acc[i][j], 0, 0, 0);
+        } else {
+          const f32x4 u = __builtin_bit_cast(f32x4, a[i]), v = __builtin_bit_cast(f32x4, b[j]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(u[q], v[q], acc[i][j], 0, 0, 0);
+        }
+      }
+  }
+}
+
+// acc += the products over SEGMENTS segments, the first of them not empty;
+// begin(g) begins segment g of both operands. Through registers: a step is on its
+// way in them while the one before it is multiplied.
 template <typename T, int NB, int SEGMENTS, typename A, typename B, typename F>
 __device__ __forceinline__ void tile_product(A& first, B& second, const TileSegment (&segments)[SEGMENTS], F begin, char* lds, f32x16 (&acc)[NB][2]) {
   constexpr int kBuffer = A::kBytes + B::kBytes, kStep = tile_step<T>();
-  const int wave = wave_uniform((int32_t)wave_id());
-  auto put = [&](int buffer) {
+  int buffer = 0;
+  auto put = [&] {
     first.put(lds + buffer);
     second.put(lds + buffer + A::kBytes);
-  };
-  auto multiply = [&](int buffer) {
-    const char *fa = lds + buffer, *fb = fa + A::kBytes;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 a[NB], b[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) b[j] = B::fragment(fb, wave / 2 * 64 + 32 * j, s);
-#pragma unroll
-      for (int i = 0; i < NB; ++i) a[i] = A::fragment(fa, wave % 2 * (32 * NB) + 32 * i, s);
-#pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          if constexpr (sizeof(T) == 2) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, b[j]), acc[i][j], 0, 0, 0);
-          } else {
-            const f32x4 u = __builtin_bit_cast(f32x4, a[i]), v = __builtin_bit_cast(f32x4, b[j]);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(u[q], v[q], acc[i][j], 0, 0, 0);
-          }
-        }
-    }
-  };
-  // the step that was asked for is put beside the one before it, which is multiplied meanwhile
-  int buffer = 0;
-  auto step = [&] {
-    __builtin_amdgcn_sched_barrier(0);  // the step's loads stay ahead of the products that they run beside, and its stores behind them
-    multiply(buffer);
-    __builtin_amdgcn_sched_barrier(0);
-    buffer = kBuffer - buffer;
-    put(buffer);
     __syncthreads();
   };
+  auto step = [&] {
+    __builtin_amdgcn_sched_barrier(0);  // the step's loads stay ahead of the products that they run beside, and its stores behind them
+    tile_multiply<T, NB, A, B>(lds + buffer, acc);
+    __builtin_amdgcn_sched_barrier(0);
+    buffer = kBuffer - buffer;
+    put();
+  };
   begin(0);
-  int64_t k0 = 0;
   if (segments[0].plain && kStep <= segments[0].K) {
     first.whole();
     second.whole();
@@ -211,9 +261,8 @@ __device__ __forceinline__ void tile_product(A& first, B& second, const TileSegm
     first.ragged(0, segments[0].K);
     second.ragged(0, segments[0].K);
   }
-  put(0);
-  __syncthreads();
-  k0 = kStep;
+  put();
+  int64_t k0 = kStep;
 #pragma unroll 1
   for (int g = 0; g < SEGMENTS; ++g) {
     if (g > 0) {
@@ -237,7 +286,96 @@ __device__ __forceinline__ void tile_product(A& first, B& second, const TileSegm
       step();
     }
   }
-  multiply(buffer);
+  tile_multiply<T, NB, A, B>(lds + buffer, acc);
+  __syncthreads();
+}
+
+// Waits until this wave's memory reads but the last LEFT have arrived, and its
+// LDS accesses, and then for the block's other waves to come here.
+template <int LEFT>
+__device__ __forceinline__ void tile_sync() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
+// The same with direct(), in three buffers: two steps are on their way while the
+// one before them is multiplied. A step goes to the buffer that was multiplied
+// before the barrier, and is read behind a barrier that every wave comes to once
+// its own part has arrived: reads arrive in order, so what is left then is the
+// step asked for last.
+template <typename T, int NB, int SEGMENTS, typename A, typename B, typename F>
+__device__ __forceinline__ void tile_product_direct(A& first, B& second, const TileSegment (&segments)[SEGMENTS], F begin, char* lds, f32x16 (&acc)[NB][2]) {
+  constexpr int kBuffer = A::kBytes + B::kBytes, kStep = tile_step<T>(), kAsked = A::kPer + B::kPer;
+  int64_t k0 = 0, K = segments[0].K;
+  int left = (int)((K + kStep - 1) / kStep + (SEGMENTS > 1 ? (segments[SEGMENTS - 1].K + kStep - 1) / kStep : 0));
+  int to = 0, from = 0;
+  bool direct = false;  // how the step asked for last comes
+  auto after = [&](int buffer) { return buffer == 2 * kBuffer ? 0 : buffer + kBuffer; };
+  auto ask_direct = [&] {
+    first.direct(lds + to);
+    second.direct(lds + to + A::kBytes);
+    to = after(to);
+    k0 += kStep;
+    --left;
+  };
+  auto ask = [&] {
+    if (SEGMENTS > 1 && k0 >= K) {
+      begin(1);
+      k0 = 0;
+      K = segments[SEGMENTS - 1].K;
+    }
+    direct = k0 + kStep <= K;
+    if (direct) {
+      ask_direct();
+    } else {
+      first.ragged(k0, K);
+      second.ragged(k0, K);
+      first.put(lds + to);
+      second.put(lds + to + A::kBytes);
+      to = after(to);
+      k0 += kStep;
+      --left;
+    }
+  };
+  auto multiply = [&] {
+    __builtin_amdgcn_sched_barrier(0);
+    tile_multiply<T, NB, A, B>(lds + from, acc);
+    __builtin_amdgcn_sched_barrier(0);
+    from = after(from);
+  };
+  auto sync = [&] {
+    if (direct) tile_sync<kAsked>();
+    else tile_sync<0>();
+  };
+  begin(0);
+  const int steps = left;
+  ask();
+  if (left > 0) ask();
+#pragma unroll 1
+  while (left > 0) {
+    if (direct) {
+#pragma unroll 1
+      while (k0 + kStep <= K) {
+        tile_sync<kAsked>();
+        ask_direct();
+        multiply();
+      }
+    }
+    if (left == 0) break;
+    sync();
+    ask();
+    multiply();
+  }
+  if (steps > 1) {
+    sync();
+    multiply();
+  }
+  tile_sync<0>();
+  multiply();
   __syncthreads();
 }
 
