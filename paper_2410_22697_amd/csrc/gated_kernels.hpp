@@ -131,9 +131,9 @@ constexpr int kGateWays = kGateNT / kGateUnits;
 template <typename T>
 struct GatedDz {
   const T *dy, *pre;
-  T* dz;         // [rows][2 n]
+  T* dz;         // [rows][2 n], or null
   float* parts;  // [parts][2 n] of db, or null
-  int64_t rows, part, dy_stride, pre_stride, dz_stride;
+  int64_t rows, part, dy_stride, pre_stride;
   int n, act, groups;
 };
 
@@ -173,8 +173,9 @@ __global__ __launch_bounds__(kGateNT) void k_gated_dz(GatedDz<T> a) {
             sums[1][q] += du[q];
           }
         }
-        store_cols<T, kV, false>(a.dz + i * a.dz_stride + c, valid, dg);
-        store_cols<T, kV, false>(a.dz + i * a.dz_stride + a.n + c, valid, du);
+        if (!a.dz) continue;
+        store_cols<T, kV, false>(a.dz + i * (2 * (int64_t)a.n) + c, valid, dg);
+        store_cols<T, kV, false>(a.dz + i * (2 * (int64_t)a.n) + a.n + c, valid, du);
       }
     }
   });
@@ -248,6 +249,41 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tile
   }
 }
 
+// A block's part of dw: row(p) is the output at position p of its 128 (a.n: none).
+template <typename T, int NB, typename F>
+__device__ __forceinline__ void dw_out(const LinearDw<T>& a, char* lds, const f32x16 (&acc)[NB][2], int64_t part, int k0, F row_at) {
+  constexpr int kV = 16 / sizeof(T);
+  typedef TileTurn<float, 32 * NB> Turn;
+  const int wave = wave_uniform((int32_t)wave_id());
+  const Turn turn = {lds + wave * Turn::kBytes};
+  const int all = a.k[0] + a.k[1], c0 = k0 + wave % 2 * (32 * NB);
+  float* dw = a.dw + part * a.n * (int64_t)all;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        turn.in(32 * i, q, v);
+      }
+    turn.units([&](int r, int c, cols_t<float, 4> v) {
+      const int at = c0 + c, s = at >= a.second ? 1 : 0, c1 = at - (s ? a.second : 0), columns = s ? a.k[1] : a.k[0];
+      const int row = row_at(wave / 2 * 64 + 32 * j + r);
+      if (row >= a.n || c1 >= round_up_to<kV>(columns)) return;
+      const int col = tile_column<T>(c1, columns);
+      float* p = dw + (int64_t)row * all + (s ? a.k[0] : 0) + col;
+      if (col + 4 <= columns) {
+        *reinterpret_cast<cols_t<float, 4>*>(p) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + e < columns) p[e] = v[e];
+      }
+    });
+  }
+}
+
 // dw = dz^T [x | x2], one part of the rows a block: 128 outputs by 64 NB columns.
 // Columns are placed in whole units, the second input's from `second` on.
 template <typename T, int NB, bool DIRECT>
@@ -284,41 +320,153 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(LinearDw<T> a, int64_t 
   };
   if constexpr (DIRECT) tile_product_direct<T, NB>(xs, dzs, segments, begin, lds, acc);
   else tile_product<T, NB>(xs, dzs, segments, begin, lds, acc);
-  const int wave = wave_uniform((int32_t)wave_id());
-  const Turn turn = {lds + wave * Turn::kBytes};
-  const int all = a.k[0] + a.k[1], c0 = k0 + wave % 2 * (32 * NB);
-  float* dw = a.dw + part * a.n * (int64_t)all;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        turn.in(32 * i, q, v);
-      }
-    const int out = n0 + wave / 2 * 64 + 32 * j;
-    turn.units([&](int r, int c, cols_t<float, 4> v) {
-      const int at = c0 + c, s = at >= a.second ? 1 : 0, c1 = at - (s ? a.second : 0), columns = s ? a.k[1] : a.k[0];
-      if (out + r >= round_up_to<kV>(a.n) || c1 >= round_up_to<kV>(columns)) return;
-      const int row = tile_column<T>(out + r, a.n), col = tile_column<T>(c1, columns);
-      if (row >= a.n) return;
-      float* p = dw + (int64_t)row * all + (s ? a.k[0] : 0) + col;
-      if (col + 4 <= columns) {
-        *reinterpret_cast<cols_t<float, 4>*>(p) = v;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (col + e < columns) p[e] = v[e];
-      }
-    });
-  }
+  const int kLast = round_up_to<kV>(a.n);
+  dw_out<T, NB>(a, lds, acc, part, k0, [&](int p) { return n0 + p < kLast ? tile_column<T>(n0 + p, a.n) : a.n; });
 }
 
-// Adds the parts of dw, four values a thread.
+// [dg | du] as an operand across k, made from dy and pre on its way to LDS: 64
+// columns of dg and the same of du, a unit of both a thread and step. It can
+// leave dz behind, and each thread adds up its columns before they are rounded.
 template <typename T>
-__global__ __launch_bounds__(kGateNT) void k_gated_join(const float* __restrict__ parts, int64_t count, int64_t values, int cols, T* __restrict__ dw, int64_t stride) {
-  const int64_t i = ((int64_t)blockIdx.x * kGateNT + threadIdx.x) * 4;
+struct TileGates {
+  static constexpr int kV = 16 / sizeof(T), kUnits = 64 / kV, kPitch = 128 * sizeof(T), kBytes = tile_step<T>() * kPitch;
+  static_assert(kTileNT / kUnits == tile_step<T>(), "");
+  const T *dy, *pre;
+  T* dz;
+  int64_t dy_stride, pre_stride;
+  int n, act;
+  bool live;  // whether the step has the thread's row
+  int64_t at; // of the step after: that row, times dz's stride
+  u32x4 vd, vg, vu;
+  float sums[2][kV] = {};
+
+  static __device__ __forceinline__ u32x4 read(const T* p) { return __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(p)); }
+  // rows from `row` on, columns from n0 on (as TileAcross has them)
+  __device__ __forceinline__ void begin(const GatedDz<T>& a, int64_t row, int n0) {
+    const int c = min(n0 + (int)threadIdx.x % kUnits * kV, a.n - kV);
+    row += threadIdx.x / kUnits;
+    n = a.n;
+    act = a.act;
+    dy_stride = a.dy_stride;
+    pre_stride = a.pre_stride;
+    dy = a.dy + row * dy_stride + c;
+    pre = a.pre + row * pre_stride + c;
+    dz = a.dz ? a.dz + row * (2 * (int64_t)n) + c : nullptr;
+    at = 0;
+  }
+  __device__ __forceinline__ void ask(int64_t ahead) {
+    vd = read(dy + ahead * dy_stride);
+    vg = read(pre + ahead * pre_stride);
+    vu = read(pre + ahead * pre_stride + n);
+    at = ahead;
+  }
+  __device__ __forceinline__ void go_on() {
+    dy += tile_step<T>() * dy_stride;
+    pre += tile_step<T>() * pre_stride;
+  }
+  __device__ __forceinline__ void whole() {
+    live = true;
+    ask(0);
+    go_on();
+  }
+  __device__ __forceinline__ void ragged(int64_t k0, int64_t K) {
+    const int r = threadIdx.x / kUnits, in = r % kV;
+    const int64_t unit = k0 + (r - in);
+    const int skip = K >= kV ? skipped<T>(unit, K) : (unit + in < K ? 0 : kV);
+    live = in >= skip;
+    vd = vg = vu = (u32x4)0u;
+    if (live) ask(skip && K >= kV ? K - kV - unit : 0);
+    go_on();
+  }
+  __device__ __forceinline__ void put(char* to) {
+    typedef cols_t<T, kV> unit_t;
+    const unit_t d = __builtin_bit_cast(unit_t, vd), g = __builtin_bit_cast(unit_t, vg), u = __builtin_bit_cast(unit_t, vu);
+    unit_t z[2];
+    with_act(act, [&](auto of) {
+#pragma unroll
+      for (int q = 0; q < kV; ++q) {
+        const float dy_u = (float)d[q] * (float)u[q];
+        const float dg = of() == kActNone ? dy_u : act_grad(dy_u, (float)g[q], of()), du = (float)d[q] * act_value((float)g[q], of());
+        sums[0][q] += dg;  // (of zeros where the step has no row)
+        sums[1][q] += du;
+        z[0][q] = (T)dg;
+        z[1][q] = (T)du;
+      }
+    });
+    const int r = threadIdx.x / kUnits, s = threadIdx.x % kUnits;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int place = h * kUnits + s;
+      *reinterpret_cast<unit_t*>(to + r * kPitch + ((place / 2 ^ r % 4) * 2 + place % 2) * 16) = z[h];
+      if (dz && live) *reinterpret_cast<unit_t*>(dz + at * (2 * (int64_t)n) + h * n) = z[h];
+    }
+    if (dz) dz += tile_step<T>() * (2 * (int64_t)n);
+  }
+  static __device__ __forceinline__ u32x4 fragment(const char* from, int c0, int s) { return TileAcross<T, 128>::fragment(from, c0, s); }
+};
+
+// dw and the sums for db, of dz as TileGates makes it: one launch that reads dy
+// and pre once, for inputs of whole units in one tile of columns.
+template <typename T, int NB>
+__global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(LinearDw<T> a, GatedDz<T> z, int64_t blocks) {
+  typedef TileAcross<T, 64 * NB> A;
+  typedef TileGates<T> B;
+  typedef TileTurn<float, 32 * NB> Turn;
+  constexpr int kV = 16 / sizeof(T);
+  constexpr int kLds = 3 * (A::kBytes + B::kBytes);
+  static_assert(kLds >= 4 * Turn::kBytes && kLds >= tile_step<T>() * 128 * (int)sizeof(float), "");
+  __shared__ __align__(16) char lds[kLds];
+  const int64_t tile = tile_of_block(blockIdx.x, blocks);
+  const int64_t part = tile / a.tiles_n;
+  const int n0 = (int)(tile % a.tiles_n) * 64;
+  const int64_t from = part * a.part, rows = min(a.part, a.rows - from);
+  A xs;
+  B dzs;
+  f32x16 acc[NB][2] = {};
+  xs.begin([&](int c, int& at, int& columns, int64_t& stride) {
+    const int s = c >= a.second && a.k[1] > 0 ? 1 : 0;
+    at = c - (s ? a.second : 0);
+    columns = s ? a.k[1] : a.k[0];
+    stride = s ? a.x[1].stride : a.x[0].stride;
+    return (s ? a.x[1].p : a.x[0].p) + from * stride;
+  });
+  dzs.begin(z, from, n0);
+  tile_product_made<T, NB>(xs, dzs, rows, lds, acc);
+  const int last = round_up_to<kV>(z.n);
+  auto row_at = [&](int p) {
+    const int c = n0 + p % 64;
+    return c < last ? p / 64 * z.n + tile_column<T>(c, z.n) : a.n;
+  };
+  if (a.dbias) {
+    // the threads that share columns add up in order
+    float* joined = reinterpret_cast<float*>(lds);
+    const int r = threadIdx.x / B::kUnits, c = threadIdx.x % B::kUnits * kV;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < kV; ++q) joined[r * 128 + h * 64 + c + q] = dzs.sums[h][q];
+    __syncthreads();
+    const int row = (int)threadIdx.x < 128 ? row_at(threadIdx.x) : a.n;
+    if (row < a.n) {
+      float t = 0.0f;
+#pragma unroll
+      for (int g = 0; g < tile_step<T>(); ++g) t += joined[g * 128 + threadIdx.x];
+      a.dbias[part * a.n + row] = t;
+    }
+    __syncthreads();
+  }
+  dw_out<T, NB>(a, lds, acc, part, 0, row_at);
+}
+
+// Adds the parts of dw (rows of `cols`) and then those of db, four values a
+// thread.
+template <typename T>
+__global__ __launch_bounds__(kGateNT) void k_gated_join(const float* __restrict__ dw_parts, const float* __restrict__ db_parts, int64_t count, int64_t dw_values, int n,
+                                                        int cols, T* __restrict__ dw, int64_t stride, T* __restrict__ db) {
+  const int64_t dw_blocks = (dw_values + 4 * kGateNT - 1) / (4 * kGateNT);
+  const bool bias = blockIdx.x >= dw_blocks;
+  const float* parts = bias ? db_parts : dw_parts;
+  const int64_t values = bias ? n : dw_values, i = ((int64_t)(blockIdx.x - (bias ? dw_blocks : 0)) * kGateNT + threadIdx.x) * 4;
   if (i >= values) return;
   const int valid = (int)min(values - i, (int64_t)4);
   float sum[4] = {};
@@ -331,7 +479,10 @@ __global__ __launch_bounds__(kGateNT) void k_gated_join(const float* __restrict_
   }
 #pragma unroll
   for (int q = 0; q < 4; ++q)
-    if (q < valid) dw[(i + q) / cols * stride + (i + q) % cols] = (T)sum[q];
+    if (q < valid) {
+      if (bias) db[i + q] = (T)sum[q];
+      else dw[(i + q) / cols * stride + (i + q) % cols] = (T)sum[q];
+    }
 }
 
 }  // namespace ms

@@ -200,31 +200,34 @@ int gated(const massive_gated_args* a, void* stream) {
   return launch(what, k_gated_few<T>, cdiv(a->rows, 32) * tiles_n, kFewNT, 0, stream, f, tiles_n);
 }
 
-// Parts of dw's rows: as many blocks as the chip holds twice over, none of less
-// than eight steps of rows where there are more.
+// dw's tiles and the parts of its rows: as many blocks as the chip holds at a
+// time, none of less than eight steps of rows where there are more. `made`: dz
+// is made on its way into the product, 64 outputs of both halves a tile.
 struct GatedDwPlan {
   int nb, second;
-  int64_t tiles_n, tiles_k, part, parts, floats;
+  int64_t tiles_n, tiles_k, part, parts, floats, sums;
 };
-GatedDwPlan gated_dw_plan(const massive_gated_grads* a) {
+GatedDwPlan gated_dw_plan(const massive_gated_grads* a, bool made) {
   GatedDwPlan p;
   const int vector = 16 / size_of(a->type), step = kTileStepBytes / size_of(a->type);
   p.second = (int)round_up(a->k, vector);
   const int64_t cols = p.second + a->k_second, n = 2 * (int64_t)a->n;
   p.nb = cols <= 128 ? 2 : 4;
-  p.tiles_n = cdiv(n, kTileSecond);
+  p.tiles_n = made ? cdiv(a->n, 64) : cdiv(n, kTileSecond);
   p.tiles_k = cdiv(cols, 64 * p.nb);
   const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 8 * step));
   p.part = std::max<int64_t>(1, round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, 512 / (p.tiles_n * p.tiles_k)))), step));
   p.parts = cdiv(a->rows, p.part);
   p.floats = a->dw ? p.parts * n * ((int64_t)a->k + a->k_second) : 0;
+  p.sums = made && a->dbias ? p.parts * n : 0;
   return p;
 }
 
-// The backward pass's workspace: dz, the parts of db, those of dw.
+// The backward pass's workspace: dz, the parts of db, those of dw. It has room
+// for both ways to dw, of which the arrays' alignment chooses one.
 struct GatedPlan {
   int64_t groups, part, parts, sums_at, dw_at, bytes;
-  GatedDwPlan dw;
+  GatedDwPlan dw, made;
 };
 GatedPlan gated_plan(const massive_gated_grads* a) {
   GatedPlan p;
@@ -232,82 +235,107 @@ GatedPlan gated_plan(const massive_gated_grads* a) {
   p.groups = cdiv(a->n, kGateUnits * (16 / size));
   p.part = std::max<int64_t>(1, cdiv(a->rows, std::max<int64_t>(1, std::min(cdiv(a->rows, 4 * kGateWays), 2048 / std::min<int64_t>(2048, p.groups)))));
   p.parts = cdiv(a->rows, p.part);
-  p.dw = gated_dw_plan(a);
-  p.sums_at = round_up(a->rows * 2 * a->n * size, 16);
-  p.dw_at = p.sums_at + (a->dbias ? round_up(p.parts * 2 * a->n * 4, 16) : 0);
-  p.bytes = p.dw_at + p.dw.floats * 4;
+  p.dw = gated_dw_plan(a, false);
+  p.made = gated_dw_plan(a, true);
+  p.sums_at = a->dx || a->dx_second || a->dw ? round_up(a->rows * 2 * a->n * size, 16) : 0;
+  p.dw_at = p.sums_at + (a->dbias ? round_up(std::max(p.parts * 2 * a->n, p.made.sums) * 4, 16) : 0);
+  p.bytes = p.dw_at + std::max(p.dw.floats, p.made.floats) * 4;
   return p;
 }
 
 template <typename T>
-int gated_dz(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
-  GatedDz<T> f;
+GatedDz<T> gates_of(const massive_gated_grads* a, char* dz) {
+  GatedDz<T> f = {};
   f.dy = (const T*)a->dy;
   f.pre = (const T*)a->pre;
-  f.dz = (T*)workspace;
-  f.parts = a->dbias ? (float*)(workspace + p.sums_at) : nullptr;
+  f.dz = (T*)dz;
   f.rows = a->rows;
-  f.part = p.part;
   f.dy_stride = a->dy_stride;
   f.pre_stride = a->pre_stride;
-  f.dz_stride = 2 * (int64_t)a->n;
   f.n = a->n;
   f.act = a->act;
-  f.groups = (int)p.groups;
+  return f;
+}
+
+// The launch that adds up the parts of dw and of db, each if there are any.
+template <typename T>
+int gated_join(const massive_gated_grads* a, const float* dw, const float* db, int64_t parts, void* stream) {
+  const int cols = a->k + a->k_second, n = 2 * a->n;
+  const int64_t values = dw ? (int64_t)n * cols : 0, blocks = cdiv(values, 4 * kGateNT) + (db ? cdiv(n, 4 * kGateNT) : 0);
+  return launch("massive_gated_backward", k_gated_join<T>, blocks, kGateNT, 0, stream, dw, db, parts, values, n, cols, (T*)a->dw, a->dw_stride, (T*)a->dbias);
+}
+
+// dz and db by themselves.
+template <typename T>
+int gated_dz(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
   const char* what = "massive_gated_backward";
+  GatedDz<T> f = gates_of<T>(a, a->dx || a->dx_second || a->dw ? workspace : nullptr);
+  f.parts = a->dbias ? (float*)(workspace + p.sums_at) : nullptr;
+  f.part = p.part;
+  f.groups = (int)p.groups;
   if (int rc = launch(what, k_gated_dz<T>, p.groups * p.parts, kGateNT, 0, stream, f)) return rc;
   if (!a->dbias) return MASSIVE_OK;
   return launch(what, k_rms_norm_join<T>, cdiv(2 * a->n, kNormNT / kNormJoinWays), kNormNT, 0, stream, (const float*)f.parts, p.parts, 2 * a->n, (T*)a->dbias);
 }
 
 template <typename T>
-int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
-  const char* what = "massive_gated_backward";
-  if (int rc = gated_dz<T>(a, p, workspace, stream)) return rc;
+int gated_dx(const massive_gated_grads* a, char* workspace, void* stream) {
   constexpr int kV = 16 / sizeof(T);
   const int n = 2 * a->n;
-  const Operand<T> dz = rows_of<T>(workspace, n, a->rows, n);
-  if (a->dx || a->dx_second) {
-    LinearDx<T> f;
-    f.dz = dz;
-    const int k0 = a->dx ? a->k : 0, k1 = a->dx_second ? a->k_second : 0;
-    f.w = {(const T*)a->w + (a->dx ? 0 : a->k), a->w_stride};
-    f.dx[0] = (T*)a->dx;
-    f.dx[1] = (T*)a->dx_second;
-    f.dx_stride[0] = a->dx_stride;
-    f.dx_stride[1] = a->dx_second_stride;
-    f.rows = a->rows;
-    f.cols = k0 + k1;
-    f.split = k0;
-    const bool direct = n % kV == 0 && in_units<T>(f.w.p, f.w.stride) && f.cols % kV == 0;
-    auto tile = [&](auto nb) {
-      const int64_t tiles_n = cdiv(f.cols, 64 * nb()), blocks = cdiv(a->rows, kTileSecond) * tiles_n;
-      return launch(what, direct ? k_gated_dx<T, nb(), true> : k_gated_dx<T, nb(), false>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
-    };
-    if (int rc = f.cols <= 128 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
-  }
-  if (!a->dw) return MASSIVE_OK;
-  LinearDw<T> f;
-  f.dz = dz;
-  f.x[0] = rows_of<T>(a->x, a->x_stride, a->rows, a->k);
-  f.x[1] = rows_of<T>(a->x_second, a->x_second_stride, a->rows, a->k_second);
-  f.dw = (float*)(workspace + p.dw_at);
-  f.dbias = nullptr;
+  LinearDx<T> f;
+  f.dz = rows_of<T>(workspace, n, a->rows, n);
+  const int k0 = a->dx ? a->k : 0, k1 = a->dx_second ? a->k_second : 0;
+  f.w = {(const T*)a->w + (a->dx ? 0 : a->k), a->w_stride};
+  f.dx[0] = (T*)a->dx;
+  f.dx[1] = (T*)a->dx_second;
+  f.dx_stride[0] = a->dx_stride;
+  f.dx_stride[1] = a->dx_second_stride;
   f.rows = a->rows;
-  f.part = p.dw.part;
-  f.n = n;
-  f.k[0] = a->k;
-  f.k[1] = a->k_second;
-  f.second = p.dw.second;
-  f.tiles_n = (int)p.dw.tiles_n;
-  f.tiles_k = (int)p.dw.tiles_k;
-  const int64_t blocks = p.dw.parts * p.dw.tiles_n * p.dw.tiles_k;
-  const bool direct = n % kV == 0 && a->k % kV == 0 && a->k_second % kV == 0 && in_units<T>(a->x, a->x_stride) && in_units<T>(a->x_second, a->x_second_stride);
-  auto tile = [&](auto nb) { return launch(what, direct ? k_gated_dw<T, nb(), true> : k_gated_dw<T, nb(), false>, blocks, kTileNT, 0, stream, f, blocks); };
-  if (int rc = p.dw.nb == 2 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
-  const int cols = a->k + a->k_second;
-  const int64_t values = (int64_t)n * cols;
-  return launch(what, k_gated_join<T>, cdiv(values, 4 * kGateNT), kGateNT, 0, stream, (const float*)f.dw, p.dw.parts, values, cols, (T*)a->dw, a->dw_stride);
+  f.cols = k0 + k1;
+  f.split = k0;
+  const bool direct = n % kV == 0 && in_units<T>(f.w.p, f.w.stride) && f.cols % kV == 0;
+  auto tile = [&](auto nb) {
+    const int64_t tiles_n = cdiv(f.cols, 64 * nb()), blocks = cdiv(a->rows, kTileSecond) * tiles_n;
+    return launch("massive_gated_backward", direct ? k_gated_dx<T, nb(), true> : k_gated_dx<T, nb(), false>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
+  };
+  return f.cols <= 128 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>());
+}
+
+template <typename T>
+int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
+  const char* what = "massive_gated_backward";
+  constexpr int kV = 16 / sizeof(T);
+  const bool dx = a->dx || a->dx_second;
+  const bool units = a->k % kV == 0 && a->k_second % kV == 0 && in_units<T>(a->x, a->x_stride) && in_units<T>(a->x_second, a->x_second_stride);
+  const bool made = a->dw && units && a->n >= kV && p.made.tiles_k == 1;
+  if (!made)
+    if (int rc = gated_dz<T>(a, p, workspace, stream)) return rc;
+  if (a->dw) {
+    const int n = 2 * a->n;
+    const GatedDwPlan& d = made ? p.made : p.dw;
+    LinearDw<T> f;
+    f.dz = rows_of<T>(workspace, n, a->rows, n);
+    f.x[0] = rows_of<T>(a->x, a->x_stride, a->rows, a->k);
+    f.x[1] = rows_of<T>(a->x_second, a->x_second_stride, a->rows, a->k_second);
+    f.dw = (float*)(workspace + p.dw_at);
+    f.dbias = made && a->dbias ? (float*)(workspace + p.sums_at) : nullptr;
+    f.rows = a->rows;
+    f.part = d.part;
+    f.n = n;
+    f.k[0] = a->k;
+    f.k[1] = a->k_second;
+    f.second = d.second;
+    f.tiles_n = (int)d.tiles_n;
+    f.tiles_k = (int)d.tiles_k;
+    const int64_t blocks = d.parts * d.tiles_n * d.tiles_k;
+    auto tile = [&](auto nb) {
+      if (made) return launch(what, k_gated_dw_made<T, nb()>, blocks, kTileNT, 0, stream, f, gates_of<T>(a, dx ? workspace : nullptr), blocks);
+      return launch(what, units && n % kV == 0 ? k_gated_dw<T, nb(), true> : k_gated_dw<T, nb(), false>, blocks, kTileNT, 0, stream, f, blocks);
+    };
+    if (int rc = d.nb == 2 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
+    if (int rc = gated_join<T>(a, f.dw, f.dbias, d.parts, stream)) return rc;
+  }
+  return dx ? gated_dx<T>(a, workspace, stream) : MASSIVE_OK;
 }
 
 }  // namespace
@@ -425,20 +453,15 @@ int massive_gated_backward(const massive_gated_grads* a, void* workspace, int64_
   for (const void* p : {a->dy, a->pre, a->x, a->x_second, a->w, (const void*)a->dx, (const void*)a->dx_second, (const void*)a->dw, (const void*)a->dbias})
     if (!aligned(p, size)) REFUSE("an array is not aligned");
   const GatedPlan p = gated_plan(a);
-  const int64_t values = a->dw ? 2 * a->n * k : 0;
-  if (p.groups * p.parts > kMostBlocks || p.dw.parts * p.dw.tiles_n * p.dw.tiles_k > kMostBlocks || cdiv(values, 4 * kGateNT) > kMostBlocks ||
+  const int64_t dw_blocks = std::max(p.dw.parts * p.dw.tiles_n * p.dw.tiles_k, p.made.parts * p.made.tiles_n * p.made.tiles_k);
+  if (p.groups * p.parts > kMostBlocks || (a->dw && (dw_blocks > kMostBlocks || cdiv(2 * a->n * k, 4 * kGateNT) + 1024 > kMostBlocks)) ||
       cdiv(a->rows, kTileSecond) * cdiv(k, 128) > kMostBlocks)
     REFUSE("too many rows and columns for one call");
   if (a->rows == 0) {  // sums over no rows
-    const char* what = "massive_gated_backward";
-    return with_type(a->type, [&](auto* t) {
-      using T = std::remove_pointer_t<decltype(t)>;
-      if (a->dw)
-        if (int rc = launch(what, k_gated_join<T>, cdiv(values, 4 * kGateNT), kGateNT, 0, stream, (const float*)nullptr, int64_t(0), values, (int)k, (T*)a->dw, a->dw_stride))
-          return rc;
-      if (!a->dbias) return MASSIVE_OK;
-      return launch(what, k_rms_norm_join<T>, cdiv(2 * a->n, kNormNT / kNormJoinWays), kNormNT, 0, stream, (const float*)nullptr, int64_t(0), 2 * a->n, (T*)a->dbias);
-    });
+    if (!a->dw && !a->dbias) return MASSIVE_OK;
+    // the pointers only say which of the two are asked for: with no parts nothing is read
+    const float *dw = (const float*)a->dw, *db = (const float*)a->dbias;
+    return a->type == MASSIVE_F32 ? gated_join<float>(a, dw, db, 0, stream) : gated_join<bf16>(a, dw, db, 0, stream);
   }
   if (!workspace || workspace_bytes < p.bytes)
     return call_error(MASSIVE_ECAPACITY, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)p.bytes);

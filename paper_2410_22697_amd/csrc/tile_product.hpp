@@ -45,7 +45,7 @@ __device__ __forceinline__ void tile_direct(const void* from, char* to) {
 
 // Four rows' 16-bit values of a column, for 16 lanes: their own 4 columns of 16,
 // row by row. (The qualifier is what tells the compiler that the read need not
-// wait for what direct() has on its way; tile_sync() has waited for what counts.)
+// wait for what direct() has on its way; tile_arrived() has waited for what counts.)
 __device__ __forceinline__ uint2 tile_turned(const char* __restrict__ p) {
   typedef short short4v __attribute__((ext_vector_type(4)));
   typedef __attribute__((address_space(3))) short4v* lds_ptr;
@@ -290,13 +290,21 @@ __device__ __forceinline__ void tile_product(A& first, B& second, const TileSegm
   __syncthreads();
 }
 
-// Waits until this wave's memory reads but the last LEFT have arrived, and its
-// LDS accesses, and then for the block's other waves to come here.
+// Waits until this wave's memory reads but the last LEFT have arrived.
 template <int LEFT>
-__device__ __forceinline__ void tile_sync() {
+__device__ __forceinline__ void tile_arrived() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4);
+  __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4 | 15 << 8);
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+// Waits until this wave's LDS accesses are done, and for the block's other waves
+// to come here.
+__device__ __forceinline__ void tile_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("" ::: "memory");
@@ -348,8 +356,9 @@ __device__ __forceinline__ void tile_product_direct(A& first, B& second, const T
     from = after(from);
   };
   auto sync = [&] {
-    if (direct) tile_sync<kAsked>();
-    else tile_sync<0>();
+    if (direct) tile_arrived<kAsked>();
+    else tile_arrived<0>();
+    tile_barrier();
   };
   begin(0);
   const int steps = left;
@@ -360,7 +369,8 @@ __device__ __forceinline__ void tile_product_direct(A& first, B& second, const T
     if (direct) {
 #pragma unroll 1
       while (k0 + kStep <= K) {
-        tile_sync<kAsked>();
+        tile_arrived<kAsked>();
+        tile_barrier();
         ask_direct();
         multiply();
       }
@@ -374,8 +384,53 @@ __device__ __forceinline__ void tile_product_direct(A& first, B& second, const T
     sync();
     multiply();
   }
-  tile_sync<0>();
+  tile_arrived<0>();
+  tile_barrier();
   multiply();
+  __syncthreads();
+}
+
+// The same for a second operand that the threads compute as they put it: the
+// first's steps come directly, one of them two ahead, and the second's through
+// registers. A thread puts its part of a step once all that it asked for has
+// arrived, which is also the first's part of that step; the barrier after that
+// makes both the block's.
+template <typename T, int NB, typename A, typename B>
+__device__ __forceinline__ void tile_product_made(A& first, B& second, int64_t K, char* lds, f32x16 (&acc)[NB][2]) {
+  constexpr int kBuffer = A::kBytes + B::kBytes, kStep = tile_step<T>();
+  const int steps = (int)((K + kStep - 1) / kStep);
+  int to = 0, from = 0, next = 0;  // buffers: asked for next, multiplied next, put next
+  int64_t k0 = 0;
+  auto after = [&](int buffer) { return buffer == 2 * kBuffer ? 0 : buffer + kBuffer; };
+  auto ask = [&] {
+    if (k0 + kStep <= K) {
+      first.direct(lds + to);
+      second.whole();
+    } else {
+      first.ragged(k0, K);
+      first.put(lds + to);
+      second.ragged(k0, K);
+    }
+    to = after(to);
+    k0 += kStep;
+  };
+  auto put = [&] {
+    tile_arrived<0>();
+    second.put(lds + next + A::kBytes);
+    next = after(next);
+  };
+  ask();
+  put();
+  if (steps > 1) ask();
+#pragma unroll 1
+  for (int s = 0; s < steps; ++s) {
+    tile_barrier();
+    if (s + 1 < steps) put();
+    if (s + 2 < steps) ask();
+    __builtin_amdgcn_sched_barrier(0);
+    tile_multiply<T, NB, A, B>(lds + from, acc);
+    from = after(from);
+  }
   __syncthreads();
 }
 
