@@ -327,17 +327,20 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(LinearDw<T> a, int64_t 
 // [dg | du] as an operand across k, made from dy and pre on its way to LDS: 64
 // columns of dg and the same of du, a unit of both a thread and step. It can
 // leave dz behind, and each thread adds up its columns before they are rounded.
-template <typename T>
+template <typename T, int ACT>
 struct TileGates {
   static constexpr int kV = 16 / sizeof(T), kUnits = 64 / kV, kPitch = 128 * sizeof(T), kBytes = tile_step<T>() * kPitch;
   static_assert(kTileNT / kUnits == tile_step<T>(), "");
   const T *dy, *pre;
   T* dz;
   int64_t dy_stride, pre_stride;
-  int n, act;
-  bool live;  // whether the step has the thread's row
-  int64_t at; // of the step after: that row, times dz's stride
-  u32x4 vd, vg, vu;
+  int n;
+  // two sets of what a thread has asked for: units of dy and of both halves, whether the step has the thread's row, and
+  // how far that lies from the place that the step has for it
+  static constexpr int kAsked = 3;
+  bool live[2];
+  int64_t at[2];
+  u32x4 vd[2], vg[2], vu[2];
   float sums[2][kV] = {};
 
   static __device__ __forceinline__ u32x4 read(const T* p) { return __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(p)); }
@@ -346,75 +349,82 @@ struct TileGates {
     const int c = min(n0 + (int)threadIdx.x % kUnits * kV, a.n - kV);
     row += threadIdx.x / kUnits;
     n = a.n;
-    act = a.act;
     dy_stride = a.dy_stride;
     pre_stride = a.pre_stride;
     dy = a.dy + row * dy_stride + c;
     pre = a.pre + row * pre_stride + c;
     dz = a.dz ? a.dz + row * (2 * (int64_t)n) + c : nullptr;
-    at = 0;
   }
+  template <int SET>
   __device__ __forceinline__ void ask(int64_t ahead) {
-    vd = read(dy + ahead * dy_stride);
-    vg = read(pre + ahead * pre_stride);
-    vu = read(pre + ahead * pre_stride + n);
-    at = ahead;
+    vd[SET] = read(dy + ahead * dy_stride);
+    vg[SET] = read(pre + ahead * pre_stride);
+    vu[SET] = read(pre + ahead * pre_stride + n);
+    at[SET] = ahead;
   }
   __device__ __forceinline__ void go_on() {
     dy += tile_step<T>() * dy_stride;
     pre += tile_step<T>() * pre_stride;
   }
+  template <int SET>
   __device__ __forceinline__ void whole() {
-    live = true;
-    ask(0);
+    live[SET] = true;
+    ask<SET>(0);
     go_on();
   }
+  template <int SET>
   __device__ __forceinline__ void ragged(int64_t k0, int64_t K) {
     const int r = threadIdx.x / kUnits, in = r % kV;
     const int64_t unit = k0 + (r - in);
     const int skip = K >= kV ? skipped<T>(unit, K) : (unit + in < K ? 0 : kV);
-    live = in >= skip;
-    vd = vg = vu = (u32x4)0u;
-    if (live) ask(skip && K >= kV ? K - kV - unit : 0);
+    live[SET] = in >= skip;
+    vd[SET] = vg[SET] = vu[SET] = (u32x4)0u;
+    if (live[SET]) ask<SET>(skip && K >= kV ? K - kV - unit : 0);
     go_on();
   }
+  // WHOLE: the step has all rows
+  template <int SET, bool WHOLE>
   __device__ __forceinline__ void put(char* to) {
     typedef cols_t<T, kV> unit_t;
-    const unit_t d = __builtin_bit_cast(unit_t, vd), g = __builtin_bit_cast(unit_t, vg), u = __builtin_bit_cast(unit_t, vu);
+    const unit_t d = __builtin_bit_cast(unit_t, vd[SET]), g = __builtin_bit_cast(unit_t, vg[SET]), u = __builtin_bit_cast(unit_t, vu[SET]);
     unit_t z[2];
-    with_act(act, [&](auto of) {
 #pragma unroll
-      for (int q = 0; q < kV; ++q) {
-        const float dy_u = (float)d[q] * (float)u[q];
-        const float dg = of() == kActNone ? dy_u : act_grad(dy_u, (float)g[q], of()), du = (float)d[q] * act_value((float)g[q], of());
-        sums[0][q] += dg;  // (of zeros where the step has no row)
-        sums[1][q] += du;
-        z[0][q] = (T)dg;
-        z[1][q] = (T)du;
-      }
-    });
+    for (int q = 0; q < kV; ++q) {
+      const float dy_u = (float)d[q] * (float)u[q];
+      const float dg = ACT == kActNone ? dy_u : act_grad(dy_u, (float)g[q], ACT), du = (float)d[q] * act_value((float)g[q], ACT);
+      sums[0][q] += dg;  // (of zeros where the step has no row)
+      sums[1][q] += du;
+      z[0][q] = (T)dg;
+      z[1][q] = (T)du;
+    }
     const int r = threadIdx.x / kUnits, s = threadIdx.x % kUnits;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int place = h * kUnits + s;
-      *reinterpret_cast<unit_t*>(to + r * kPitch + ((place / 2 ^ r % 4) * 2 + place % 2) * 16) = z[h];
-      if (dz && live) *reinterpret_cast<unit_t*>(dz + at * (2 * (int64_t)n) + h * n) = z[h];
+      *reinterpret_cast<u32x4*>(to + r * kPitch + ((place / 2 ^ r % 4) * 2 + place % 2) * 16) = __builtin_bit_cast(u32x4, z[h]);
     }
-    if (dz) dz += tile_step<T>() * (2 * (int64_t)n);
+    if (dz) {
+      if (WHOLE || live[SET]) {
+        T* p = WHOLE ? dz : dz + at[SET] * (2 * (int64_t)n);
+        *reinterpret_cast<unit_t*>(p) = z[0];
+        *reinterpret_cast<unit_t*>(p + n) = z[1];
+      }
+      dz += tile_step<T>() * (2 * (int64_t)n);
+    }
   }
   static __device__ __forceinline__ u32x4 fragment(const char* from, int c0, int s) { return TileAcross<T, 128>::fragment(from, c0, s); }
 };
 
 // dw and the sums for db, of dz as TileGates makes it: one launch that reads dy
 // and pre once, for inputs of whole units in one tile of columns.
-template <typename T, int NB>
+template <typename T, int NB, int ACT>
 __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(LinearDw<T> a, GatedDz<T> z, int64_t blocks) {
   typedef TileAcross<T, 64 * NB> A;
-  typedef TileGates<T> B;
+  typedef TileGates<T, ACT> B;
   typedef TileTurn<float, 32 * NB> Turn;
   constexpr int kV = 16 / sizeof(T);
-  constexpr int kLds = 3 * (A::kBytes + B::kBytes);
-  static_assert(kLds >= 4 * Turn::kBytes && kLds >= tile_step<T>() * 128 * (int)sizeof(float), "");
+  constexpr int kMade = tile_made_lds<T, NB, A, B>(), kLds = kMade > 4 * Turn::kBytes ? kMade : 4 * Turn::kBytes;
+  static_assert(kLds >= tile_step<T>() * 128 * (int)sizeof(float), "");
   __shared__ __align__(16) char lds[kLds];
   const int64_t tile = tile_of_block(blockIdx.x, blocks);
   const int64_t part = tile / a.tiles_n;

@@ -257,6 +257,16 @@ GatedDz<T> gates_of(const massive_gated_grads* a, char* dz) {
   return f;
 }
 
+template <typename F>
+int with_act_of(int act, F f) {
+  switch (act) {
+    case MASSIVE_ACT_RELU: return f(std::integral_constant<int, kActRelu>());
+    case MASSIVE_ACT_GELU: return f(std::integral_constant<int, kActGelu>());
+    case MASSIVE_ACT_SILU: return f(std::integral_constant<int, kActSilu>());
+    default: return f(std::integral_constant<int, kActNone>());
+  }
+}
+
 // The launch that adds up the parts of dw and of db, each if there are any.
 template <typename T>
 int gated_join(const massive_gated_grads* a, const float* dw, const float* db, int64_t parts, void* stream) {
@@ -329,7 +339,10 @@ int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* works
     f.tiles_k = (int)d.tiles_k;
     const int64_t blocks = d.parts * d.tiles_n * d.tiles_k;
     auto tile = [&](auto nb) {
-      if (made) return launch(what, k_gated_dw_made<T, nb()>, blocks, kTileNT, 0, stream, f, gates_of<T>(a, dx ? workspace : nullptr), blocks);
+      if (made)
+        return with_act_of(a->act, [&](auto act) {
+          return launch(what, k_gated_dw_made<T, nb(), act()>, blocks, kTileNT, 0, stream, f, gates_of<T>(a, dx ? workspace : nullptr), blocks);
+        });
       return launch(what, units && n % kV == 0 ? k_gated_dw<T, nb(), true> : k_gated_dw<T, nb(), false>, blocks, kTileNT, 0, stream, f, blocks);
     };
     if (int rc = d.nb == 2 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;

@@ -208,17 +208,17 @@ struct TileSegment {
 };
 
 // acc[i][j] += the products of the first operand's columns wave % 2 * 32 NB + 32 i
-// on and the second's wave / 2 * 64 + 32 j on, in the step at `from`.
+// on and the second's wave / 2 * 64 + 32 j on, in the step that both have in LDS.
 template <typename T, int NB, typename A, typename B>
-__device__ __forceinline__ void tile_multiply(const char* from, f32x16 (&acc)[NB][2]) {
+__device__ __forceinline__ void tile_multiply(const char* first, const char* second, f32x16 (&acc)[NB][2]) {
   const int wave = wave_uniform((int32_t)wave_id());
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     u32x4 a[NB], b[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) b[j] = B::fragment(from + A::kBytes, wave / 2 * 64 + 32 * j, s);
+    for (int j = 0; j < 2; ++j) b[j] = B::fragment(second, wave / 2 * 64 + 32 * j, s);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) a[i] = A::fragment(from, wave % 2 * (32 * NB) + 32 * i, s);
+    for (int i = 0; i < NB; ++i) a[i] = A::fragment(first, wave % 2 * (32 * NB) + 32 * i, s);
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -248,7 +248,7 @@ __device__ __forceinline__ void tile_product(A& first, B& second, const TileSegm
   };
   auto step = [&] {
     __builtin_amdgcn_sched_barrier(0);  // the step's loads stay ahead of the products that they run beside, and its stores behind them
-    tile_multiply<T, NB, A, B>(lds + buffer, acc);
+    tile_multiply<T, NB, A, B>(lds + buffer, lds + buffer + A::kBytes, acc);
     __builtin_amdgcn_sched_barrier(0);
     buffer = kBuffer - buffer;
     put();
@@ -286,7 +286,7 @@ __device__ __forceinline__ void tile_product(A& first, B& second, const TileSegm
       step();
     }
   }
-  tile_multiply<T, NB, A, B>(lds + buffer, acc);
+  tile_multiply<T, NB, A, B>(lds + buffer, lds + buffer + A::kBytes, acc);
   __syncthreads();
 }
 
@@ -351,7 +351,7 @@ __device__ __forceinline__ void tile_product_direct(A& first, B& second, const T
   };
   auto multiply = [&] {
     __builtin_amdgcn_sched_barrier(0);
-    tile_multiply<T, NB, A, B>(lds + from, acc);
+    tile_multiply<T, NB, A, B>(lds + from, lds + from + A::kBytes, acc);
     __builtin_amdgcn_sched_barrier(0);
     from = after(from);
   };
@@ -390,46 +390,83 @@ __device__ __forceinline__ void tile_product_direct(A& first, B& second, const T
   __syncthreads();
 }
 
-// The same for a second operand that the threads compute as they put it: the
-// first's steps come directly, one of them two ahead, and the second's through
-// registers. A thread puts its part of a step once all that it asked for has
-// arrived, which is also the first's part of that step; the barrier after that
-// makes both the block's.
+// The same for a second operand that the threads compute as they put it. The
+// first's steps come directly, two ahead; the second's through registers, three
+// ahead, in two sets, and a thread puts its part of a step a step ahead. What a
+// wave asks for arrives in the order of asking, a step's part of the first
+// before the next but one's of the second: so much may be left when a step is
+// multiplied (kLeft) and when the next is put (kLeftPut).
+template <typename T, int NB, typename A, typename B>
+constexpr int tile_made_lds() {
+  return 3 * A::kBytes + 2 * B::kBytes;
+}
 template <typename T, int NB, typename A, typename B>
 __device__ __forceinline__ void tile_product_made(A& first, B& second, int64_t K, char* lds, f32x16 (&acc)[NB][2]) {
-  constexpr int kBuffer = A::kBytes + B::kBytes, kStep = tile_step<T>();
+  constexpr int kStep = tile_step<T>(), kLeftPut = A::kPer + B::kAsked, kLeft = B::kAsked + kLeftPut;
   const int steps = (int)((K + kStep - 1) / kStep);
-  int to = 0, from = 0, next = 0;  // buffers: asked for next, multiplied next, put next
-  int64_t k0 = 0;
-  auto after = [&](int buffer) { return buffer == 2 * kBuffer ? 0 : buffer + kBuffer; };
-  auto ask = [&] {
-    if (k0 + kStep <= K) {
+  const bool whole = K % kStep == 0;  // the last step too
+  int to = 0, from = 0;
+  auto after = [&](int buffer) { return buffer == 2 * A::kBytes ? 0 : buffer + A::kBytes; };
+  auto ask_first = [&](int s) {
+    if (s + 1 < steps || whole) {
       first.direct(lds + to);
-      second.whole();
     } else {
-      first.ragged(k0, K);
+      first.ragged((int64_t)s * kStep, K);
       first.put(lds + to);
-      second.ragged(k0, K);
     }
     to = after(to);
-    k0 += kStep;
   };
-  auto put = [&] {
-    tile_arrived<0>();
-    second.put(lds + next + A::kBytes);
-    next = after(next);
+  auto ask_second = [&](int s, auto set) {
+    if (s + 1 < steps || whole) second.template whole<set()>();
+    else second.template ragged<set()>((int64_t)s * kStep, K);
   };
-  ask();
-  put();
-  if (steps > 1) ask();
-#pragma unroll 1
-  for (int s = 0; s < steps; ++s) {
-    tile_barrier();
-    if (s + 1 < steps) put();
-    if (s + 2 < steps) ask();
+  auto put = [&](auto set, auto all) { second.template put<set(), all()>(lds + 3 * A::kBytes + set() * B::kBytes); };
+  auto multiply = [&](auto set) {
     __builtin_amdgcn_sched_barrier(0);
-    tile_multiply<T, NB, A, B>(lds + from, acc);
+    tile_multiply<T, NB, A, B>(lds + from, lds + 3 * A::kBytes + set() * B::kBytes, acc);
+    __builtin_amdgcn_sched_barrier(0);
     from = after(from);
+  };
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> odd;
+  auto step = [&](int s, auto now, auto next) {  // any step
+    tile_arrived<0>();
+    tile_barrier();
+    if (s + 1 < steps) put(next, std::false_type());
+    if (s + 2 < steps) ask_first(s + 2);
+    if (s + 3 < steps) ask_second(s + 3, next);
+    multiply(now);
+  };
+  auto step_between = [&](auto now, auto next) {  // the steps asked for are whole
+    tile_arrived<kLeft>();
+    tile_barrier();
+    tile_arrived<kLeftPut>();
+    put(next, std::true_type());
+    first.direct(lds + to);
+    to = after(to);
+    second.template whole<next()>();
+    multiply(now);
+  };
+  ask_first(0);
+  ask_second(0, even);
+  tile_arrived<0>();
+  put(even, std::false_type());
+  if (steps > 1) ask_first(1);
+  if (steps > 1) ask_second(1, odd);
+  if (steps > 2) ask_second(2, even);
+  int s = 0;
+  step(s++, even, odd);
+  if (s < steps) step(s++, odd, even);
+  tile_arrived<0>();  // (whichever way the steps so far came: the compiler's own count of what is on its way begins anew)
+#pragma unroll 1
+  for (; s + 5 < steps; s += 2) {
+    step_between(even, odd);
+    step_between(odd, even);
+  }
+#pragma unroll 1
+  for (; s < steps; s += 2) {
+    step(s, even, odd);
+    if (s + 1 < steps) step(s + 1, odd, even);
   }
   __syncthreads();
 }
