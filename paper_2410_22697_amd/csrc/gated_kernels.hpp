@@ -194,35 +194,58 @@ __global__ __launch_bounds__(kGateNT) void k_gated_dz(GatedDz<T> a) {
   }
 }
 
-// dx = dz w over many rows: 128 rows by 64 NB columns a block.
+// dx = dz w: 128 rows by 64 NB columns a block, and of dz's columns as many as a
+// part has. parts: [parts][rows][cols] if there are several, else null.
 template <typename T, int NB, bool DIRECT>
-__global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tiles_n, int64_t blocks) {
+__global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, float* parts, int64_t part, int tiles_n, int64_t tiles, int64_t blocks) {
   typedef TileAcross<T, 64 * NB> A;
   typedef TileAlong<T, kTileSecond> B;
   typedef TileTurn<T, 32 * NB> Turn;
-  constexpr int kLds = tile_lds<A, B>(DIRECT) > 4 * Turn::kBytes ? tile_lds<A, B>(DIRECT) : 4 * Turn::kBytes;
+  constexpr int kTurns = 4 * TileTurn<float, 32 * NB>::kBytes, kLds = tile_lds<A, B>(DIRECT) > kTurns ? tile_lds<A, B>(DIRECT) : kTurns;
   __shared__ __align__(16) char lds[kLds];
-  const int64_t tile = tile_of_block(blockIdx.x, blocks);
+  const int64_t block = tile_of_block(blockIdx.x, blocks), tile = block % tiles, p = block / tiles, from = p * part;
   const int64_t r0 = tile / tiles_n * kTileSecond;
   const int n0 = (int)(tile % tiles_n) * (64 * NB);
   A weights;
   B rows;
   f32x16 acc[NB][2] = {};
-  const TileSegment segments[1] = {{a.dz.K, a.cols >= 16 / (int)sizeof(T)}};
+  const TileSegment segments[1] = {{min(part, a.dz.K - from), a.cols >= 16 / (int)sizeof(T)}};
   auto begin = [&](int) {
         weights.begin([&](int c, int& at, int& columns, int64_t& stride) {
           at = n0 + c;
           columns = a.cols;
           stride = a.w.stride;
-          return a.w.p;
+          return a.w.p + from * stride;
         });
-        rows.begin([&](int r) { return a.dz.p + min(r0 + r, a.rows - 1) * a.dz.stride; });
+        rows.begin([&](int r) { return a.dz.p + from + min(r0 + r, a.rows - 1) * a.dz.stride; });
   };
   if constexpr (DIRECT) tile_product_direct<T, NB>(weights, rows, segments, begin, lds, acc);
   else tile_product<T, NB>(weights, rows, segments, begin, lds, acc);
   const int wave = wave_uniform((int32_t)wave_id());
-  const Turn turn = {lds + wave * Turn::kBytes};
   const int c0 = n0 + wave % 2 * (32 * NB);
+  if (parts) {
+    typedef TileTurn<float, 32 * NB> WideTurn;
+    const WideTurn turn = {lds + wave * WideTurn::kBytes};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+          turn.in(32 * i, q, v);
+        }
+      const int64_t at = r0 + wave / 2 * 64 + 32 * j;
+      turn.units([&](int r, int c, cols_t<float, 4> v) {
+        if (at + r >= a.rows || c0 + c >= round_up_to<16 / (int)sizeof(T)>(a.cols)) return;
+        const int col = tile_column<T>(c0 + c, a.cols);
+        const float four[4] = {v[0], v[1], v[2], v[3]};
+        store_cols<float, 4, false>(parts + (p * a.rows + at + r) * a.cols + col, a.cols - col, four);
+      });
+    }
+    return;
+  }
+  const Turn turn = {lds + wave * Turn::kBytes};
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -249,15 +272,26 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, int tile
   }
 }
 
+// dw = dz^T [x | x2] and db by parts of the rows, or as they are if one part has
+// all rows (`parts` and `sums` null).
+template <typename T>
+struct GatedDw {
+  Operand<T> dz, x[2];
+  float *parts, *sums;  // [parts][n][k0 + k1], [parts][n]
+  T *dw, *db;           // db null: not asked for
+  int64_t dw_stride, rows, part;
+  int n, k[2], second;  // n: outputs of both halves; second: the position of the second input's first column
+  int tiles_n, tiles_k;
+};
+
 // A block's part of dw: row(p) is the output at position p of its 128 (a.n: none).
 template <typename T, int NB, typename F>
-__device__ __forceinline__ void dw_out(const LinearDw<T>& a, char* lds, const f32x16 (&acc)[NB][2], int64_t part, int k0, F row_at) {
+__device__ __forceinline__ void dw_out(const GatedDw<T>& a, char* lds, const f32x16 (&acc)[NB][2], int64_t part, int k0, F row_at) {
   constexpr int kV = 16 / sizeof(T);
   typedef TileTurn<float, 32 * NB> Turn;
   const int wave = wave_uniform((int32_t)wave_id());
   const Turn turn = {lds + wave * Turn::kBytes};
   const int all = a.k[0] + a.k[1], c0 = k0 + wave % 2 * (32 * NB);
-  float* dw = a.dw + part * a.n * (int64_t)all;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -271,15 +305,10 @@ __device__ __forceinline__ void dw_out(const LinearDw<T>& a, char* lds, const f3
       const int at = c0 + c, s = at >= a.second ? 1 : 0, c1 = at - (s ? a.second : 0), columns = s ? a.k[1] : a.k[0];
       const int row = row_at(wave / 2 * 64 + 32 * j + r);
       if (row >= a.n || c1 >= round_up_to<kV>(columns)) return;
-      const int col = tile_column<T>(c1, columns);
-      float* p = dw + (int64_t)row * all + (s ? a.k[0] : 0) + col;
-      if (col + 4 <= columns) {
-        *reinterpret_cast<cols_t<float, 4>*>(p) = v;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (col + e < columns) p[e] = v[e];
-      }
+      const int col = tile_column<T>(c1, columns), to = (s ? a.k[0] : 0) + col;
+      const float four[4] = {v[0], v[1], v[2], v[3]};
+      if (a.parts) store_cols<float, 4, false>(a.parts + (part * a.n + row) * (int64_t)all + to, columns - col, four);
+      else store_cols<T, 4, false>(a.dw + row * a.dw_stride + to, columns - col, four);
     });
   }
 }
@@ -287,7 +316,7 @@ __device__ __forceinline__ void dw_out(const LinearDw<T>& a, char* lds, const f3
 // dw = dz^T [x | x2], one part of the rows a block: 128 outputs by 64 NB columns.
 // Columns are placed in whole units, the second input's from `second` on.
 template <typename T, int NB, bool DIRECT>
-__global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(LinearDw<T> a, int64_t blocks) {
+__global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(GatedDw<T> a, int64_t blocks) {
   typedef TileAcross<T, 64 * NB> A;
   typedef TileAcross<T, kTileSecond> B;
   typedef TileTurn<float, 32 * NB> Turn;
@@ -418,7 +447,7 @@ struct TileGates {
 // dw and the sums for db, of dz as TileGates makes it: one launch that reads dy
 // and pre once, for inputs of whole units in one tile of columns.
 template <typename T, int NB, int ACT>
-__global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(LinearDw<T> a, GatedDz<T> z, int64_t blocks) {
+__global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(GatedDw<T> a, GatedDz<T> z, int64_t blocks) {
   typedef TileAcross<T, 64 * NB> A;
   typedef TileGates<T, ACT> B;
   typedef TileTurn<float, 32 * NB> Turn;
@@ -447,7 +476,7 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(LinearDw<T> a, Gat
     const int c = n0 + p % 64;
     return c < last ? p / 64 * z.n + tile_column<T>(c, z.n) : a.n;
   };
-  if (a.dbias) {
+  if (a.db) {
     // the threads that share columns add up in order
     float* joined = reinterpret_cast<float*>(lds);
     const int r = threadIdx.x / B::kUnits, c = threadIdx.x % B::kUnits * kV;
@@ -461,37 +490,64 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(LinearDw<T> a, Gat
       float t = 0.0f;
 #pragma unroll
       for (int g = 0; g < tile_step<T>(); ++g) t += joined[g * 128 + threadIdx.x];
-      a.dbias[part * a.n + row] = t;
+      if (a.sums) a.sums[part * a.n + row] = t;
+      else a.db[row] = (T)t;
     }
     __syncthreads();
   }
   dw_out<T, NB>(a, lds, acc, part, 0, row_at);
 }
 
-// Adds the parts of dw (rows of `cols`) and then those of db, four values a
-// thread.
+// Adds parts of arrays of rows, four values a thread, WAYS threads a value, each
+// over every WAYS-th part, then in order: for dw and db, or dx.
 template <typename T>
-__global__ __launch_bounds__(kGateNT) void k_gated_join(const float* __restrict__ dw_parts, const float* __restrict__ db_parts, int64_t count, int64_t dw_values, int n,
-                                                        int cols, T* __restrict__ dw, int64_t stride, T* __restrict__ db) {
-  const int64_t dw_blocks = (dw_values + 4 * kGateNT - 1) / (4 * kGateNT);
-  const bool bias = blockIdx.x >= dw_blocks;
-  const float* parts = bias ? db_parts : dw_parts;
-  const int64_t values = bias ? n : dw_values, i = ((int64_t)(blockIdx.x - (bias ? dw_blocks : 0)) * kGateNT + threadIdx.x) * 4;
-  if (i >= values) return;
+struct GatedJoin {
+  const float* parts[2];
+  T* to[2];
+  int64_t values[2], stride[2], count;
+  int cols[2], split;  // column split of the first's rows is another array's
+  T* beyond;
+  int64_t beyond_stride;
+};
+template <typename T, int WAYS>
+__global__ __launch_bounds__(kGateNT) void k_gated_join(GatedJoin<T> a) {
+  constexpr int kValues = kGateNT / WAYS * 4;
+  __shared__ __align__(16) float sums[WAYS][kValues];
+  const int64_t blocks = (a.values[0] + kValues - 1) / kValues;
+  const bool other = blockIdx.x >= blocks;
+  const float* parts = other ? a.parts[1] : a.parts[0];
+  const int64_t values = other ? a.values[1] : a.values[0];
+  const int way = threadIdx.x / (kGateNT / WAYS), at = threadIdx.x % (kGateNT / WAYS) * 4;
+  const int64_t i = (int64_t)(blockIdx.x - (other ? blocks : 0)) * kValues + at;
   const int valid = (int)min(values - i, (int64_t)4);
   float sum[4] = {};
-#pragma unroll 8
-  for (int64_t p = 0; p < count; ++p) {
-    float v[4];
-    load_cols<float, 4>(parts + p * values + i, valid, v);
+  if (valid > 0) {
+#pragma unroll 4
+    for (int64_t p = way; p < a.count; p += WAYS) {
+      float v[4];
+      load_cols<float, 4>(parts + p * values + i, valid, v);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) sum[q] += v[q];
+      for (int q = 0; q < 4; ++q) sum[q] += v[q];
+    }
   }
+  if constexpr (WAYS > 1) {
+    *reinterpret_cast<f32x4*>(&sums[way][at]) = f32x4{sum[0], sum[1], sum[2], sum[3]};
+    __syncthreads();
+    if (way) return;
+#pragma unroll
+    for (int w = 1; w < WAYS; ++w)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum[q] += sums[w][at + q];
+  }
+  const int cols = other ? a.cols[1] : a.cols[0];
 #pragma unroll
   for (int q = 0; q < 4; ++q)
     if (q < valid) {
-      if (bias) db[i + q] = (T)sum[q];
-      else dw[(i + q) / cols * stride + (i + q) % cols] = (T)sum[q];
+      const int64_t row = (i + q) / cols;
+      const int col = (int)((i + q) % cols);
+      if (other) a.to[1][row * a.stride[1] + col] = (T)sum[q];
+      else if (col < a.split) a.to[0][row * a.stride[0] + col] = (T)sum[q];
+      else a.beyond[row * a.beyond_stride + col - a.split] = (T)sum[q];
     }
 }
 

@@ -170,6 +170,16 @@ bool in_units(const void* p, int64_t stride) {
   return !p || (aligned(p, 16) && stride * (int64_t)sizeof(T) % 16 == 0);
 }
 
+// Whether a call takes the form in which a block's waves share the reduction: for
+// few results, and in bf16 for a reduction long enough that one block's steps
+// last longer than that (us, few / tiles, graph: bf16 16 rows of 256 -> 1024
+// 7.8 / 6.6, 250 9.0 / 7.2; fp32 250 rows 12.1 / 22.7, 1000 33 / 24; 1000 rows of
+// 128 -> 256 10.7 / 13.7, 4000 27 / 14.5).
+template <typename T>
+bool gated_few(const massive_gated_args* a) {
+  return a->rows * round_up(a->n, 32) <= int64_t(1) << 18 && (sizeof(T) == 4 || a->k + a->k_second > 448);
+}
+
 template <typename T>
 int gated(const massive_gated_args* a, void* stream) {
   const char* what = "massive_gated";
@@ -186,7 +196,7 @@ int gated(const massive_gated_args* a, void* stream) {
   f.rows = a->rows;
   f.n = a->n;
   f.act = a->act;
-  if (a->rows * round_up(a->n, 32) >= int64_t(1) << 20) {
+  if (!gated_few<T>(a)) {
     const bool direct = in_units<T>(a->x, a->x_stride) && in_units<T>(a->x_second, a->x_second_stride) && in_units<T>(a->w, a->w_stride) &&
                         (!a->x_second || a->k * sizeof(T) % 16 == 0);
     auto tile = [&](auto nb) {
@@ -194,18 +204,21 @@ int gated(const massive_gated_args* a, void* stream) {
       if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
       return launch(what, direct ? k_gated_tile<T, nb(), true> : k_gated_tile<T, nb(), false>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
     };
-    return a->n <= 64 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>());
+    // narrow tiles until there are two rounds of wide ones for the chip (256 -> 1024 in bf16: 4000 rows 11.8 us wide, 10.8
+    // narrow, 16000 30.3 and 30.1, 110K 171 and 183)
+    return cdiv(a->rows, kTileSecond) * cdiv(a->n, 128) < 1024 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>());
   }
   const int tiles_n = (int)cdiv(a->n, 32);
   return launch(what, k_gated_few<T>, cdiv(a->rows, 32) * tiles_n, kFewNT, 0, stream, f, tiles_n);
 }
 
 // dw's tiles and the parts of its rows: as many blocks as the chip holds at a
-// time, none of less than eight steps of rows where there are more. `made`: dz
+// time, none of less than eight steps of rows (four in fp32, whose steps last
+// longer) where there are more. `made`: dz
 // is made on its way into the product, 64 outputs of both halves a tile.
 struct GatedDwPlan {
   int nb, second;
-  int64_t tiles_n, tiles_k, part, parts, floats, sums;
+  int64_t tiles_n, tiles_k, part, parts, floats, sums;  // floats, sums: of parts, none of a single one
 };
 GatedDwPlan gated_dw_plan(const massive_gated_grads* a, bool made) {
   GatedDwPlan p;
@@ -215,19 +228,49 @@ GatedDwPlan gated_dw_plan(const massive_gated_grads* a, bool made) {
   p.nb = cols <= 128 ? 2 : 4;
   p.tiles_n = made ? cdiv(a->n, 64) : cdiv(n, kTileSecond);
   p.tiles_k = cdiv(cols, 64 * p.nb);
-  const int64_t most = std::max<int64_t>(1, cdiv(a->rows, 8 * step));
+  const int64_t most = std::max<int64_t>(1, cdiv(a->rows, (a->type == MASSIVE_F32 ? 4 : 8) * step));
   p.part = std::max<int64_t>(1, round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, 512 / (p.tiles_n * p.tiles_k)))), step));
   p.parts = cdiv(a->rows, p.part);
-  p.floats = a->dw ? p.parts * n * ((int64_t)a->k + a->k_second) : 0;
-  p.sums = made && a->dbias ? p.parts * n : 0;
+  p.floats = a->dw && p.parts > 1 ? p.parts * n * ((int64_t)a->k + a->k_second) : 0;
+  p.sums = made && a->dbias && p.parts > 1 ? p.parts * n : 0;
   return p;
 }
 
-// The backward pass's workspace: dz, the parts of db, those of dw. It has room
-// for both ways to dw, of which the arrays' alignment chooses one.
+// dx's tiles, narrow ones where wide ones are less than a round for the chip, and
+// the parts of its reduction over dz's columns where there are few tiles. A step
+// takes a block about 0.4 us (bf16; fp32 1), and a part's values 8 bytes written
+// and read at ~4 TB/s; with the join's launch, 4 us, that says how many parts pay
+// (us of all gradients in bf16, parts / none: 16 rows of 256 -> 1024 20 / 42,
+// 1000 rows 50 / 56; with four parts wherever tiles leave room, 16K rows of 128 ->
+// 256 65, with none 36).
+struct GatedDxPlan {
+  int nb;
+  int64_t tiles_n, tiles, part, parts, floats;
+};
+GatedDxPlan gated_dx_plan(const massive_gated_grads* a) {
+  GatedDxPlan p;
+  const int64_t cols = (a->dx ? a->k : 0) + (a->dx_second ? a->k_second : 0), n = 2 * (int64_t)a->n, step = kTileStepBytes / size_of(a->type);
+  const int64_t row_tiles = cdiv(a->rows, kTileSecond), steps = cdiv(n, step);
+  p.nb = cols <= 128 || row_tiles * cdiv(cols, 256) < 512 ? 2 : 4;
+  p.tiles_n = std::max<int64_t>(1, cdiv(cols, 64 * p.nb));
+  p.tiles = row_tiles * p.tiles_n;
+  const double all = steps * (a->type == MASSIVE_F32 ? 1.0 : 0.4), each = 2e-6 * a->rows * cols;
+  int64_t parts = (int64_t)std::min(std::sqrt(all / std::max(each, 1e-9)), 512.0 / std::max<int64_t>(1, p.tiles));
+  parts = std::max<int64_t>(1, std::min(parts, steps / 4));
+  if (all * (1 - 1.0 / parts) < 4 + parts * each) parts = 1;
+  p.part = round_up(cdiv(n, parts), step);
+  p.parts = cdiv(n, p.part);
+  p.floats = p.parts > 1 ? p.parts * a->rows * cols : 0;
+  return p;
+}
+
+// The backward pass's workspace: dz, the parts of db, those of dw or, later, of
+// dx. It has room for both ways to dw, of which the arrays' alignment chooses
+// one.
 struct GatedPlan {
   int64_t groups, part, parts, sums_at, dw_at, bytes;
   GatedDwPlan dw, made;
+  GatedDxPlan dx;
 };
 GatedPlan gated_plan(const massive_gated_grads* a) {
   GatedPlan p;
@@ -239,7 +282,8 @@ GatedPlan gated_plan(const massive_gated_grads* a) {
   p.made = gated_dw_plan(a, true);
   p.sums_at = a->dx || a->dx_second || a->dw ? round_up(a->rows * 2 * a->n * size, 16) : 0;
   p.dw_at = p.sums_at + (a->dbias ? round_up(std::max(p.parts * 2 * a->n, p.made.sums) * 4, 16) : 0);
-  p.bytes = p.dw_at + std::max(p.dw.floats, p.made.floats) * 4;
+  p.dx = gated_dx_plan(a);
+  p.bytes = p.dw_at + std::max(std::max(p.dw.floats, p.made.floats), p.dx.floats) * 4;
   return p;
 }
 
@@ -267,12 +311,14 @@ int with_act_of(int act, F f) {
   }
 }
 
-// The launch that adds up the parts of dw and of db, each if there are any.
+// Adds up parts, by as many threads a value as fill the chip.
 template <typename T>
-int gated_join(const massive_gated_grads* a, const float* dw, const float* db, int64_t parts, void* stream) {
-  const int cols = a->k + a->k_second, n = 2 * a->n;
-  const int64_t values = dw ? (int64_t)n * cols : 0, blocks = cdiv(values, 4 * kGateNT) + (db ? cdiv(n, 4 * kGateNT) : 0);
-  return launch("massive_gated_backward", k_gated_join<T>, blocks, kGateNT, 0, stream, dw, db, parts, values, n, cols, (T*)a->dw, a->dw_stride, (T*)a->dbias);
+int gated_join(const GatedJoin<T>& j, void* stream) {
+  auto ways = [&](auto w) {
+    constexpr int kValues = kGateNT / w() * 4;
+    return launch("massive_gated_backward", k_gated_join<T, w()>, cdiv(j.values[0], kValues) + cdiv(j.values[1], kValues), kGateNT, 0, stream, j);
+  };
+  return j.count <= 2 ? ways(std::integral_constant<int, 1>()) : ways(std::integral_constant<int, 16>());
 }
 
 // dz and db by themselves.
@@ -289,8 +335,9 @@ int gated_dz(const massive_gated_grads* a, const GatedPlan& p, char* workspace, 
 }
 
 template <typename T>
-int gated_dx(const massive_gated_grads* a, char* workspace, void* stream) {
+int gated_dx(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
   constexpr int kV = 16 / sizeof(T);
+  const GatedDxPlan& d = p.dx;
   const int n = 2 * a->n;
   LinearDx<T> f;
   f.dz = rows_of<T>(workspace, n, a->rows, n);
@@ -303,12 +350,43 @@ int gated_dx(const massive_gated_grads* a, char* workspace, void* stream) {
   f.rows = a->rows;
   f.cols = k0 + k1;
   f.split = k0;
+  float* parts = d.parts > 1 ? (float*)(workspace + p.dw_at) : nullptr;
   const bool direct = n % kV == 0 && in_units<T>(f.w.p, f.w.stride) && f.cols % kV == 0;
   auto tile = [&](auto nb) {
-    const int64_t tiles_n = cdiv(f.cols, 64 * nb()), blocks = cdiv(a->rows, kTileSecond) * tiles_n;
-    return launch("massive_gated_backward", direct ? k_gated_dx<T, nb(), true> : k_gated_dx<T, nb(), false>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
+    return launch("massive_gated_backward", direct ? k_gated_dx<T, nb(), true> : k_gated_dx<T, nb(), false>, d.tiles * d.parts, kTileNT, 0, stream, f, parts, d.part,
+                  (int)d.tiles_n, d.tiles, d.tiles * d.parts);
   };
-  return f.cols <= 128 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>());
+  if (int rc = d.nb == 2 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
+  if (!parts) return MASSIVE_OK;
+  GatedJoin<T> j = {};
+  j.parts[0] = parts;
+  j.to[0] = f.dx[0];
+  j.values[0] = a->rows * f.cols;
+  j.stride[0] = a->dx_stride;
+  j.count = d.parts;
+  j.cols[0] = f.cols;
+  j.split = k0;
+  j.beyond = f.dx[1];
+  j.beyond_stride = a->dx_second_stride;
+  return gated_join(j, stream);
+}
+
+// The joins of dw and db, each if there are any.
+template <typename T>
+GatedJoin<T> dw_join(const massive_gated_grads* a, const float* dw, const float* db, int64_t parts) {
+  GatedJoin<T> j = {};
+  const int cols = a->k + a->k_second, n = 2 * a->n;
+  j.parts[0] = dw;
+  j.parts[1] = db;
+  j.to[0] = (T*)a->dw;
+  j.to[1] = (T*)a->dbias;
+  j.values[0] = dw ? (int64_t)n * cols : 0;
+  j.values[1] = db ? n : 0;
+  j.stride[0] = a->dw_stride;
+  j.count = parts;
+  j.cols[0] = j.split = cols;
+  j.cols[1] = n;
+  return j;
 }
 
 template <typename T>
@@ -323,12 +401,16 @@ int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* works
   if (a->dw) {
     const int n = 2 * a->n;
     const GatedDwPlan& d = made ? p.made : p.dw;
-    LinearDw<T> f;
+    const bool several = d.parts > 1;
+    GatedDw<T> f;
     f.dz = rows_of<T>(workspace, n, a->rows, n);
     f.x[0] = rows_of<T>(a->x, a->x_stride, a->rows, a->k);
     f.x[1] = rows_of<T>(a->x_second, a->x_second_stride, a->rows, a->k_second);
-    f.dw = (float*)(workspace + p.dw_at);
-    f.dbias = made && a->dbias ? (float*)(workspace + p.sums_at) : nullptr;
+    f.parts = several ? (float*)(workspace + p.dw_at) : nullptr;
+    f.sums = several && made && a->dbias ? (float*)(workspace + p.sums_at) : nullptr;
+    f.dw = (T*)a->dw;
+    f.db = made ? (T*)a->dbias : nullptr;
+    f.dw_stride = a->dw_stride;
     f.rows = a->rows;
     f.part = d.part;
     f.n = n;
@@ -346,9 +428,10 @@ int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* works
       return launch(what, units && n % kV == 0 ? k_gated_dw<T, nb(), true> : k_gated_dw<T, nb(), false>, blocks, kTileNT, 0, stream, f, blocks);
     };
     if (int rc = d.nb == 2 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
-    if (int rc = gated_join<T>(a, f.dw, f.dbias, d.parts, stream)) return rc;
+    if (several)
+      if (int rc = gated_join(dw_join<T>(a, f.parts, f.sums, d.parts), stream)) return rc;
   }
-  return dx ? gated_dx<T>(a, workspace, stream) : MASSIVE_OK;
+  return dx ? gated_dx<T>(a, p, workspace, stream) : MASSIVE_OK;
 }
 
 }  // namespace
@@ -467,14 +550,14 @@ int massive_gated_backward(const massive_gated_grads* a, void* workspace, int64_
     if (!aligned(p, size)) REFUSE("an array is not aligned");
   const GatedPlan p = gated_plan(a);
   const int64_t dw_blocks = std::max(p.dw.parts * p.dw.tiles_n * p.dw.tiles_k, p.made.parts * p.made.tiles_n * p.made.tiles_k);
-  if (p.groups * p.parts > kMostBlocks || (a->dw && (dw_blocks > kMostBlocks || cdiv(2 * a->n * k, 4 * kGateNT) + 1024 > kMostBlocks)) ||
+  if (p.groups * p.parts > kMostBlocks || (a->dw && (dw_blocks > kMostBlocks || cdiv(2 * a->n * k, kGateNT / 16 * 4) + (1 << 15) > kMostBlocks)) ||
       cdiv(a->rows, kTileSecond) * cdiv(k, 128) > kMostBlocks)
     REFUSE("too many rows and columns for one call");
   if (a->rows == 0) {  // sums over no rows
     if (!a->dw && !a->dbias) return MASSIVE_OK;
     // the pointers only say which of the two are asked for: with no parts nothing is read
     const float *dw = (const float*)a->dw, *db = (const float*)a->dbias;
-    return a->type == MASSIVE_F32 ? gated_join<float>(a, dw, db, 0, stream) : gated_join<bf16>(a, dw, db, 0, stream);
+    return a->type == MASSIVE_F32 ? gated_join(dw_join<float>(a, dw, db, 0), stream) : gated_join(dw_join<bf16>(a, dw, db, 0), stream);
   }
   if (!workspace || workspace_bytes < p.bytes)
     return call_error(MASSIVE_ECAPACITY, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)p.bytes);

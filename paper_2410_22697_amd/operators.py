@@ -465,6 +465,11 @@ def linear_backward(dy, x, weight, act: str = "none", pre=None, x2=None, bias: b
     return dx, dx2, dw, db
 
 
+def _like(x):
+    """A new tensor of x's shape and type, contiguous whatever x is."""
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 # ---------------------------------------------------------------------- dropout
 def _seed(seed, draw):
     """The seed as (64 bits, or the tensor that holds them), and draw, checked."""
@@ -487,7 +492,7 @@ def _dropout(x, p, seed, draw, residual):
     res_stride = 0 if residual is None else _matrix(residual, "residual", cols=d, rows=rows, dtype=x.dtype)
     if not 0 <= p <= 1:
         raise ValueError("p must be in [0, 1], not %r" % (p,))
-    y = torch.empty((rows, d), dtype=x.dtype, device="cuda")
+    y = _like(x)
     a = _DropoutArgs(x.data_ptr(), _ptr(residual), y.data_ptr(), _ptr(at), rows, stride, res_stride, d, bits, p, draw, d, _TYPES[x.dtype])
     if d:
         _check(_load().massive_dropout(ctypes.byref(a), _stream(here)))
@@ -550,7 +555,7 @@ def _rms_norm(x, weight, eps, residual, fmt, out, slots):
     if fmt is None:
         if out is not None or slots is not None:
             raise ValueError("out and slots are for packed rows, which fmt asks for")
-        y = torch.empty((rows, d), dtype=dtype, device="cuda")
+        y = _like(x)
     else:
         if fmt.d != d:
             raise ValueError("x has %d columns, and the row format %d" % (d, fmt.d))
@@ -564,7 +569,7 @@ def _rms_norm(x, weight, eps, residual, fmt, out, slots):
         if slots is None and table_rows < rows:
             raise ValueError("out has %d rows, and x %d" % (table_rows, rows))
         y = out
-    total = None if residual is None else torch.empty((rows, d), dtype=dtype, device="cuda")
+    total = None if residual is None else _like(x)
     a = _NormArgs(x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(total), y.data_ptr(), None if fmt is None else ctypes.pointer(fmt.c), _ptr(slots),
                   table_rows, rows, stride, res_stride, d, d, eps, d, _TYPES[dtype])
     if d:
@@ -627,7 +632,7 @@ def rms_norm_backward(dy, s, weight=None, eps: float = 1e-6, ds=None, need_dx: b
     ds_stride = 0 if ds is None else _matrix(ds, "ds", cols=d, rows=rows, dtype=dtype)
     if weight is not None:
         _vector(weight, "weight", d, dtype)
-    dx = torch.empty((rows, d), dtype=dtype, device="cuda") if need_dx else None
+    dx = _like(s) if need_dx else None
     dw = torch.empty(d, dtype=dtype, device="cuda") if need_dweight and weight is not None else None
     if d and (dx is not None or dw is not None):
         g = _NormGrads(dy.data_ptr(), s.data_ptr(), _ptr(weight), _ptr(ds), _ptr(dx), _ptr(dw), rows, dy_stride, stride, ds_stride, d, eps, d,
