@@ -252,8 +252,9 @@ int massive_get_timing(massive_ctx* ctx, double* out_ms, int64_t* out_calls);
 
 /* ------------------------------------------------------------------------
  * Operators of a training step on what massive_sample gathers: rows held in
- * few bits, the mean over a sampled block, a layer's product and the step on
- * the weights, with their gradients.
+ * few bits, the mean over a sampled block, a layer's product, a gated layer,
+ * the norm and the dropout between them and the step on the weights, with
+ * their gradients.
  *
  * They take no context. Every call checks its arguments on the host, enqueues
  * its kernels on `stream` and returns without waiting; it allocates nothing
@@ -265,7 +266,7 @@ int massive_get_timing(massive_ctx* ctx, double* out_ms, int64_t* out_calls);
  * (MASSIVE_F32, MASSIVE_BF16) at their natural alignment; strides are in
  * elements. Sums, products' accumulators and statistics are fp32; a result is
  * rounded to nearest even where it is stored, and nothing before it is rounded
- * to fewer bits, but for dz in massive_linear_grads. Results do not depend on
+ * to fewer bits, but for dz in massive_linear_grads and massive_gated_grads. Results do not depend on
  * the order in which the device runs a call's blocks: the same call on the
  * same inputs gives the same bits. An empty extent (no rows, no tensors) is
  * MASSIVE_OK and does nothing. On failure the message is in
@@ -273,7 +274,8 @@ int massive_get_timing(massive_ctx* ctx, double* out_ms, int64_t* out_calls);
  *
  * A call may be captured into a HIP graph. Its replays read and write the same
  * addresses, and keep the arguments that the call had on the host, among them
- * massive_adamw's lr and t: every replay repeats the captured step's bias
+ * massive_dropout's seed (but not what it reads at seed_at) and massive_adamw's
+ * lr and t: every replay repeats the captured step's bias
  * corrections. That is right only once both are 1; until then the step belongs
  * outside the graph.
  */

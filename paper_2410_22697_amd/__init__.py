@@ -4,8 +4,9 @@
 `Massive` samples minibatches and gathers their rows; `operators` has what a
 training step does with them: rows held in few bits (`RowFormat`, `pack_rows`,
 `unpack_rows`), the mean over a sampled block (`block_mean`), a layer
-(`linear`) and the step on the weights (`AdamW`). Everything runs in
-libmassive's HIP kernels; making a `Massive`, or calling an operator, raises
+(`linear`), a gated one (`gated`), the norm and the dropout between them
+(`rms_norm`, `dropout`) and the step on the weights (`AdamW`). Everything runs
+in libmassive's HIP kernels; making a `Massive`, or calling an operator, raises
 if libmassive.so has not been built.
 """
 import importlib

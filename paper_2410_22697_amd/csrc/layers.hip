@@ -311,14 +311,16 @@ int with_act_of(int act, F f) {
   }
 }
 
-// Adds up parts, by as many threads a value as fill the chip.
+// Adds up parts, by as many threads a value as fill the chip (us, one / sixteen: 33
+// parts of 524K values 14-18 / 19; all gradients with 250 parts of 8K 90 / 34).
 template <typename T>
 int gated_join(const GatedJoin<T>& j, void* stream) {
   auto ways = [&](auto w) {
     constexpr int kValues = kGateNT / w() * 4;
     return launch("massive_gated_backward", k_gated_join<T, w()>, cdiv(j.values[0], kValues) + cdiv(j.values[1], kValues), kGateNT, 0, stream, j);
   };
-  return j.count <= 2 ? ways(std::integral_constant<int, 1>()) : ways(std::integral_constant<int, 16>());
+  if (j.count <= 2 || j.values[0] >= 1 << 19) return ways(std::integral_constant<int, 1>());
+  return j.values[0] >= 1 << 17 ? ways(std::integral_constant<int, 4>()) : ways(std::integral_constant<int, 16>());
 }
 
 // dz and db by themselves.
@@ -550,7 +552,7 @@ int massive_gated_backward(const massive_gated_grads* a, void* workspace, int64_
     if (!aligned(p, size)) REFUSE("an array is not aligned");
   const GatedPlan p = gated_plan(a);
   const int64_t dw_blocks = std::max(p.dw.parts * p.dw.tiles_n * p.dw.tiles_k, p.made.parts * p.made.tiles_n * p.made.tiles_k);
-  if (p.groups * p.parts > kMostBlocks || (a->dw && (dw_blocks > kMostBlocks || cdiv(2 * a->n * k, kGateNT / 16 * 4) + (1 << 15) > kMostBlocks)) ||
+  if (p.groups * p.parts > kMostBlocks || (a->dw && (dw_blocks > kMostBlocks || cdiv(2 * a->n * k, 4 * kGateNT) + (1 << 15) > kMostBlocks)) ||
       cdiv(a->rows, kTileSecond) * cdiv(k, 128) > kMostBlocks)
     REFUSE("too many rows and columns for one call");
   if (a->rows == 0) {  // sums over no rows

@@ -1,14 +1,15 @@
 """What a training step does with the rows that `Massive` gathers (the
 operators of include/massive.h): rows held in few bits, the mean over a sampled
-block, a layer and the step on its weights.
+block, a layer, a gated layer, the norm and the dropout between them, and the
+step on their weights.
 
 As in the rest of the binding, Python only checks and marshals arguments: every
 operator runs in the library's HIP kernels, on the current stream of the
 tensors' device, and returns without waiting. Outputs and workspaces come from
-torch's allocator. `linear` and `block_mean` take part in autograd (once, in
-reverse: their gradients are not differentiated again, and tensors with
-forward-mode tangents are refused), and their gradients are also there as calls
-of their own. What a call changes in place counts as changed there: a
+torch's allocator. `linear`, `gated`, `rms_norm`, `dropout` and `block_mean`
+take part in autograd (once, in reverse: their gradients are not differentiated
+again, and tensors with forward-mode tangents are refused), and their gradients
+are also there as calls of their own. What a call changes in place counts as changed there: a
 backward pass that would read it raises. Wrong arguments raise ValueError here,
 or MassiveError where the library refuses them.
 """
@@ -472,20 +473,20 @@ def _like(x):
 
 # ---------------------------------------------------------------------- dropout
 def _seed(seed, draw):
-    """The seed as (64 bits, or the tensor that holds them), and draw, checked."""
-    if not isinstance(draw, int) or not 0 <= draw < 2 ** 32:
+    """The seed as 64 bits or the tensor that holds them, and draw, checked."""
+    if not hasattr(draw, "__index__") or not 0 <= operator.index(draw) < 2 ** 32:
         raise ValueError("draw must be a whole number in 0..2^32 - 1, not %r" % (draw,))
     if isinstance(seed, torch.Tensor):
         if seed.dtype != torch.int64 or seed.numel() != 1:
             raise ValueError("a seed in a tensor must be one int64 value")
-        return 0, seed
-    if not isinstance(seed, int) or not -2 ** 63 <= seed < 2 ** 64:
+        return 0, seed, operator.index(draw)
+    if not hasattr(seed, "__index__") or not -2 ** 63 <= operator.index(seed) < 2 ** 64:
         raise ValueError("seed must be a whole number of 64 bits, or an int64 tensor, not %r" % (seed,))
-    return seed % 2 ** 64, None
+    return operator.index(seed) % 2 ** 64, None, operator.index(draw)
 
 
 def _dropout(x, p, seed, draw, residual):
-    bits, at = _seed(seed, draw)
+    bits, at, draw = _seed(seed, draw)
     stride = _matrix(x, "x")
     here = _on_gpu(x, residual, at)
     rows, d = x.shape
