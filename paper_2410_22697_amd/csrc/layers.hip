@@ -21,6 +21,19 @@ using namespace ms;
 constexpr int64_t kMostRows = int64_t(1) << 29;
 constexpr int64_t kMostCols = 1 << 20;
 
+// Columns a lane takes of rows of d columns: 16 bytes, but 8 where rows are whole
+// in units of 8 bytes and not in units of 16, as those of 100 columns in bf16
+// are: a lane's 16 bytes would straddle lines and the row's end be read value by
+// value (854K such rows, us, 16 bytes / 8: norm 122 / 75, with the residual 243 /
+// 137, gradients 235 / 178). By d alone, so that results
+// do not hang on where the arrays lie.
+template <typename T, typename F>
+int with_unit(int64_t d, F f) {
+  if constexpr (sizeof(T) == 2)
+    if (d % 8 == 4) return f(std::integral_constant<int, 4>());
+  return f(std::integral_constant<int, 16 / sizeof(T)>());
+}
+
 // ------------------------------------------------------------------- dropout
 template <typename T>
 int dropout(const massive_dropout_args* a, uint64_t below, void* stream) {
@@ -39,9 +52,12 @@ int dropout(const massive_dropout_args* a, uint64_t below, void* stream) {
   f.all = below >> 32;
   f.d = a->d;
   f.scale = f.all ? 0.0f : (float)(1.0 / (1.0 - a->p));
-  const int team = team_of(a->d, 16 / sizeof(T));
-  const int64_t blocks = std::min(cdiv(a->rows, kDropAhead * (kDropNT / team)), kMostBlocks);
-  return with_team(team, [&](auto t) { return launch("massive_dropout", k_dropout<T, t()>, blocks, kDropNT, 0, stream, f); });
+  return with_unit<T>(a->d, [&](auto q) {
+    const int64_t units = cdiv(a->d, q()), all = a->rows * units;
+    // rounded up: at * inverse / 2^32 is at / units for all at and units below kDropChunk + units
+    const uint32_t inverse = units > 1 ? (uint32_t)(((uint64_t(1) << 32) + units - 1) / units) : 0;
+    return launch("massive_dropout", k_dropout<T, q()>, std::min(cdiv(all, kDropChunk), kMostBlocks), kDropNT, 0, stream, f, (uint32_t)units, inverse, all);
+  });
 }
 
 // ---------------------------------------------------------------------- norm
@@ -63,7 +79,10 @@ int with_norm(int64_t d, F f) {
 }
 
 constexpr int64_t kNormBlocks = 8192;      // a block takes several rows: it reads the weights once
-constexpr int64_t kNormGradBlocks = 1024;  // and leaves one part of dw
+// The gradient's blocks leave a part of dw each: 1024 of them, and 2048 where a
+// team would have over 64 rows one after the other (us, 1024 / 2048: 854K x 100
+// bf16, 104 rows a team, 178 / 117; 242K x 256, 30 rows, 71 / 80).
+constexpr int64_t kNormGradBlocks = 1024, kNormGradRows = 64;
 
 template <typename T>
 int rms_norm(const massive_norm_args* a, const PackedRows& packed, void* stream) {
@@ -92,23 +111,24 @@ int rms_norm(const massive_norm_args* a, const PackedRows& packed, void* stream)
     });
   };
   using std::integral_constant;
-  if (!a->fmt) return go(integral_constant<int, 0>(), integral_constant<int, 16 / sizeof(T)>());
+  if (!a->fmt) return with_unit<T>(a->d, [&](auto q) { return go(integral_constant<int, 0>(), q); });
   return with_bits(a->fmt->bits, [&](auto bits) { return go(bits, integral_constant<int, kRowsQ>()); });
 }
 
 // Blocks of the gradient's kernel, which are also the parts of dw.
 int64_t norm_blocks(const massive_norm_grads* a) {
-  const int q = 16 / size_of(a->type);
-  int64_t blocks = 0;
-  auto of = [&](auto team, auto) {
-    constexpr int kTeams = team() > MS_WAVE ? 1 : kNormNT / team();
-    // long rows' parts are kept to 256 MB
-    blocks = std::min(cdiv(a->rows, kTeams), team() > MS_WAVE ? std::max<int64_t>(1, std::min<int64_t>(512, (int64_t(1) << 26) / a->d)) : kNormGradBlocks);
-    return 0;
-  };
-  if (q == 4) with_norm<4>(a->d, of);
-  else with_norm<8>(a->d, of);
-  return blocks;
+  return with_type(a->type, [&](auto* t) -> int {
+    using T = std::remove_pointer_t<decltype(t)>;
+    return with_unit<T>(a->d, [&](auto q) {
+      return with_norm<q()>(a->d, [&](auto team, auto) {
+        constexpr int kTeams = team() > MS_WAVE ? 1 : kNormNT / team();
+        // long rows' parts are kept to 256 MB
+        const int64_t all = cdiv(a->rows, kTeams);
+        if (team() > MS_WAVE) return (int)std::min(all, std::max<int64_t>(1, std::min<int64_t>(512, (int64_t(1) << 26) / a->d)));
+        return (int)std::min(all, all > kNormGradRows * kNormGradBlocks ? 2 * kNormGradBlocks : kNormGradBlocks);
+      });
+    });
+  });
 }
 
 int check_norm(const massive_norm_grads* a) {
@@ -139,8 +159,10 @@ int rms_norm_backward(const massive_norm_grads* a, void* workspace, void* stream
   n.eps = a->eps > 0 ? std::max((float)a->eps, std::numeric_limits<float>::min()) : 0.0f;
   const int64_t blocks = norm_blocks(a);
   if (a->rows > 0) {
-    const int rc = with_norm<16 / sizeof(T)>(a->d, [&](auto team, auto turns) {
-      return launch(what, k_rms_norm_backward<T, team(), turns(), 16 / sizeof(T)>, blocks, team() > MS_WAVE ? team() : kNormNT, 0, stream, n);
+    const int rc = with_unit<T>(a->d, [&](auto q) {
+      return with_norm<q()>(a->d, [&](auto team, auto turns) {
+        return launch(what, k_rms_norm_backward<T, team(), turns(), q()>, blocks, team() > MS_WAVE ? team() : kNormNT, 0, stream, n);
+      });
     });
     if (rc) return rc;
   }
