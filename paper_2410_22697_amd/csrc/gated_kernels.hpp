@@ -40,6 +40,11 @@ __device__ __forceinline__ void with_act(int act, F f) {
 
 // Many rows: 128 rows by 32 NB outputs of both halves a block; a wave has 16 NB
 // outputs of the gate and the same of the other half.
+// Bound by the products' way from L2 to LDS, and by a tile's end, which has no
+// products beside it. 110K x 256 -> 1024 bf16 170 us (680 TFLOP/s; 118 of it in the
+// products), with pre 287; 16391 x 100 + 100 -> 323 fp32 70 (60 TFLOP/s of what is
+// asked for: 323 outputs take 384, two inputs of 100 take 224 of k, and 774 tiles
+// are a few more than the chip holds at a time).
 template <typename T, int NB, bool DIRECT>
 __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles_n, int64_t blocks) {
   typedef TileAlong<T, 64 * NB> A;
@@ -62,13 +67,13 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles
   f32x16 acc[NB][2] = {};
   const TileSegment segments[2] = {{a.x[0].K, true}, {a.x[1].K, true}};
   auto begin = [&](int g) {
-        const T *xp = g ? a.x[1].p : a.x[0].p, *wp = g ? a.w[1].p : a.w[0].p;
-        const int64_t x_stride = g ? a.x[1].stride : a.x[0].stride;
-        weights.begin([&](int c) {
-          const int square = c / 32 % NB, out = n0 + c / (32 * NB) * kOut + square % (NB / 2) * 32 + c % 32;
-          return wp + (int64_t)((square >= NB / 2 ? a.n : 0) + min(out, a.n - 1)) * a.w[0].stride;
-        });
-        rows.begin([&](int r) { return xp + min(r0 + r, a.rows - 1) * x_stride; });  // those that are not there repeat the last one
+    const T *xp = g ? a.x[1].p : a.x[0].p, *wp = g ? a.w[1].p : a.w[0].p;
+    const int64_t x_stride = g ? a.x[1].stride : a.x[0].stride;
+    weights.begin([&](int c) {
+      const int square = c / 32 % NB, out = n0 + c / (32 * NB) * kOut + square % (NB / 2) * 32 + c % 32;
+      return wp + (int64_t)((square >= NB / 2 ? a.n : 0) + min(out, a.n - 1)) * a.w[0].stride;
+    });
+    rows.begin([&](int r) { return xp + min(r0 + r, a.rows - 1) * x_stride; });  // those that are not there repeat the last one
   };
   if constexpr (DIRECT) tile_product_direct<T, NB>(weights, rows, segments, begin, lds, acc);
   else tile_product<T, NB>(weights, rows, segments, begin, lds, acc);
@@ -102,7 +107,9 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles
 }
 
 // Few rows: 32 rows by 32 outputs of both halves a block, its eight waves share
-// the reduction.
+// the reduction. Bound by the trips to memory that follow each other: a wave makes
+// an eighth of those that a tile makes. 250 x 256 ->
+// 1024 fp32 12.1 us where narrow tiles take 22.7.
 template <typename T>
 __global__ __launch_bounds__(kFewNT) void k_gated_few(Gated<T> a, int tiles_n) {
   __shared__ float halves[2][32 * 32];
@@ -138,7 +145,7 @@ struct GatedDz {
 };
 
 // dz = [dg | du], and the sums of each part of the rows, of dz before it is
-// rounded.
+// rounded. Bound by memory: 110K x 1024 bf16 212 us (5.3 TB/s).
 template <typename T>
 __global__ __launch_bounds__(kGateNT) void k_gated_dz(GatedDz<T> a) {
   constexpr int kV = 16 / sizeof(T), kAhead = 2;
@@ -196,6 +203,9 @@ __global__ __launch_bounds__(kGateNT) void k_gated_dz(GatedDz<T> a) {
 
 // dx = dz w: 128 rows by 64 NB columns a block, and of dz's columns as many as a
 // part has. parts: [parts][rows][cols] if there are several, else null.
+// 110K x 256 -> 1024 bf16 168 to 180 us (690 TFLOP/s; 860 tiles where the chip
+// holds 512 at a time are two rounds), fp32 16391 x 200 -> 323 80 with the parts'
+// sum 11 more (95 in one part).
 template <typename T, int NB, bool DIRECT>
 __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, float* parts, int64_t part, int tiles_n, int64_t tiles, int64_t blocks) {
   typedef TileAcross<T, 64 * NB> A;
@@ -211,13 +221,13 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, float* p
   f32x16 acc[NB][2] = {};
   const TileSegment segments[1] = {{min(part, a.dz.K - from), a.cols >= 16 / (int)sizeof(T)}};
   auto begin = [&](int) {
-        weights.begin([&](int c, int& at, int& columns, int64_t& stride) {
-          at = n0 + c;
-          columns = a.cols;
-          stride = a.w.stride;
-          return a.w.p + from * stride;
-        });
-        rows.begin([&](int r) { return a.dz.p + from + min(r0 + r, a.rows - 1) * a.dz.stride; });
+    weights.begin([&](int c, int& at, int& columns, int64_t& stride) {
+      at = n0 + c;
+      columns = a.cols;
+      stride = a.w.stride;
+      return a.w.p + from * stride;
+    });
+    rows.begin([&](int r) { return a.dz.p + from + min(r0 + r, a.rows - 1) * a.dz.stride; });
   };
   if constexpr (DIRECT) tile_product_direct<T, NB>(weights, rows, segments, begin, lds, acc);
   else tile_product<T, NB>(weights, rows, segments, begin, lds, acc);
@@ -333,19 +343,19 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(GatedDw<T> a, int64_t b
   constexpr int kV = 16 / sizeof(T);
   const TileSegment segments[1] = {{rows, a.n >= kV && a.k[0] >= kV && (a.k[1] == 0 || a.k[1] >= kV)}};
   auto begin = [&](int) {
-        xs.begin([&](int c, int& at, int& columns, int64_t& stride) {
-          const int s = k0 + c >= a.second && a.k[1] > 0 ? 1 : 0;
-          at = k0 + c - (s ? a.second : 0);
-          columns = s ? a.k[1] : a.k[0];
-          stride = s ? a.x[1].stride : a.x[0].stride;
-          return (s ? a.x[1].p : a.x[0].p) + from * stride;
-        });
-        dzs.begin([&](int c, int& at, int& columns, int64_t& stride) {
-          at = n0 + c;
-          columns = a.n;
-          stride = a.dz.stride;
-          return a.dz.p + from * stride;
-        });
+    xs.begin([&](int c, int& at, int& columns, int64_t& stride) {
+      const int s = k0 + c >= a.second && a.k[1] > 0 ? 1 : 0;
+      at = k0 + c - (s ? a.second : 0);
+      columns = s ? a.k[1] : a.k[0];
+      stride = s ? a.x[1].stride : a.x[0].stride;
+      return (s ? a.x[1].p : a.x[0].p) + from * stride;
+    });
+    dzs.begin([&](int c, int& at, int& columns, int64_t& stride) {
+      at = n0 + c;
+      columns = a.n;
+      stride = a.dz.stride;
+      return a.dz.p + from * stride;
+    });
   };
   if constexpr (DIRECT) tile_product_direct<T, NB>(xs, dzs, segments, begin, lds, acc);
   else tile_product<T, NB>(xs, dzs, segments, begin, lds, acc);
@@ -445,7 +455,10 @@ struct TileGates {
 };
 
 // dw and the sums for db, of dz as TileGates makes it: one launch that reads dy
-// and pre once, for inputs of whole units in one tile of columns.
+// and pre once, for inputs of whole units in one tile of columns. Bound by the
+// activation's slope and by memory, which have to share a wave's turns with the
+// products: 110K x 256 -> 1024 bf16 295 us and the parts' sum 17 (k_gated_dz, 212,
+// and k_gated_dw, 160, each at its own bound, take 60 more).
 template <typename T, int NB, int ACT>
 __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(GatedDw<T> a, GatedDz<T> z, int64_t blocks) {
   typedef TileAcross<T, 64 * NB> A;
@@ -499,7 +512,8 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(GatedDw<T> a, Gate
 }
 
 // Adds parts of arrays of rows, four values a thread, WAYS threads a value, each
-// over every WAYS-th part, then in order: for dw and db, or dx.
+// over every WAYS-th part, then in order: for dw and db, or dx. (As many threads a
+// value as keep the chip busy: 646 x 200 of 79 parts 11.8 us.)
 template <typename T>
 struct GatedJoin {
   const float* parts[2];

@@ -10,8 +10,9 @@
 // all their rows and leave a part each.
 //
 // Measured: 242K x 256 bf16 41 us (6.0 TB/s of x and y), with the residual and the
-// sum 77 (6.4), the same to 8 bits 81 (5.4); gradients 71 (5.2), 96 with ds; 854K x
-// 100 fp32 124 (5.5), bf16 75 (4.6).
+// sum 77 (6.4), the same to 8 bits 76 (5.7); gradients 71 (5.2), 93 with ds; 854K x
+// 100 fp32 120 (5.7), bf16 75 (4.6). A long row keeps a block waiting, of which a CU
+// holds two: 30K x 5000 bf16 162 (3.7), gradients 419 (2.1).
 #pragma once
 
 #include "common.hpp"
