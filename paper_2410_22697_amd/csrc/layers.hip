@@ -62,8 +62,12 @@ int dropout(const massive_dropout_args* a, uint64_t below, void* stream) {
 
 // ---------------------------------------------------------------------- norm
 // f(team, turns that a team holds in registers): a wave or a part of one for
-// rows of up to 32 values a lane, else a block.
-template <int Q, typename F>
+// rows of up to 32 values a lane, else a block. The gradients' rows of more than
+// one turn of 16-byte units in bf16 take a block of twice the threads: with two
+// turns in registers a CU would hold one block of half the waves (us, two turns /
+// twice the threads: 30K x 5000 418 / 312, 20K x 8192 316 / 239, 8000 x 20000 698 /
+// 608; in units of four values, and forward, two turns are as fast or faster).
+template <int Q, bool GRADS, typename F>
 int with_norm(int64_t d, F f) {
   using std::integral_constant;
   const integral_constant<int, 1> one;
@@ -75,7 +79,9 @@ int with_norm(int64_t d, F f) {
   if constexpr (Q == 4)
     if (d <= 8 * MS_WAVE * Q) return f(wave, integral_constant<int, 8>());
   const integral_constant<int, kNormLong> block;
-  return d <= kNormLong * Q ? f(block, one) : f(block, two);
+  if (d <= kNormLong * Q) return f(block, one);
+  if constexpr (GRADS && Q == 8) return f(integral_constant<int, 2 * kNormLong>(), one);
+  else return f(block, two);
 }
 
 constexpr int64_t kNormBlocks = 8192;      // a block takes several rows: it reads the weights once
@@ -105,7 +111,7 @@ int rms_norm(const massive_norm_args* a, const PackedRows& packed, void* stream)
   n.inv_d = 1.0f / a->d;
   n.eps = a->eps > 0 ? std::max((float)a->eps, std::numeric_limits<float>::min()) : 0.0f;
   auto go = [&](auto bits, auto q) {
-    return with_norm<q()>(a->d, [&](auto team, auto turns) {
+    return with_norm<q(), false>(a->d, [&](auto team, auto turns) {
       constexpr int kNT = team() > MS_WAVE ? team() : kNormNT, kTeams = kNT / team();
       return launch("massive_rms_norm", k_rms_norm<T, team(), turns(), q(), bits()>, std::min(cdiv(a->rows, kTeams), kNormBlocks), kNT, 0, stream, n);
     });
@@ -120,7 +126,7 @@ int64_t norm_blocks(const massive_norm_grads* a) {
   return with_type(a->type, [&](auto* t) -> int {
     using T = std::remove_pointer_t<decltype(t)>;
     return with_unit<T>(a->d, [&](auto q) {
-      return with_norm<q()>(a->d, [&](auto team, auto) {
+      return with_norm<q(), true>(a->d, [&](auto team, auto) {
         constexpr int kTeams = team() > MS_WAVE ? 1 : kNormNT / team();
         // long rows' parts are kept to 256 MB
         const int64_t all = cdiv(a->rows, kTeams);
@@ -160,7 +166,7 @@ int rms_norm_backward(const massive_norm_grads* a, void* workspace, void* stream
   const int64_t blocks = norm_blocks(a);
   if (a->rows > 0) {
     const int rc = with_unit<T>(a->d, [&](auto q) {
-      return with_norm<q()>(a->d, [&](auto team, auto turns) {
+      return with_norm<q(), true>(a->d, [&](auto team, auto turns) {
         return launch(what, k_rms_norm_backward<T, team(), turns(), q()>, blocks, team() > MS_WAVE ? team() : kNormNT, 0, stream, n);
       });
     });

@@ -12,7 +12,7 @@
 // Measured: 242K x 256 bf16 41 us (6.0 TB/s of x and y), with the residual and the
 // sum 77 (6.4), the same to 8 bits 76 (5.7); gradients 71 (5.2), 93 with ds; 854K x
 // 100 fp32 120 (5.7), bf16 75 (4.6). A long row keeps a block waiting, of which a CU
-// holds two: 30K x 5000 bf16 162 (3.7), gradients 419 (2.1).
+// holds few: 30K x 5000 bf16 162 (3.7), gradients 312 (2.9).
 #pragma once
 
 #include "common.hpp"
@@ -22,7 +22,7 @@
 namespace ms {
 
 constexpr int kNormNT = 256;     // threads of a block of teams
-constexpr int kNormLong = 512;   // threads of a block that has one row at a time
+constexpr int kNormLong = 512;   // threads of a block that has one row at a time (the gradients' longest rows: twice as many)
 
 template <typename T>
 struct Norm {
