@@ -10,7 +10,7 @@
 // Bound by memory, in bf16 without a residual by the generator's ten rounds (20
 // products of 32 by 32 bits a block: about 1.2 T words/s over the chip).
 // Measured: 242K x 256 bf16 53 to 58 us (4.3 to 4.7 TB/s), with the residual 66
-// (5.6); 110K x 1024 fp32 143 (6.3); 854K x 100 bf16 94 us (147 with a team of lanes a row,
+// (5.6); 110K x 1024 fp32 143 (6.3); 854K x 100 bf16 94 to 102 us (147 with a team of lanes a row,
 // three in sixteen of them idle).
 #pragma once
 
@@ -70,8 +70,8 @@ __global__ __launch_bounds__(kDropNT) void k_dropout(Dropout<T> a, uint32_t unit
       row[u] = row0 + over;
       col[u] = (int)(at - over * units) * Q;
       if (row[u] >= a.rows) continue;
-      load_cols<T, Q>(a.x + row[u] * a.x_stride + col[u], a.d - col[u], x[u]);
-      if (a.residual) load_cols<T, Q>(a.residual + row[u] * a.residual_stride + col[u], a.d - col[u], res[u]);
+      load_row<T, Q>(a.x + row[u] * a.x_stride + col[u], a.d - col[u], x[u]);
+      if (a.residual) load_row<T, Q>(a.residual + row[u] * a.residual_stride + col[u], a.d - col[u], res[u]);
     }
 #pragma unroll
     for (int u = 0; u < kDropAhead; ++u) {
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kDropNT) void k_dropout(Dropout<T> a, uint32_t unit
 #pragma unroll
         for (int q = 0; q < Q; ++q) y[q] += res[u][q];
       }
-      store_cols<T, Q>(a.y + row[u] * a.y_stride + col[u], a.d - col[u], y);
+      store_row<T, Q>(a.y + row[u] * a.y_stride + col[u], a.d - col[u], y);
     }
   }
 }

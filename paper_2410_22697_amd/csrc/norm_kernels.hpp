@@ -125,10 +125,10 @@ __global__ __launch_bounds__(TEAM > MS_WAVE ? TEAM : kNormNT) void k_rms_norm(No
   const int64_t x_on = step * a.x_stride, res_on = res ? step * a.residual_stride : 0, sum_on = sum ? step * a.sum_stride : 0, out_on = BITS == 0 ? step * a.y_stride : 0;
   for (; i < a.rows; i += step, x += x_on, res += res_on, sum += sum_on, out += out_on) {
     auto load = [&](int c, float (&s)[Q]) {
-      load_cols<T, Q>(x + c, d - c, s);
+      load_row<T, Q>(x + c, d - c, s);
       if (res) {
         float r[Q];
-        load_cols<T, Q>(res + c, d - c, r);
+        load_row<T, Q>(res + c, d - c, r);
 #pragma unroll
         for (int q = 0; q < Q; ++q) s[q] += r[q];
       }
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(TEAM > MS_WAVE ? TEAM : kNormNT) void k_rms_norm(No
     };
     if (a.sum)
       turns([&](int c, const float (&v)[Q], const float (&)[Q]) {
-        if (c < d) store_cols<T, Q>(sum + c, d - c, v);
+        if (c < d) store_row<T, Q>(sum + c, d - c, v);
       });
     scale = norm_scale<TEAM>(
         [&](auto f) {
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(TEAM > MS_WAVE ? TEAM : kNormNT) void k_rms_norm(No
       turns([&](int c, const float (&v)[Q], const float (&wv)[Q]) {
         float y[Q];
         normed(v, wv, y);
-        if (c < d) store_cols<T, Q>(out + c, d - c, y);
+        if (c < d) store_row<T, Q>(out + c, d - c, y);
       });
     } else {
       const int64_t slot = a.slots ? (int64_t)a.slots[i] : i;
@@ -286,9 +286,9 @@ __global__ __launch_bounds__(TEAM > MS_WAVE ? TEAM : kNormNT) void k_rms_norm_ba
 #pragma unroll
         for (int q = 0; q < Q; ++q) s_of[u][t][q] = dy_of[u][t][q] = ds_of[u][t][q] = 0.0f;
         if (i < a.rows && c < d) {
-          load_cols<T, Q>(s_at + u * s_on + c, d - c, s_of[u][t]);
-          load_cols<T, Q>(dy_at + u * dy_on + c, d - c, dy_of[u][t]);
-          if (a.ds) load_cols<T, Q>(ds_at + u * ds_on + c, d - c, ds_of[u][t]);
+          load_row<T, Q>(s_at + u * s_on + c, d - c, s_of[u][t]);
+          load_row<T, Q>(dy_at + u * dy_on + c, d - c, dy_of[u][t]);
+          if (a.ds) load_row<T, Q>(ds_at + u * ds_on + c, d - c, ds_of[u][t]);
         }
       }
     }
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(TEAM > MS_WAVE ? TEAM : kNormNT) void k_rms_norm_ba
           const int c = t * kTurn + lane * Q;
           float v[Q];
           back(dy[t], s[t], ds[t], v);
-          if (c < d) store_cols<T, Q>(dxr + c, d - c, v);
+          if (c < d) store_row<T, Q>(dxr + c, d - c, v);
         }
         if constexpr (kLong)
           beyond([&](int c, const float (&n)[Q], const float (&g)[Q], const float (&v)[Q]) {
