@@ -10,8 +10,8 @@
 // Bound by memory, in bf16 without a residual by the generator's ten rounds (20
 // products of 32 by 32 bits a block: about 1.2 T words/s over the chip).
 // Measured: 242K x 256 bf16 53 to 58 us (4.3 to 4.7 TB/s), with the residual 66
-// (5.6); 110K x 1024 fp32 143 (6.3); 854K x 100 bf16 94 to 102 us (147 with a team of lanes a row,
-// three in sixteen of them idle).
+// (5.6); 110K x 1024 fp32 143 (6.3); 854K x 100 bf16 94 to 102 (147 with a team of
+// lanes a row, three in sixteen of them idle).
 #pragma once
 
 #include "common.hpp"

@@ -108,8 +108,8 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_tile(Gated<T> a, int tiles
 
 // Few rows: 32 rows by 32 outputs of both halves a block, its eight waves share
 // the reduction. Bound by the trips to memory that follow each other: a wave makes
-// an eighth of those that a tile makes. 250 x 256 ->
-// 1024 fp32 12.1 us where narrow tiles take 22.7.
+// an eighth of those that a tile makes. 250 x 256 -> 1024 fp32 12.1 us where
+// narrow tiles take 22.7.
 template <typename T>
 __global__ __launch_bounds__(kFewNT) void k_gated_few(Gated<T> a, int tiles_n) {
   __shared__ float halves[2][32 * 32];
@@ -162,9 +162,9 @@ __global__ __launch_bounds__(kGateNT) void k_gated_dz(GatedDz<T> a) {
       for (int v = 0; v < kAhead; ++v) {
         const int64_t i = i0 + v * kGateWays;
         if (i >= end) continue;
-        load_cols<T, kV>(a.dy + i * a.dy_stride + c, valid, dy[v]);
-        load_cols<T, kV>(a.pre + i * a.pre_stride + c, valid, g[v]);
-        load_cols<T, kV>(a.pre + i * a.pre_stride + a.n + c, valid, u[v]);
+        load_row<T, kV>(a.dy + i * a.dy_stride + c, valid, dy[v]);
+        load_row<T, kV>(a.pre + i * a.pre_stride + c, valid, g[v]);
+        load_row<T, kV>(a.pre + i * a.pre_stride + a.n + c, valid, u[v]);
       }
 #pragma unroll
       for (int v = 0; v < kAhead; ++v) {
