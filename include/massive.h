@@ -433,9 +433,9 @@ int massive_dropout(const massive_dropout_args* args, void* stream);
  * (fmt->d = d), y is a table of table_rows packed rows as massive_pack_rows
  * writes them, row i of the norm going to row slots[i], or to row i if slots is
  * NULL; y_stride is ignored. An eps between 0 and 2^-126 counts as 2^-126. Rows
- * whose squares leave fp32's range are normed all the same; a row of zeros with
- * an eps of 0 is NaN, and in a row with an infinity the finite values give 0
- * and the infinities NaN. */
+ * whose squares leave fp32's range are normed all the same; a row with a NaN is
+ * NaN, as a row of zeros with an eps of 0 is, and in a row with an infinity the
+ * finite values give 0 and the infinities NaN. */
 typedef struct {
   const void* x;        /* [rows, d]                                          */
   const void* residual; /* [rows, d] or NULL                                  */

@@ -91,8 +91,9 @@ __device__ __forceinline__ NormScale norm_scale(E each, float inv_d, float eps) 
   // squares too large or too small for fp32, or not finite: again, by the largest magnitude's power of two
   uint32_t bits = 0;
   each([&](float s) { bits = max(bits, __float_as_uint(s) & 0x7FFFFFFFu); });
-  const float most = fmaxf(__uint_as_float(norm_max<TEAM>(bits)), sqrtf(eps));
-  if (!(most < __builtin_inff())) return {most == __builtin_inff() ? 0.0f : __builtin_nanf(""), 0};
+  const float largest = __uint_as_float(norm_max<TEAM>(bits));  // (a NaN's bits are above all others)
+  if (!(largest < __builtin_inff())) return {largest == __builtin_inff() ? 0.0f : __builtin_nanf(""), 0};
+  const float most = fmaxf(largest, sqrtf(eps));
   if (most == 0.0f) return {__builtin_inff(), 0};
   int e;
   frexpf(most, &e);
