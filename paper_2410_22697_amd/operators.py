@@ -554,8 +554,6 @@ def _rms_norm(x, weight, eps, residual, fmt, out, slots):
         raise ValueError("x has %d rows, and there are %d slots" % (rows, slots.numel()))
     table_rows = 0
     if fmt is None:
-        if out is not None or slots is not None:
-            raise ValueError("out and slots are for packed rows, which fmt asks for")
         y = _like(x)
     else:
         if fmt.d != d:
@@ -611,8 +609,10 @@ def rms_norm(x, weight=None, eps: float = 1e-6, residual=None, fmt: Optional[Row
     to `out`, its rows slots[i] or its first ones; packed rows have no gradient,
     and tensors that ask for one are refused."""
     _no_tangent(x, weight, residual)
+    if fmt is None and (out is not None or slots is not None):
+        raise ValueError("out and slots are for packed rows, which fmt asks for")
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, residual)):
-        if fmt is not None or out is not None:
+        if fmt is not None:
             raise ValueError("packed rows have no gradient, and a tensor requires one")
         return _RmsNorm.apply(x, weight, eps, residual)
     y, total = _rms_norm(x, weight, eps, residual, fmt, out, slots)
