@@ -393,12 +393,24 @@ __device__ __forceinline__ void tile_product_direct(A& first, B& second, const T
   __syncthreads();
 }
 
+// Keeps a wave's memory reads and writes before it and behind it on their sides
+// (other instructions may pass: with none passing, silu's gradients in bf16 spill
+// three registers).
+__device__ __forceinline__ void tile_in_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(1);
+}
+
 // The same for a second operand that the threads compute as they put it. The
 // first's steps come directly, two ahead; the second's through registers, three
 // ahead, in two sets, and a thread puts its part of a step a step ahead. What a
 // wave asks for arrives in the order of asking, a step's part of the first
 // before the next but one's of the second: so much may be left when a step is
-// multiplied (kLeft) and when the next is put (kLeftPut).
+// multiplied (kLeft) and when the next is put (kLeftPut). Both counts hang on
+// that order of asking, which is why it is not left to the compiler
+// (tile_in_order()): a read for the second that overtook the first's would leave
+// a buffer on its way when it is multiplied. (What put() stores is in the queue
+// too, ahead of what is asked for behind it, and makes a wait longer at most.)
 template <typename T, int NB, typename A, typename B>
 constexpr int tile_made_lds() {
   return 3 * A::kBytes + 2 * B::kBytes;
@@ -432,7 +444,7 @@ __device__ __forceinline__ void tile_product_made(A& first, B& second, int64_t K
   };
   const std::integral_constant<int, 0> even;
   const std::integral_constant<int, 1> odd;
-  auto step = [&](int s, auto now, auto next) {  // any step
+  auto step = [&](int s, auto now, auto next) {  // any step: waits for all, so no count hangs on its order
     tile_arrived<0>();
     tile_barrier();
     if (s + 1 < steps) put(next, std::false_type());
@@ -447,6 +459,7 @@ __device__ __forceinline__ void tile_product_made(A& first, B& second, int64_t K
     put(next, std::true_type());
     first.direct(lds + to);
     to = after(to);
+    tile_in_order();
     second.template whole<next()>();
     multiply(now);
   };
