@@ -494,7 +494,9 @@ int massive_gated(const massive_gated_args* args, void* stream);
  * (columns of x and x2 apart), dw = [dg | du]^T [x | x2], dbias = sum of
  * [dg | du] over the rows. dx, dx_second, dw and dbias may each be NULL. With
  * MASSIVE_BF16, dg and du are rounded to bf16 before the products dx and dw,
- * as massive_linear_backward rounds dz; dbias sums them unrounded. */
+ * as massive_linear_backward rounds dz; dbias sums them unrounded. The order of
+ * the sums goes by the sizes, that of dx's also by which of dx and dx_second are
+ * asked for, and not by where the arrays lie. */
 typedef struct {
   const void *dy, *pre, *x, *x_second, *w;
   void *dx, *dx_second, *dw, *dbias;

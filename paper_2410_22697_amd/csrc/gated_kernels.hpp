@@ -363,13 +363,14 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(GatedDw<T> a, int64_t b
   dw_out<T, NB>(a, lds, acc, part, k0, [&](int p) { return n0 + p < kLast ? tile_column<T>(n0 + p, a.n) : a.n; });
 }
 
-// [dg | du] as an operand across k, made from dy and pre on its way to LDS: 64
-// columns of dg and the same of du, a unit of both a thread and step. It can
-// leave dz behind, and each thread adds up its columns before they are rounded.
-template <typename T, int ACT>
+// [dg | du] as an operand across k, made from dy and pre on its way to LDS: COLS
+// columns of dg and the same of du, a unit (or W of its columns) of both a thread
+// and step. It can leave dz behind, and each thread adds up its columns before
+// they are rounded.
+template <typename T, int ACT, int COLS = 64, int W = 16 / sizeof(T)>
 struct TileGates {
-  static constexpr int kV = 16 / sizeof(T), kUnits = 64 / kV, kPitch = 128 * sizeof(T), kBytes = tile_step<T>() * kPitch;
-  static_assert(kTileNT / kUnits == tile_step<T>(), "");
+  static constexpr int kCols = COLS, kV = 16 / sizeof(T), kUnits = COLS / W, kNT = kUnits * tile_step<T>(), kPitch = 2 * COLS * sizeof(T), kBytes = tile_step<T>() * kPitch;
+  typedef cols_t<T, W> unit_t;
   const T *dy, *pre;
   T* dz;
   int64_t dy_stride, pre_stride;
@@ -379,13 +380,14 @@ struct TileGates {
   static constexpr int kAsked = 3;
   bool live[2];
   int64_t at[2];
-  u32x4 vd[2], vg[2], vu[2];
-  float sums[2][kV] = {};
+  typedef uint32_t raw __attribute__((ext_vector_type(W * sizeof(T) / 4)));
+  raw vd[2], vg[2], vu[2];
+  float sums[2][W] = {};
 
-  static __device__ __forceinline__ u32x4 read(const T* p) { return __builtin_bit_cast(u32x4, *reinterpret_cast<const cols_t<T, kV>*>(p)); }
+  static __device__ __forceinline__ raw read(const T* p) { return __builtin_bit_cast(raw, *reinterpret_cast<const unit_t*>(p)); }
   // rows from `row` on, columns from n0 on (as TileAcross has them)
   __device__ __forceinline__ void begin(const GatedDz<T>& a, int64_t row, int n0) {
-    const int c = min(n0 + (int)threadIdx.x % kUnits * kV, a.n - kV);
+    const int s = threadIdx.x % kUnits * W, c = min(n0 + s / kV * kV, a.n - kV) + s % kV;
     row += threadIdx.x / kUnits;
     n = a.n;
     dy_stride = a.dy_stride;
@@ -417,42 +419,88 @@ struct TileGates {
     const int64_t unit = k0 + (r - in);
     const int skip = K >= kV ? skipped<T>(unit, K) : (unit + in < K ? 0 : kV);
     live[SET] = in >= skip;
-    vd[SET] = vg[SET] = vu[SET] = (u32x4)0u;
+    vd[SET] = vg[SET] = vu[SET] = (raw)0u;
     if (live[SET]) ask<SET>(skip && K >= kV ? K - kV - unit : 0);
     go_on();
   }
-  // WHOLE: the step has all rows
-  template <int SET, bool WHOLE>
-  __device__ __forceinline__ void put(char* to) {
-    typedef cols_t<T, kV> unit_t;
+  // (an addition of its own, never one with the product that v may be: the kernels that sum have the same bits)
+  static __device__ __forceinline__ void add(float& sum, float v) {
+#pragma clang fp contract(off)
+    sum += v;
+  }
+  // a step's dg and du, which join the sums
+  template <int SET>
+  __device__ __forceinline__ void make(unit_t (&z)[2]) {
     const unit_t d = __builtin_bit_cast(unit_t, vd[SET]), g = __builtin_bit_cast(unit_t, vg[SET]), u = __builtin_bit_cast(unit_t, vu[SET]);
-    unit_t z[2];
 #pragma unroll
-    for (int q = 0; q < kV; ++q) {
+    for (int q = 0; q < W; ++q) {
       const float dy_u = (float)d[q] * (float)u[q];
       const float dg = ACT == kActNone ? dy_u : act_grad(dy_u, (float)g[q], ACT), du = (float)d[q] * act_value((float)g[q], ACT);
-      sums[0][q] += dg;  // (of zeros where the step has no row)
-      sums[1][q] += du;
+      add(sums[0][q], dg);  // (of zeros where the step has no row)
+      add(sums[1][q], du);
       z[0][q] = (T)dg;
       z[1][q] = (T)du;
     }
+  }
+  // leaves them behind; WHOLE: the step has all rows
+  template <int SET, bool WHOLE>
+  __device__ __forceinline__ void leave(const unit_t (&z)[2]) {
+    if (!dz) return;
+    if (WHOLE || live[SET]) {
+      T* p = WHOLE ? dz : dz + at[SET] * (2 * (int64_t)n);
+      *reinterpret_cast<unit_t*>(p) = z[0];
+      *reinterpret_cast<unit_t*>(p + n) = z[1];
+    }
+    dz += tile_step<T>() * (2 * (int64_t)n);
+  }
+  template <int SET, bool WHOLE>
+  __device__ __forceinline__ void put(char* to) {
+    static_assert(W == kV && kNT == kTileNT, "");
+    unit_t z[2];
+    make<SET>(z);
     const int r = threadIdx.x / kUnits, s = threadIdx.x % kUnits;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int place = h * kUnits + s;
       *reinterpret_cast<u32x4*>(to + r * kPitch + ((place / 2 ^ r % 4) * 2 + place % 2) * 16) = __builtin_bit_cast(u32x4, z[h]);
     }
-    if (dz) {
-      if (WHOLE || live[SET]) {
-        T* p = WHOLE ? dz : dz + at[SET] * (2 * (int64_t)n);
-        *reinterpret_cast<unit_t*>(p) = z[0];
-        *reinterpret_cast<unit_t*>(p + n) = z[1];
-      }
-      dz += tile_step<T>() * (2 * (int64_t)n);
-    }
+    leave<SET, WHOLE>(z);
   }
-  static __device__ __forceinline__ u32x4 fragment(const char* from, int c0, int s) { return TileAcross<T, 128>::fragment(from, c0, s); }
+  static __device__ __forceinline__ u32x4 fragment(const char* from, int c0, int s) { return TileAcross<T, 2 * COLS>::fragment(from, c0, s); }
 };
+
+// The output at each position of a block's COLS of both halves, from column n0 on
+// (2 n: none).
+template <typename T, int COLS>
+__device__ __forceinline__ auto gates_rows(int n0, int n) {
+  const int last = round_up_to<16 / (int)sizeof(T)>(n);
+  return [=](int p) {
+    const int c = n0 + p % COLS;
+    return c < last ? p / COLS * n + tile_column<T>(c, n) : 2 * n;
+  };
+}
+// db's sums of a part of the rows, or db if there is one: the threads that share
+// columns add up in order. `lds` holds tile_step() rows of 2 COLS floats.
+template <typename T, typename B, typename F>
+__device__ __forceinline__ void gates_sums(const B& dzs, const GatedDw<T>& a, char* lds, int64_t part, F row_at) {
+  float* joined = reinterpret_cast<float*>(lds);
+  constexpr int kCols = B::kCols, kW = kCols / B::kUnits;
+  const int r = threadIdx.x / B::kUnits, c = threadIdx.x % B::kUnits * kW;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int q = 0; q < kW; ++q) joined[(r * 2 + h) * kCols + c + q] = dzs.sums[h][q];
+  __syncthreads();
+  const int row = (int)threadIdx.x < 2 * kCols ? row_at(threadIdx.x) : a.n;
+  if (row < a.n) {
+    float t = 0.0f;
+#pragma unroll
+    for (int g = 0; g < tile_step<T>(); ++g) t += joined[g * (2 * kCols) + threadIdx.x];
+    if (a.sums) a.sums[part * a.n + row] = t;
+    else a.db[row] = (T)t;
+  }
+  __syncthreads();
+}
 
 // dw and the sums for db, of dz as TileGates makes it: one launch that reads dy
 // and pre once, for inputs of whole units in one tile of columns. Bound by the
@@ -464,7 +512,6 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(GatedDw<T> a, Gate
   typedef TileAcross<T, 64 * NB> A;
   typedef TileGates<T, ACT> B;
   typedef TileTurn<float, 32 * NB> Turn;
-  constexpr int kV = 16 / sizeof(T);
   constexpr int kMade = tile_made_lds<T, NB, A, B>(), kLds = kMade > 4 * Turn::kBytes ? kMade : 4 * Turn::kBytes;
   static_assert(kLds >= tile_step<T>() * 128 * (int)sizeof(float), "");
   __shared__ __align__(16) char lds[kLds];
@@ -484,31 +531,62 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw_made(GatedDw<T> a, Gate
   });
   dzs.begin(z, from, n0);
   tile_product_made<T, NB>(xs, dzs, rows, lds, acc);
-  const int last = round_up_to<kV>(z.n);
-  auto row_at = [&](int p) {
-    const int c = n0 + p % 64;
-    return c < last ? p / 64 * z.n + tile_column<T>(c, z.n) : a.n;
-  };
-  if (a.db) {
-    // the threads that share columns add up in order
-    float* joined = reinterpret_cast<float*>(lds);
-    const int r = threadIdx.x / B::kUnits, c = threadIdx.x % B::kUnits * kV;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int q = 0; q < kV; ++q) joined[r * 128 + h * 64 + c + q] = dzs.sums[h][q];
-    __syncthreads();
-    const int row = (int)threadIdx.x < 128 ? row_at(threadIdx.x) : a.n;
-    if (row < a.n) {
-      float t = 0.0f;
-#pragma unroll
-      for (int g = 0; g < tile_step<T>(); ++g) t += joined[g * 128 + threadIdx.x];
-      if (a.sums) a.sums[part * a.n + row] = t;
-      else a.db[row] = (T)t;
-    }
-    __syncthreads();
-  }
+  const auto row_at = gates_rows<T, 64>(n0, z.n);
+  if (a.db) gates_sums(dzs, a, lds, part, row_at);
   dw_out<T, NB>(a, lds, acc, part, 0, row_at);
+}
+
+// dz and the sums for db alone, as k_gated_dw_made has them, for its sizes where
+// it is not taken (dw is not asked for, or x lies where it cannot go to LDS
+// directly): db then has the same bits whichever of the two makes it. Half a unit
+// a thread, so that twice the waves share a CU: slopes take as long as memory.
+// Whole lines of 256 bytes a block's row (of 128, 40 us more at the first size).
+// us, this / k_gated_dz and its join: db alone, 110K x 1024 bf16 127 / 141; with
+// dx, 110K x 256 -> 1024 404 / 383, 110K x 64 -> 512 172 / 172; 40K x 128 -> 64 all
+// gradients 36 / 51; 27.5K x 128 -> 1024 fp32 404 / 402.
+constexpr int kSumsCols = 128, kSumsNT = 1024;
+template <typename T, int ACT>
+__global__ __launch_bounds__(kSumsNT) void k_gated_sums(GatedDw<T> a, GatedDz<T> z, int groups, int64_t blocks) {
+  constexpr int kStep = tile_step<T>();
+  typedef TileGates<T, ACT, kSumsCols, 8 / sizeof(T)> B;
+  static_assert(B::kNT == kSumsNT, "");
+  __shared__ __align__(16) char lds[kStep * 2 * kSumsCols * sizeof(float)];
+  const int64_t tile = tile_of_block(blockIdx.x, blocks);
+  const int64_t part = tile / groups;
+  const int n0 = (int)(tile % groups) * kSumsCols;
+  const int64_t from = part * a.part, rows = min(a.part, a.rows - from);
+  B dzs;
+  dzs.begin(z, from, n0);
+  const int64_t whole = rows / kStep, steps = whole + (rows % kStep ? 1 : 0);
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> odd;
+  auto ask = [&](int64_t s, auto set) {
+    if (s < whole) dzs.template whole<set()>();
+    else if (s < steps) dzs.template ragged<set()>(s * kStep, rows);
+  };
+  auto make = [&](auto set, auto all) {
+    typename B::unit_t made[2];
+    dzs.template make<set()>(made);
+    dzs.template leave<set(), all()>(made);
+  };
+  ask(0, even);
+  ask(1, odd);
+  int64_t s = 0;
+#pragma unroll 1
+  for (; s + 3 < whole; s += 2) {
+    make(even, std::true_type());
+    dzs.template whole<even()>();
+    make(odd, std::true_type());
+    dzs.template whole<odd()>();
+  }
+#pragma unroll 1
+  for (; s < steps; s += 2) {
+    make(even, std::false_type());
+    ask(s + 2, even);
+    if (s + 1 < steps) make(odd, std::false_type());
+    ask(s + 3, odd);
+  }
+  gates_sums(dzs, a, lds, part, gates_rows<T, kSumsCols>(n0, z.n));
 }
 
 // Adds parts of arrays of rows, four values a thread, WAYS threads a value, each

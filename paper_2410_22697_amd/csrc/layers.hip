@@ -240,27 +240,26 @@ int gated(const massive_gated_args* a, void* stream) {
   return launch(what, k_gated_few<T>, cdiv(a->rows, 32) * tiles_n, kFewNT, 0, stream, f, tiles_n);
 }
 
-// dw's tiles and the parts of its rows: as many blocks as the chip holds at a
-// time, none of less than eight steps of rows (four in fp32, whose steps last
-// longer) where there are more. `made`: dz
-// is made on its way into the product, 64 outputs of both halves a tile.
+// dw's tiles (128 outputs of both halves; made on the way, 64 of each) and the
+// parts of its rows: as many blocks as the chip holds at a time, none of less
+// than eight steps of rows (four in fp32, whose steps last longer) where there
+// are more.
 struct GatedDwPlan {
   int nb, second;
-  int64_t tiles_n, tiles_k, part, parts, floats, sums;  // floats, sums: of parts, none of a single one
+  int64_t tiles_n, tiles_k, part, parts, floats;  // floats: of the parts, none of a single one
 };
-GatedDwPlan gated_dw_plan(const massive_gated_grads* a, bool made) {
+GatedDwPlan gated_dw_plan(const massive_gated_grads* a) {
   GatedDwPlan p;
   const int vector = 16 / size_of(a->type), step = kTileStepBytes / size_of(a->type);
   p.second = (int)round_up(a->k, vector);
   const int64_t cols = p.second + a->k_second, n = 2 * (int64_t)a->n;
   p.nb = cols <= 128 ? 2 : 4;
-  p.tiles_n = made ? cdiv(a->n, 64) : cdiv(n, kTileSecond);
+  p.tiles_n = cdiv(n, kTileSecond);
   p.tiles_k = cdiv(cols, 64 * p.nb);
   const int64_t most = std::max<int64_t>(1, cdiv(a->rows, (a->type == MASSIVE_F32 ? 4 : 8) * step));
   p.part = std::max<int64_t>(1, round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, 512 / (p.tiles_n * p.tiles_k)))), step));
   p.parts = cdiv(a->rows, p.part);
   p.floats = a->dw && p.parts > 1 ? p.parts * n * ((int64_t)a->k + a->k_second) : 0;
-  p.sums = made && a->dbias && p.parts > 1 ? p.parts * n : 0;
   return p;
 }
 
@@ -293,25 +292,26 @@ GatedDxPlan gated_dx_plan(const massive_gated_grads* a) {
 }
 
 // The backward pass's workspace: dz, the parts of db, those of dw or, later, of
-// dx. It has room for both ways to dw, of which the arrays' alignment chooses
-// one.
+// dx. It has room for dz also where dw is all that is asked for and dz may never
+// be written: that hangs on where x lies, which its size does not.
 struct GatedPlan {
   int64_t groups, part, parts, sums_at, dw_at, bytes;
-  GatedDwPlan dw, made;
+  bool in_units;  // sizes for which dz can be made on its way into dw; db is summed in that way's order then, by any way
+  GatedDwPlan dw;
   GatedDxPlan dx;
 };
 GatedPlan gated_plan(const massive_gated_grads* a) {
   GatedPlan p;
-  const int size = size_of(a->type);
-  p.groups = cdiv(a->n, kGateUnits * (16 / size));
+  const int size = size_of(a->type), vector = 16 / size;
+  p.groups = cdiv(a->n, kGateUnits * vector);
   p.part = std::max<int64_t>(1, cdiv(a->rows, std::max<int64_t>(1, std::min(cdiv(a->rows, 4 * kGateWays), 2048 / std::min<int64_t>(2048, p.groups)))));
   p.parts = cdiv(a->rows, p.part);
-  p.dw = gated_dw_plan(a, false);
-  p.made = gated_dw_plan(a, true);
+  p.dw = gated_dw_plan(a);
+  p.in_units = a->k % vector == 0 && a->k_second % vector == 0 && a->n >= vector && p.dw.tiles_k == 1;
   p.sums_at = a->dx || a->dx_second || a->dw ? round_up(a->rows * 2 * a->n * size, 16) : 0;
-  p.dw_at = p.sums_at + (a->dbias ? round_up(std::max(p.parts * 2 * a->n, p.made.sums) * 4, 16) : 0);
+  p.dw_at = p.sums_at + (a->dbias ? round_up((p.in_units ? p.dw.parts : p.parts) * 2 * a->n * 4, 16) : 0);
   p.dx = gated_dx_plan(a);
-  p.bytes = p.dw_at + std::max(std::max(p.dw.floats, p.made.floats), p.dx.floats) * 4;
+  p.bytes = p.dw_at + std::max(p.dw.floats, p.dx.floats) * 4;
   return p;
 }
 
@@ -339,16 +339,17 @@ int with_act_of(int act, F f) {
   }
 }
 
-// Adds up parts, by as many threads a value as fill the chip (us, one / sixteen: 33
-// parts of 524K values 14-18 / 19; all gradients with 250 parts of 8K 90 / 34).
+// Adds up parts, by as many threads a value as fill the chip where there are
+// `values` of them (us, one / sixteen: 33 parts of 524K values 14-18 / 19; all
+// gradients with 250 parts of 8K 90 / 34).
 template <typename T>
-int gated_join(const GatedJoin<T>& j, void* stream) {
+int gated_join(const GatedJoin<T>& j, int64_t values, void* stream) {
   auto ways = [&](auto w) {
     constexpr int kValues = kGateNT / w() * 4;
     return launch("massive_gated_backward", k_gated_join<T, w()>, cdiv(j.values[0], kValues) + cdiv(j.values[1], kValues), kGateNT, 0, stream, j);
   };
-  if (j.count <= 2 || j.values[0] >= 1 << 19) return ways(std::integral_constant<int, 1>());
-  return j.values[0] >= 1 << 17 ? ways(std::integral_constant<int, 4>()) : ways(std::integral_constant<int, 16>());
+  if (j.count <= 2 || values >= 1 << 19) return ways(std::integral_constant<int, 1>());
+  return values >= 1 << 17 ? ways(std::integral_constant<int, 4>()) : ways(std::integral_constant<int, 16>());
 }
 
 // dz and db by themselves.
@@ -398,12 +399,12 @@ int gated_dx(const massive_gated_grads* a, const GatedPlan& p, char* workspace, 
   j.split = k0;
   j.beyond = f.dx[1];
   j.beyond_stride = a->dx_second_stride;
-  return gated_join(j, stream);
+  return gated_join(j, j.values[0], stream);
 }
 
 // The joins of dw and db, each if there are any.
 template <typename T>
-GatedJoin<T> dw_join(const massive_gated_grads* a, const float* dw, const float* db, int64_t parts) {
+int dw_join(const massive_gated_grads* a, const float* dw, const float* db, int64_t parts, void* stream) {
   GatedJoin<T> j = {};
   const int cols = a->k + a->k_second, n = 2 * a->n;
   j.parts[0] = dw;
@@ -416,7 +417,7 @@ GatedJoin<T> dw_join(const massive_gated_grads* a, const float* dw, const float*
   j.count = parts;
   j.cols[0] = j.split = cols;
   j.cols[1] = n;
-  return j;
+  return gated_join(j, (int64_t)n * cols, stream);  // (db's order does not hang on whether dw is there)
 }
 
 template <typename T>
@@ -425,30 +426,37 @@ int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* works
   constexpr int kV = 16 / sizeof(T);
   const bool dx = a->dx || a->dx_second;
   const bool units = a->k % kV == 0 && a->k_second % kV == 0 && in_units<T>(a->x, a->x_stride) && in_units<T>(a->x_second, a->x_second_stride);
-  const bool made = a->dw && units && a->n >= kV && p.made.tiles_k == 1;
-  if (!made)
+  const bool made = a->dw && units && p.in_units, sums = !made && a->dbias && p.in_units;
+  const GatedDwPlan& d = p.dw;
+  const bool several = d.parts > 1;
+  const int n = 2 * a->n;
+  GatedDw<T> f;
+  f.dz = rows_of<T>(workspace, n, a->rows, n);
+  f.x[0] = rows_of<T>(a->x, a->x_stride, a->rows, a->k);
+  f.x[1] = rows_of<T>(a->x_second, a->x_second_stride, a->rows, a->k_second);
+  f.parts = several && a->dw ? (float*)(workspace + p.dw_at) : nullptr;
+  f.sums = several && a->dbias && p.in_units ? (float*)(workspace + p.sums_at) : nullptr;
+  f.dw = (T*)a->dw;
+  f.db = (T*)a->dbias;
+  f.dw_stride = a->dw_stride;
+  f.rows = a->rows;
+  f.part = d.part;
+  f.n = n;
+  f.k[0] = a->k;
+  f.k[1] = a->k_second;
+  f.second = d.second;
+  f.tiles_n = (int)d.tiles_n;
+  f.tiles_k = (int)d.tiles_k;
+  if (sums) {
+    const int64_t groups = cdiv(a->n, kSumsCols), blocks = d.parts * groups;
+    const int rc = with_act_of(a->act, [&](auto act) {
+      return launch(what, k_gated_sums<T, act()>, blocks, kSumsNT, 0, stream, f, gates_of<T>(a, dx || a->dw ? workspace : nullptr), (int)groups, blocks);
+    });
+    if (rc) return rc;
+  } else if (!made) {
     if (int rc = gated_dz<T>(a, p, workspace, stream)) return rc;
+  }
   if (a->dw) {
-    const int n = 2 * a->n;
-    const GatedDwPlan& d = made ? p.made : p.dw;
-    const bool several = d.parts > 1;
-    GatedDw<T> f;
-    f.dz = rows_of<T>(workspace, n, a->rows, n);
-    f.x[0] = rows_of<T>(a->x, a->x_stride, a->rows, a->k);
-    f.x[1] = rows_of<T>(a->x_second, a->x_second_stride, a->rows, a->k_second);
-    f.parts = several ? (float*)(workspace + p.dw_at) : nullptr;
-    f.sums = several && made && a->dbias ? (float*)(workspace + p.sums_at) : nullptr;
-    f.dw = (T*)a->dw;
-    f.db = made ? (T*)a->dbias : nullptr;
-    f.dw_stride = a->dw_stride;
-    f.rows = a->rows;
-    f.part = d.part;
-    f.n = n;
-    f.k[0] = a->k;
-    f.k[1] = a->k_second;
-    f.second = d.second;
-    f.tiles_n = (int)d.tiles_n;
-    f.tiles_k = (int)d.tiles_k;
     const int64_t blocks = d.parts * d.tiles_n * d.tiles_k;
     auto tile = [&](auto nb) {
       if (made)
@@ -458,9 +466,9 @@ int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* works
       return launch(what, units && n % kV == 0 ? k_gated_dw<T, nb(), true> : k_gated_dw<T, nb(), false>, blocks, kTileNT, 0, stream, f, blocks);
     };
     if (int rc = d.nb == 2 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
-    if (several)
-      if (int rc = gated_join(dw_join<T>(a, f.parts, f.sums, d.parts), stream)) return rc;
   }
+  if (f.parts || f.sums)
+    if (int rc = dw_join<T>(a, f.parts, f.sums, d.parts, stream)) return rc;
   return dx ? gated_dx<T>(a, p, workspace, stream) : MASSIVE_OK;
 }
 
@@ -579,7 +587,7 @@ int massive_gated_backward(const massive_gated_grads* a, void* workspace, int64_
   for (const void* p : {a->dy, a->pre, a->x, a->x_second, a->w, (const void*)a->dx, (const void*)a->dx_second, (const void*)a->dw, (const void*)a->dbias})
     if (!aligned(p, size)) REFUSE("an array is not aligned");
   const GatedPlan p = gated_plan(a);
-  const int64_t dw_blocks = std::max(p.dw.parts * p.dw.tiles_n * p.dw.tiles_k, p.made.parts * p.made.tiles_n * p.made.tiles_k);
+  const int64_t dw_blocks = p.dw.parts * p.dw.tiles_n * p.dw.tiles_k;
   if (p.groups * p.parts > kMostBlocks || (a->dw && (dw_blocks > kMostBlocks || cdiv(2 * a->n * k, 4 * kGateNT) + (1 << 15) > kMostBlocks)) ||
       cdiv(a->rows, kTileSecond) * cdiv(k, 128) > kMostBlocks)
     REFUSE("too many rows and columns for one call");
@@ -587,7 +595,7 @@ int massive_gated_backward(const massive_gated_grads* a, void* workspace, int64_
     if (!a->dw && !a->dbias) return MASSIVE_OK;
     // the pointers only say which of the two are asked for: with no parts nothing is read
     const float *dw = (const float*)a->dw, *db = (const float*)a->dbias;
-    return a->type == MASSIVE_F32 ? gated_join(dw_join<float>(a, dw, db, 0), stream) : gated_join(dw_join<bf16>(a, dw, db, 0), stream);
+    return a->type == MASSIVE_F32 ? dw_join<float>(a, dw, db, 0, stream) : dw_join<bf16>(a, dw, db, 0, stream);
   }
   if (!workspace || workspace_bytes < p.bytes)
     return call_error(MASSIVE_ECAPACITY, "workspace of %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)p.bytes);
