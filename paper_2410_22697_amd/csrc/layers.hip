@@ -76,12 +76,16 @@ int with_norm(int64_t d, F f) {
   const integral_constant<int, MS_WAVE> wave;
   if (d <= 2 * MS_WAVE * Q) return f(wave, two);
   if (d <= 4 * MS_WAVE * Q) return f(wave, integral_constant<int, 4>());
-  if constexpr (Q == 4)
-    if (d <= 8 * MS_WAVE * Q) return f(wave, integral_constant<int, 8>());
   const integral_constant<int, kNormLong> block;
-  if (d <= kNormLong * Q) return f(block, one);
-  if constexpr (GRADS && Q == 8) return f(integral_constant<int, 2 * kNormLong>(), one);
-  else return f(block, two);
+  if constexpr (Q == 4) {
+    static_assert(kNormLong <= 8 * MS_WAVE, "a block's first turn has no columns that a wave's eight have not");
+    if (d <= 8 * MS_WAVE * Q) return f(wave, integral_constant<int, 8>());
+    return f(block, two);
+  } else {
+    if (d <= kNormLong * Q) return f(block, one);
+    if constexpr (GRADS) return f(integral_constant<int, 2 * kNormLong>(), one);
+    else return f(block, two);
+  }
 }
 
 constexpr int64_t kNormBlocks = 8192;      // a block takes several rows: it reads the weights once
