@@ -13,14 +13,13 @@
 #include "../../include/massive.h"
 #include "call_error.hpp"
 #include "common.hpp"
+#include "launch_rules.hpp"
 #include "values.hpp"
 
 namespace ms {
 
 constexpr int64_t kMostBlocks = 1 << 23;  // of a launch: 256 threads each stay below 2^32 in all
 
-inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline int64_t round_up(int64_t a, int64_t b) { return cdiv(a, b) * b; }
 
 #define REFUSE(...) return ms::call_error(MASSIVE_EINVAL, __VA_ARGS__)
 

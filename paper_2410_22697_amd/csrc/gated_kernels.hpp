@@ -8,6 +8,7 @@
 // and the product need no other pass over memory.
 #pragma once
 
+#include "gated_rules.hpp"
 #include "linear_few.hpp"
 #include "linear_kernels.hpp"
 #include "tile_product.hpp"
@@ -131,9 +132,6 @@ __global__ __launch_bounds__(kFewNT) void k_gated_few(Gated<T> a, int tiles_n) {
 }
 
 // ------------------------------------------------------------------ gradients
-constexpr int kGateNT = 256;
-constexpr int kGateUnits = 32;  // units of 16 bytes of a row that a block takes
-constexpr int kGateWays = kGateNT / kGateUnits;
 
 template <typename T>
 struct GatedDz {

@@ -7,6 +7,9 @@
 
 namespace ms {
 
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t round_up(int64_t a, int64_t b) { return cdiv(a, b) * b; }
+
 // How the blocks of a single-pass scan take their tiles. A tile waits for the
 // tiles before it. In block order it could wait for ever if other launches kept
 // those off the chip for good, which only other scans can do, as their blocks

@@ -12,6 +12,7 @@
 #include "call_launch.hpp"
 #include "dropout_kernels.hpp"
 #include "gated_kernels.hpp"
+#include "gated_rules.hpp"
 #include "norm_kernels.hpp"
 
 namespace {
@@ -196,22 +197,6 @@ Operand<T> rows_of(const void* p, int64_t stride, int64_t rows, int64_t k) {
   return Operand<T>{(const T*)p, nullptr, stride, 0, rows, k, MASSIVE_ACT_NONE};
 }
 
-// Whether rows begin at multiples of 16 bytes (NULL counts as such).
-template <typename T>
-bool in_units(const void* p, int64_t stride) {
-  return !p || (aligned(p, 16) && stride * (int64_t)sizeof(T) % 16 == 0);
-}
-
-// Whether a call takes the form in which a block's waves share the reduction: for
-// few results, and in bf16 for a reduction long enough that one block's steps
-// last longer than that (us, few / tiles, graph: bf16 16 rows of 256 -> 1024
-// 7.8 / 6.6, 250 9.0 / 7.2; fp32 250 rows 12.1 / 22.7, 1000 33 / 24; 1000 rows of
-// 128 -> 256 10.7 / 13.7, 4000 27 / 14.5).
-template <typename T>
-bool gated_few(const massive_gated_args* a) {
-  return a->rows * round_up(a->n, 32) <= int64_t(1) << 18 && (sizeof(T) == 4 || a->k + a->k_second > 448);
-}
-
 template <typename T>
 int gated(const massive_gated_args* a, void* stream) {
   const char* what = "massive_gated";
@@ -228,95 +213,17 @@ int gated(const massive_gated_args* a, void* stream) {
   f.rows = a->rows;
   f.n = a->n;
   f.act = a->act;
-  if (!gated_few<T>(a)) {
-    const bool direct = in_units<T>(a->x, a->x_stride) && in_units<T>(a->x_second, a->x_second_stride) && in_units<T>(a->w, a->w_stride) &&
-                        (!a->x_second || a->k * sizeof(T) % 16 == 0);
+  if (!gated_few(a)) {
+    const bool direct = gated_direct(a);
     auto tile = [&](auto nb) {
       const int64_t tiles_n = cdiv(a->n, 32 * nb()), blocks = cdiv(a->rows, kTileSecond) * tiles_n;
       if (blocks > kMostBlocks) REFUSE("too many rows and columns for one call");
       return launch(what, direct ? k_gated_tile<T, nb(), true> : k_gated_tile<T, nb(), false>, blocks, kTileNT, 0, stream, f, (int)tiles_n, blocks);
     };
-    // narrow tiles until there are two rounds of wide ones for the chip (256 -> 1024 in bf16: 4000 rows 11.8 us wide, 10.8
-    // narrow, 16000 30.3 and 30.1, 110K 171 and 183)
-    return cdiv(a->rows, kTileSecond) * cdiv(a->n, 128) < 1024 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>());
+    return gated_narrow(a) ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>());
   }
   const int tiles_n = (int)cdiv(a->n, 32);
   return launch(what, k_gated_few<T>, cdiv(a->rows, 32) * tiles_n, kFewNT, 0, stream, f, tiles_n);
-}
-
-// dw's tiles (128 outputs of both halves; made on the way, 64 of each) and the
-// parts of its rows: as many blocks as the chip holds at a time, none of less
-// than eight steps of rows (four in fp32, whose steps last longer) where there
-// are more.
-struct GatedDwPlan {
-  int nb, second;
-  int64_t tiles_n, tiles_k, part, parts, floats;  // floats: of the parts, none of a single one
-};
-GatedDwPlan gated_dw_plan(const massive_gated_grads* a) {
-  GatedDwPlan p;
-  const int vector = 16 / size_of(a->type), step = kTileStepBytes / size_of(a->type);
-  p.second = (int)round_up(a->k, vector);
-  const int64_t cols = p.second + a->k_second, n = 2 * (int64_t)a->n;
-  p.nb = cols <= 128 ? 2 : 4;
-  p.tiles_n = cdiv(n, kTileSecond);
-  p.tiles_k = cdiv(cols, 64 * p.nb);
-  const int64_t most = std::max<int64_t>(1, cdiv(a->rows, (a->type == MASSIVE_F32 ? 4 : 8) * step));
-  p.part = std::max<int64_t>(1, round_up(cdiv(a->rows, std::min(most, std::max<int64_t>(1, 512 / (p.tiles_n * p.tiles_k)))), step));
-  p.parts = cdiv(a->rows, p.part);
-  p.floats = a->dw && p.parts > 1 ? p.parts * n * ((int64_t)a->k + a->k_second) : 0;
-  return p;
-}
-
-// dx's tiles, narrow ones where wide ones are less than a round for the chip, and
-// the parts of its reduction over dz's columns where there are few tiles. A step
-// takes a block about 0.4 us (bf16; fp32 1), and a part's values 8 bytes written
-// and read at ~4 TB/s; with the join's launch, 4 us, that says how many parts pay
-// (us of all gradients in bf16, parts / none: 16 rows of 256 -> 1024 20 / 42,
-// 1000 rows 50 / 56; with four parts wherever tiles leave room, 16K rows of 128 ->
-// 256 65, with none 36).
-struct GatedDxPlan {
-  int nb;
-  int64_t tiles_n, tiles, part, parts, floats;
-};
-GatedDxPlan gated_dx_plan(const massive_gated_grads* a) {
-  GatedDxPlan p;
-  const int64_t cols = (a->dx ? a->k : 0) + (a->dx_second ? a->k_second : 0), n = 2 * (int64_t)a->n, step = kTileStepBytes / size_of(a->type);
-  const int64_t row_tiles = cdiv(a->rows, kTileSecond), steps = cdiv(n, step);
-  p.nb = cols <= 128 || row_tiles * cdiv(cols, 256) < 512 ? 2 : 4;
-  p.tiles_n = std::max<int64_t>(1, cdiv(cols, 64 * p.nb));
-  p.tiles = row_tiles * p.tiles_n;
-  const double all = steps * (a->type == MASSIVE_F32 ? 1.0 : 0.4), each = 2e-6 * a->rows * cols;
-  int64_t parts = (int64_t)std::min(std::sqrt(all / std::max(each, 1e-9)), (p.nb == 2 ? 768.0 : 512.0) / std::max<int64_t>(1, p.tiles));
-  parts = std::max<int64_t>(1, std::min(parts, steps / 4));
-  if (all * (1 - 1.0 / parts) < 4 + parts * each) parts = 1;
-  p.part = round_up(cdiv(n, parts), step);
-  p.parts = cdiv(n, p.part);
-  p.floats = p.parts > 1 ? p.parts * a->rows * cols : 0;
-  return p;
-}
-
-// The backward pass's workspace: dz, the parts of db, those of dw or, later, of
-// dx. It has room for dz also where dw is all that is asked for and dz may never
-// be written: that hangs on where x lies, which its size does not.
-struct GatedPlan {
-  int64_t groups, part, parts, sums_at, dw_at, bytes;
-  bool in_units;  // sizes for which dz can be made on its way into dw; db is summed in that way's order then, by any way
-  GatedDwPlan dw;
-  GatedDxPlan dx;
-};
-GatedPlan gated_plan(const massive_gated_grads* a) {
-  GatedPlan p;
-  const int size = size_of(a->type), vector = 16 / size;
-  p.groups = cdiv(a->n, kGateUnits * vector);
-  p.part = std::max<int64_t>(1, cdiv(a->rows, std::max<int64_t>(1, std::min(cdiv(a->rows, 4 * kGateWays), 2048 / std::min<int64_t>(2048, p.groups)))));
-  p.parts = cdiv(a->rows, p.part);
-  p.dw = gated_dw_plan(a);
-  p.in_units = a->k % vector == 0 && a->k_second % vector == 0 && a->n >= vector && p.dw.tiles_k == 1;
-  p.sums_at = a->dx || a->dx_second || a->dw ? round_up(a->rows * 2 * a->n * size, 16) : 0;
-  p.dw_at = p.sums_at + (a->dbias ? round_up((p.in_units ? p.dw.parts : p.parts) * 2 * a->n * 4, 16) : 0);
-  p.dx = gated_dx_plan(a);
-  p.bytes = p.dw_at + std::max(p.dw.floats, p.dx.floats) * 4;
-  return p;
 }
 
 template <typename T>
@@ -343,17 +250,18 @@ int with_act_of(int act, F f) {
   }
 }
 
-// Adds up parts, by as many threads a value as fill the chip where there are
-// `values` of them (us, one / sixteen: 33 parts of 524K values 14-18 / 19; all
-// gradients with 250 parts of 8K 90 / 34).
+// Adds up parts, of which the sizes say that there are `values`.
 template <typename T>
 int gated_join(const GatedJoin<T>& j, int64_t values, void* stream) {
   auto ways = [&](auto w) {
     constexpr int kValues = kGateNT / w() * 4;
     return launch("massive_gated_backward", k_gated_join<T, w()>, cdiv(j.values[0], kValues) + cdiv(j.values[1], kValues), kGateNT, 0, stream, j);
   };
-  if (j.count <= 2 || values >= 1 << 19) return ways(std::integral_constant<int, 1>());
-  return values >= 1 << 17 ? ways(std::integral_constant<int, 4>()) : ways(std::integral_constant<int, 16>());
+  switch (gated_ways(j.count, values)) {
+    case 1: return ways(std::integral_constant<int, 1>());
+    case 4: return ways(std::integral_constant<int, 4>());
+    default: return ways(std::integral_constant<int, 16>());
+  }
 }
 
 // dz and db by themselves.
@@ -371,7 +279,6 @@ int gated_dz(const massive_gated_grads* a, const GatedPlan& p, char* workspace, 
 
 template <typename T>
 int gated_dx(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
-  constexpr int kV = 16 / sizeof(T);
   const GatedDxPlan& d = p.dx;
   const int n = 2 * a->n;
   LinearDx<T> f;
@@ -386,7 +293,7 @@ int gated_dx(const massive_gated_grads* a, const GatedPlan& p, char* workspace, 
   f.cols = k0 + k1;
   f.split = k0;
   float* parts = d.parts > 1 ? (float*)(workspace + p.dw_at) : nullptr;
-  const bool direct = n % kV == 0 && in_units<T>(f.w.p, f.w.stride) && f.cols % kV == 0;
+  const bool direct = gated_dx_direct(a);
   auto tile = [&](auto nb) {
     return launch("massive_gated_backward", direct ? k_gated_dx<T, nb(), true> : k_gated_dx<T, nb(), false>, d.tiles * d.parts, kTileNT, 0, stream, f, parts, d.part,
                   (int)d.tiles_n, d.tiles, d.tiles * d.parts);
@@ -427,10 +334,8 @@ int dw_join(const massive_gated_grads* a, const float* dw, const float* db, int6
 template <typename T>
 int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* workspace, void* stream) {
   const char* what = "massive_gated_backward";
-  constexpr int kV = 16 / sizeof(T);
   const bool dx = a->dx || a->dx_second;
-  const bool units = a->k % kV == 0 && a->k_second % kV == 0 && in_units<T>(a->x, a->x_stride) && in_units<T>(a->x_second, a->x_second_stride);
-  const bool made = a->dw && units && p.in_units, sums = !made && a->dbias && p.in_units;
+  const bool made = gated_dw_made(a, p), sums = !made && a->dbias && p.in_units;
   const GatedDwPlan& d = p.dw;
   const bool several = d.parts > 1;
   const int n = 2 * a->n;
@@ -467,7 +372,7 @@ int gated_backward(const massive_gated_grads* a, const GatedPlan& p, char* works
         return with_act_of(a->act, [&](auto act) {
           return launch(what, k_gated_dw_made<T, nb(), act()>, blocks, kTileNT, 0, stream, f, gates_of<T>(a, dx ? workspace : nullptr), blocks);
         });
-      return launch(what, units && n % kV == 0 ? k_gated_dw<T, nb(), true> : k_gated_dw<T, nb(), false>, blocks, kTileNT, 0, stream, f, blocks);
+      return launch(what, gated_dw_direct(a) ? k_gated_dw<T, nb(), true> : k_gated_dw<T, nb(), false>, blocks, kTileNT, 0, stream, f, blocks);
     };
     if (int rc = d.nb == 2 ? tile(std::integral_constant<int, 2>()) : tile(std::integral_constant<int, 4>())) return rc;
   }

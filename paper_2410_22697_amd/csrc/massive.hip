@@ -48,7 +48,7 @@ struct TimedRange {
   int group;
 };
 
-inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+using ms::cdiv;
 inline unsigned grid_for(int64_t n, int nt, int64_t cap = 16384) {
   int64_t g = cdiv(std::max<int64_t>(n, 1), nt);
   return (unsigned)std::min<int64_t>(std::max<int64_t>(g, 1), cap);

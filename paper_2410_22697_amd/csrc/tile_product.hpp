@@ -18,14 +18,13 @@
 // products, and L2 gives about 14 TB/s. The products alone, from LDS, take 68.
 #pragma once
 
+#include "gated_rules.hpp"
 #include "linear_kernels.hpp"
 #include "linear_weights.hpp"
 
 namespace ms {
 
 constexpr int kTileNT = 256;
-constexpr int kTileSecond = 128;  // columns of the second operand
-constexpr int kTileStepBytes = 64;
 
 // k of a step: four units of 16 bytes, two products.
 template <typename T>
