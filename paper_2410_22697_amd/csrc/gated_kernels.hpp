@@ -200,7 +200,8 @@ __global__ __launch_bounds__(kGateNT) void k_gated_dz(GatedDz<T> a) {
 }
 
 // dx = dz w: 128 rows by 64 NB columns a block, and of dz's columns as many as a
-// part has. parts: [parts][rows][cols] if there are several, else null.
+// part has. parts: [parts][rows][cols] if there are several, else null; of wide
+// tiles there are always enough for one part.
 // 110K x 256 -> 1024 bf16 168 to 180 us (690 TFLOP/s; 860 tiles where the chip
 // holds 512 at a time are two rounds), fp32 16391 x 200 -> 323 80 with the parts'
 // sum 11 more (95 in one part).
@@ -209,7 +210,8 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, float* p
   typedef TileAcross<T, 64 * NB> A;
   typedef TileAlong<T, kTileSecond> B;
   typedef TileTurn<T, 32 * NB> Turn;
-  constexpr int kTurns = 4 * TileTurn<float, 32 * NB>::kBytes, kLds = tile_lds<A, B>(DIRECT) > kTurns ? tile_lds<A, B>(DIRECT) : kTurns;
+  typedef TileTurn<float, 32 * NB> WideTurn;
+  constexpr int kTurns = 4 * (NB == 2 ? WideTurn::kBytes : Turn::kBytes), kLds = tile_lds<A, B>(DIRECT) > kTurns ? tile_lds<A, B>(DIRECT) : kTurns;
   __shared__ __align__(16) char lds[kLds];
   const int64_t block = tile_of_block(blockIdx.x, blocks), tile = block % tiles, p = block / tiles, from = p * part;
   const int64_t r0 = tile / tiles_n * kTileSecond;
@@ -231,27 +233,28 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dx(LinearDx<T> a, float* p
   else tile_product<T, NB>(weights, rows, segments, begin, lds, acc);
   const int wave = wave_uniform((int32_t)wave_id());
   const int c0 = n0 + wave % 2 * (32 * NB);
-  if (parts) {
-    typedef TileTurn<float, 32 * NB> WideTurn;
-    const WideTurn turn = {lds + wave * WideTurn::kBytes};
+  if constexpr (NB == 2) {
+    if (parts) {
+      const WideTurn turn = {lds + wave * WideTurn::kBytes};
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < 2; ++j) {
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
+        for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-          turn.in(32 * i, q, v);
-        }
-      const int64_t at = r0 + wave / 2 * 64 + 32 * j;
-      turn.units([&](int r, int c, cols_t<float, 4> v) {
-        if (at + r >= a.rows || c0 + c >= round_up_to<16 / (int)sizeof(T)>(a.cols)) return;
-        const int col = tile_column<T>(c0 + c, a.cols);
-        const float four[4] = {v[0], v[1], v[2], v[3]};
-        store_cols<float, 4, false>(parts + (p * a.rows + at + r) * a.cols + col, a.cols - col, four);
-      });
+          for (int q = 0; q < 4; ++q) {
+            const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            turn.in(32 * i, q, v);
+          }
+        const int64_t at = r0 + wave / 2 * 64 + 32 * j;
+        turn.units([&](int r, int c, cols_t<float, 4> v) {
+          if (at + r >= a.rows || c0 + c >= round_up_to<16 / (int)sizeof(T)>(a.cols)) return;
+          const int col = tile_column<T>(c0 + c, a.cols);
+          const float four[4] = {v[0], v[1], v[2], v[3]};
+          store_cols<float, 4, false>(parts + (p * a.rows + at + r) * a.cols + col, a.cols - col, four);
+        });
+      }
+      return;
     }
-    return;
   }
   const Turn turn = {lds + wave * Turn::kBytes};
 #pragma unroll

@@ -90,7 +90,7 @@ inline GatedDxPlan gated_dx_plan(const massive_gated_grads* a) {
   p.tiles_n = std::max<int64_t>(1, cdiv(cols, 64 * p.nb));
   p.tiles = row_tiles * p.tiles_n;
   const double all = steps * (a->type == MASSIVE_F32 ? 1.0 : 0.4), each = 2e-6 * a->rows * cols;
-  int64_t parts = (int64_t)std::min(std::sqrt(all / std::max(each, 1e-9)), (p.nb == 2 ? 768.0 : 512.0) / std::max<int64_t>(1, p.tiles));
+  int64_t parts = p.nb == 4 ? 1 : (int64_t)std::min(std::sqrt(all / std::max(each, 1e-9)), 768.0 / std::max<int64_t>(1, p.tiles));
   parts = std::max<int64_t>(1, std::min(parts, steps / 4));
   if (all * (1 - 1.0 / parts) < 4 + parts * each) parts = 1;
   p.part = round_up(cdiv(n, parts), step);
