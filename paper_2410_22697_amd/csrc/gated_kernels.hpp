@@ -41,9 +41,10 @@ __device__ __forceinline__ void with_act(int act, F f) {
 
 // Many rows: 128 rows by 32 NB outputs of both halves a block; a wave has 16 NB
 // outputs of the gate and the same of the other half.
-// Bound by the products' way from L2 to LDS, and by a tile's end, which has no
-// products beside it. 110K x 256 -> 1024 bf16 170 us (680 TFLOP/s; 118 of it in the
-// products), with pre 287; 16391 x 100 + 100 -> 323 fp32 70 (60 TFLOP/s of what is
+// 110K x 256 -> 1024 bf16 171 us (680 TFLOP/s): by the slope in k, 90 to 117 are the
+// loop (tile_product.hpp says what of), the others the begin and the end of tiles,
+// beside which a block neither loads nor multiplies; with pre, whose end stores
+// three times as much, 286. 16391 x 100 + 100 -> 323 fp32 70 (60 TFLOP/s of what is
 // asked for: 323 outputs take 384, two inputs of 100 take 224 of k, and 774 tiles
 // are a few more than the chip holds at a time).
 template <typename T, int NB, bool DIRECT>
@@ -367,7 +368,10 @@ __global__ __launch_bounds__(kTileNT, 2) void k_gated_dw(GatedDw<T> a, int64_t b
 // [dg | du] as an operand across k, made from dy and pre on its way to LDS: COLS
 // columns of dg and the same of du, a unit (or W of its columns) of both a thread
 // and step. It can leave dz behind, and each thread adds up its columns before
-// they are rounded.
+// they are rounded. In bf16 dg and du are rounded to it, as the matrix unit takes
+// them: that puts dx's and dw's error at 0.0023 of their size, where the results' own
+// rounding leaves 0.0017 (0.0017 too against products of the rounded dz, at 110K x
+// 256 -> 1024). The bits that it drops would be a second product each.
 template <typename T, int ACT, int COLS = 64, int W = 16 / sizeof(T)>
 struct TileGates {
   static constexpr int kCols = COLS, kV = 16 / sizeof(T), kUnits = COLS / W, kNT = kUnits * tile_step<T>(), kPitch = 2 * COLS * sizeof(T), kBytes = tile_step<T>() * kPitch;

@@ -29,9 +29,11 @@ inline bool in_units(const void* p, int64_t stride, int32_t type) {
 // ------------------------------------------------------------------- forward
 // Whether a call takes the form in which a block's waves share the reduction: for
 // few results, and in bf16 for a reduction long enough that one block's steps
-// last longer than that (us, few / tiles, graph: bf16 16 rows of 256 -> 1024
-// 7.8 / 6.6, 250 9.0 / 7.2; fp32 250 rows 12.1 / 22.7, 1000 33 / 24; 1000 rows of
-// 128 -> 256 10.7 / 13.7, 4000 27 / 14.5).
+// last longer than that. us in a graph, few / tiles: bf16, 16 rows -> 1024 by k:
+// 256 7.3 / 6.2, 448 8.3 / 8.2, 512 8.7 / 8.9, 1024 12.9 / 14.6, 2048 21 / 26 (250 rows
+// 8.3 / 6.5, 9.5 / 8.5, 9.7 / 9.3, 13.9 / 15.1, 22 / 26); fp32, k 128 8.7 / 12.3, 256
+// 9.9 / 21, 2048 50 / 144. At the limit of results, 250 rows of 256 -> 1024 fp32 11 / 22,
+// beyond it 1000 33 / 24 and 4000 of 128 -> 256 27 / 14.5.
 inline bool gated_few(const massive_gated_args* a) {
   return a->rows * round_up(a->n, 32) <= int64_t(1) << 18 && (a->type == MASSIVE_F32 || a->k + a->k_second > 448);
 }
@@ -51,7 +53,12 @@ inline bool gated_direct(const massive_gated_args* a) {
 // dw's tiles (128 outputs of both halves; made on the way, 64 of each) and the
 // parts of its rows: as many blocks as the chip holds at a time, none of less
 // than eight steps of rows (four in fp32, whose steps last longer) where there
-// are more.
+// are more. us of all gradients but dx. Narrow tiles / wide ones, 110K rows -> 1024
+// bf16: 96 columns 160 / 196, 128 166 / 199, 160 381 / 205 (dz can no longer be made on
+// its way); 2000 rows 20 / 26, 21 / 26, 31 / 28; fp32 27.5K 146 / 248, 151 / 250, 350 / 252.
+// Least steps 2, 4, 8, 16: bf16 1000 x 256 -> 1024 33, 28, 27, 31, 4000 36, 35, 32,
+// 35, 2000 x 128 -> 128 14, 14, 17, 22; fp32 1000 x 256 -> 1024 38, 35, 41, 53, 2000 x
+// 128 -> 128 18, 17, 22, 31.
 struct GatedDwPlan {
   int nb, second;
   int64_t tiles_n, tiles_k, part, parts, floats;  // floats: of the parts, none of a single one
@@ -71,13 +78,17 @@ inline GatedDwPlan gated_dw_plan(const massive_gated_grads* a) {
   return p;
 }
 
-// dx's tiles, narrow ones where wide ones are less than a round for the chip, and
+// dx's tiles, narrow ones where wide ones are less than a round for the chip (us of
+// dz and dx, narrow / wide, -> 1024 in bf16 and 512 in fp32: 256 columns, 16K rows
+// 58 / 69, 48K 176 / 177, 64K 231 / 218, 110K 372 / 362; 512 columns, 32K 148 / 137, 110K
+// 490 / 458; 128 columns, 110K 343 / 357; fp32 256, 32K 196 / 198, 64K 396 / 384), and
 // the parts of its reduction over dz's columns where there are few tiles. A step
 // takes a block about 0.4 us (bf16; fp32 1), and a part's values 8 bytes written
 // and read at ~4 TB/s; with the join's launch, 4 us, that says how many parts pay
 // (us of all gradients in bf16, parts / none: 16 rows of 256 -> 1024 20 / 42,
 // 1000 rows 50 / 56; with four parts wherever tiles leave room, 16K rows of 128 ->
-// 256 65, with none 36).
+// 256 65, with none 36), up to 768 blocks (at most 512, 768, 1024: fp32 4000 x 512 ->
+// 2048 174, 179, 201, 16391 x 200 -> 323 112, 104, 104).
 struct GatedDxPlan {
   int nb;
   int64_t tiles_n, tiles, part, parts, floats;
@@ -138,7 +149,9 @@ inline bool gated_dx_direct(const massive_gated_grads* a) {
 
 // Threads a value that add up `count` parts, as many as fill the chip where there
 // are `values` of them (us, one / sixteen: 33 parts of 524K values 14-18 / 19; all
-// gradients with 250 parts of 8K 90 / 34).
+// gradients with 250 parts of 8K 90 / 34; one / four / sixteen, all but dx in bf16:
+// 110K x 64 -> 512, 65K values 95 / 87 / 85, x 128, 131K 102 / 94 / 94, x 256, 262K 127 / 122 /
+// 124, 20K x 160, 164K 48 / 39 / 41, 4000 x 256 -> 1024, 524K 32 / 32 / 33).
 inline int gated_ways(int64_t count, int64_t values) { return count <= 2 || values >= 1 << 19 ? 1 : values >= 1 << 17 ? 4 : 16; }
 
 }  // namespace ms

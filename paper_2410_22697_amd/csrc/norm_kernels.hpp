@@ -11,8 +11,17 @@
 //
 // Measured: 242K x 256 bf16 41 us (6.0 TB/s of x and y), with the residual and the
 // sum 77 (6.4), the same to 8 bits 76 (5.7); gradients 71 (5.2), 93 with ds; 854K x
-// 100 fp32 120 (5.7), bf16 75 (4.6). A long row keeps a block waiting, of which a CU
-// holds few: 30K x 5000 bf16 162 (3.7), gradients 312 (2.9).
+// 100 fp32 120 (5.7), bf16 75 (4.6).
+// Packed rows that are read and written in less are bound by the vector unit, which
+// their codes keep busy all the time (36 instructions a value: the normed values are
+// made once for their ends and once for the codes): 242K x 256 to 4 bits 56, 854K x
+// 100 to 8 bits 91 (units of 8 columns, of which such a row leaves a lane's half
+// and three lanes of sixteen empty).
+// A long row keeps a block waiting, of which a CU holds one or two, with nothing of
+// the next row asked for: 30K x 5000 bf16 166 (3.6; waves wait for three quarters
+// of their time, the vector unit is busy for a third of it), gradients 312 to 327
+// (2.8). The gradients of columns beyond the registers (8192 in bf16) also read,
+// add to and write their part of dw in memory for every row.
 #pragma once
 
 #include "common.hpp"

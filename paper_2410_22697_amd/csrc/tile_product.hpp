@@ -12,10 +12,14 @@
 // lane ends up with four neighbours of the first at a time, for one of the
 // second.
 //
-// Measured: rows along k, 110K by 2048 outputs in bf16, 118 us for each 256 of k
-// (980 TFLOP/s; through registers 130) beside what begins and ends a tile. The
-// loads alone take 99 of it: a tile of 256 by 128 reads a byte for each 85
-// products, and L2 gives about 14 TB/s. The products alone, from LDS, take 68.
+// Measured: rows along k, 110K by 2048 outputs in bf16, us for each 256 of k from
+// 512 to 1024, beside what begins and ends a tile: 108 to 117 (1 PFLOP/s; through
+// registers 128; fp32 at 137 TFLOP/s). Parts of the loop in turn, on one card
+// where the whole was 114: without the LDS reads 94, without the loads 76, the
+// products alone 46, the loads alone 87 to 105 (a tile of 256 by 128 reads a byte
+// for each 43 products, so that is 13 to 15 TB/s from L2). The loads are the
+// longest part and the LDS reads, for which the loop's waves wait too, come on top
+// of them: neither alone is what bounds it.
 #pragma once
 
 #include "gated_rules.hpp"
