@@ -31,7 +31,8 @@ inline bool in_units(const void* p, int64_t stride, int32_t type) {
 // few results, and in bf16 for a reduction long enough that one block's steps
 // last longer than that. us in a graph, few / tiles: bf16, 16 rows -> 1024 by k:
 // 256 7.3 / 6.2, 448 8.3 / 8.2, 512 8.7 / 8.9, 1024 12.9 / 14.6, 2048 21 / 26 (250 rows
-// 8.3 / 6.5, 9.5 / 8.5, 9.7 / 9.3, 13.9 / 15.1, 22 / 26); fp32, k 128 8.7 / 12.3, 256
+// 8.3 / 6.5, 9.5 / 8.5, 9.7 / 9.3, 13.9 / 15.1, 22 / 26; the rule's worst, 1000 rows
+// of 2048 -> 256, 36 / 26); fp32, k 128 8.7 / 12.3, 256
 // 9.9 / 21, 2048 50 / 144. At the limit of results, 250 rows of 256 -> 1024 fp32 11 / 22,
 // beyond it 1000 33 / 24 and 4000 of 128 -> 256 27 / 14.5.
 inline bool gated_few(const massive_gated_args* a) {
